@@ -477,6 +477,127 @@ int sun_prefill(sun_kv_pool* pool, const sun_weights* weights, int n_tokens, con
                 float* logits_out, int32_t* next_token_out, void* workspace, size_t workspace_bytes,
                 void* stream, unsigned flags);
 
+/* ------------------------------------------------------------------ 8-bit cache */
+
+/*
+ * A paged pool that holds keys and values in 8 bits, for callers that compute q, k and v themselves: half the bytes of
+ * sun_kv_pool, so twice the requests in the same memory and close to half the time of an attention that is bound by reading
+ * them.  A cached vector y (head_dim values of one position and KV head) is stored as e4m3 codes and one power of two of its
+ * own: e is the smallest integer >= -100 with max |y| <= 448 * 2^e over its finite values, code = y * 2^-e rounded to the
+ * nearest e4m3 number (ties to even; not-a-number for a y that is not finite), scale byte = e + 127,
+ * value = code * 2^(scale byte - 127).  Every vector finds its own power when it is appended, so caches of different
+ * source models share a pool without calibration.
+ * Byte offsets into the pool:
+ *   K(layer,page,head,token,dim) = k_off + layer*k_layer + page*k_page + head*k_head + token*k_token + dim*k_dim, V with v_,
+ *   scale of K(layer,page,head,token) = ks_off + layer*s_layer + page*s_page + head*s_head + token, of V with vs_off.
+ * K is [token][dim], V [dim][token] inside a (layer, page, head) block, as in sun_kv_layout.
+ */
+typedef struct sun_kv8_layout {
+    int64_t n_pages;
+    int32_t page_tokens, reserved;
+    int64_t k_off, k_layer, k_page, k_head, k_token, k_dim;
+    int64_t v_off, v_layer, v_page, v_head, v_token, v_dim;
+    int64_t ks_off, vs_off, s_layer, s_page, s_head;
+    int64_t total_bytes;
+} sun_kv8_layout;
+
+typedef struct sun_kv8_pool sun_kv8_pool;
+
+/* Bytes of device memory an 8-bit pool of n_pages pages needs. */
+size_t sun_kv8_pool_bytes(const sun_model_cfg* cfg, int64_t n_pages, int page_tokens);
+
+/*
+ * Wraps caller-owned device memory (256-byte aligned, borrowed until destroy) as an 8-bit pool; bytes / page size gives
+ * n_pages.  Of cfg the layer count, the heads and the rotation and head-norm options are used.  page_tokens must be 16.
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE, SUN_ERR_POOL_SIZE.
+ */
+int sun_kv8_pool_create(const sun_model_cfg* cfg, void* dev_mem, size_t bytes, int page_tokens, sun_kv8_pool** out);
+int sun_kv8_pool_layout(const sun_kv8_pool* pool, sun_kv8_layout* out);
+void sun_kv8_pool_destroy(sun_kv8_pool* pool);
+
+/*
+ * Appends keys and values of `rows` new positions of up to n_requests requests to one layer, the rotation applied on the
+ * way: one row per request in a decode step, any number per request in a prefill.  Enqueued on `stream`.
+ *   dtype      of q, k, v, the gains and q_out: SUN_F32 or SUN_BF16
+ *   q          dev [rows, Hq*d], row stride ld_q elements, or NULL with q_out NULL: keys and values alone
+ *   k, v       dev [rows, Hkv*d], row strides ld_k, ld_v: not rotated, biases added
+ *   positions  dev int32 [rows]: position of the row in its request; < 0: a padding row, which reads and writes nothing
+ *   requests   dev int32 [rows]: row of page_tables, in [0, n_requests)
+ *   page_tables dev int32 [n_requests, max_pages]
+ *   q_norm, k_norm  dev [d]: gains of the head norm (RMSNorm over head_dim, eps = rms_eps, before the rotation); required
+ *              if cfg.qk_norm (q_norm only with q), NULL if not
+ *   q_out      dev [rows, Hq*d], contiguous: q, normed and rotated; may be q itself where ld_q = Hq*d
+ * Angles are computed in 64 bits from cfg.rope_* and their cosines and sines rounded to 32; a key is computed in 64 bits and
+ * rounded to 32 once before it is rounded to the cache's 8.  A row whose position has no page (beyond the table, or an entry outside
+ * the pool, or a request outside [0, n_requests)) leaves the pool as it is; its q_out is written.  Only the entries of the
+ * given positions are written.  No two rows may name the same position of the same page, and a position must not be
+ * read by work of another stream meanwhile.
+ * With SUN_VALIDATE positions, requests and tables are copied to the host (synchronises) and checked.
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, rows < 1, n_requests < 1, max_pages outside [1, 2^26], dtype, a pointer that is not
+ * 16-byte aligned, a row stride that is shorter than a row or no multiple of 16 bytes, q and q_out not given together); under
+ * SUN_VALIDATE also SUN_ERR_SEQ_LEN (position beyond the table, two rows at one place) and SUN_ERR_PAGE_RANGE (request
+ * or page).
+ */
+int sun_kv8_append(sun_kv8_pool* pool, int layer, int rows, int dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                   const void* v, int64_t ld_v, const int32_t* positions, const int32_t* requests,
+                   const int32_t* page_tables, int n_requests, int max_pages, const void* q_norm, const void* k_norm,
+                   void* q_out, void* stream, unsigned flags);
+
+/* Bytes of device workspace sun_kv8_attention needs for up to `batch` requests with max_pages table columns, any window. */
+size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages);
+
+/*
+ * Attention of one new token per request over one layer of an 8-bit pool, split over each cache's length and joined:
+ * softmax(q K^T / sqrt(d)) V, query head h reading KV head h / (Hq/Hkv).  Enqueued on `stream`; reads the pool only.
+ *   dtype      of q and out: SUN_F32 or SUN_BF16
+ *   q          dev [batch, Hq*d], rotated (sun_kv8_append's q_out)
+ *   n_tokens   dev int32 [batch]: positions 0 .. n_tokens[i] - 1 are cached; counts are cut to [0, max_pages*16]
+ *   window     > 0: only the last `window` of them are attended to, and table entries of pages in front of them are not read as
+ *              pages (they may be -1); 0: all
+ *   out        dev [batch, Hq*d]; a request without a token gets zeros
+ * Tokens of a page outside the pool are left out.  A request's result does not depend on the others of the batch.
+ * Cached numbers enter exactly; weights of the softmax carry 16 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
+ * Under SUN_VALIDATE counts and tables are copied to the host (synchronises) and checked.
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, batch outside [1, 1024], max_pages outside [1, 2^26], window < 0, dtype, q or out not
+ * 16-byte aligned), SUN_ERR_WORKSPACE (too small or not 256-byte aligned); under SUN_VALIDATE also SUN_ERR_SEQ_LEN and SUN_ERR_PAGE_RANGE.
+ */
+int sun_kv8_attention(const sun_kv8_pool* pool, int layer, int batch, int dtype, const void* q, const int32_t* page_tables,
+                      int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace, size_t workspace_bytes,
+                      void* stream, unsigned flags);
+
+/* ------------------------------------------------------------------ microscaled 4-bit floats */
+
+/*
+ * The 4-bit format of the Open Compute Project's microscaling formats 1.0 (MXFP4), beside the integer format of
+ * sun_quantize_w4: every 32 consecutive columns of a row share a scale byte s, and
+ *   W[n, k] = e2m1(code[n, k]) * 2^(s[n, k/32] - 127),  e2m1 = 0, 0.5, 1, 1.5, 2, 3, 4, 6 for codes 0 to 7, negative for 8 to 15.
+ * codes [rows, cols/2] bytes (low half = even column), scales [rows, cols/32] bytes; scale byte 255: the block is
+ * not-a-number.  cols must be a multiple of 32.  Matrices are contiguous, codes and dense arrays 16-byte aligned.
+ *
+ * sun_mx4_quantize: w dev dense, dtype SUN_F32 or SUN_BF16 -> codes, scales.  s = max(floor(log2 max|w|) - 2, -127) + 127 over
+ * the block, code = w * 2^(127 - s) rounded to the nearest (ties to the even code), at most 6; a block with a value that is
+ * not finite gets scale byte 255 and codes 0, one of zeros scale byte 0.
+ * sun_mx4_dequantize: the values, exact in either type.
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (rows < 1, cols < 32 or no multiple of 32, dtype, alignment).
+ */
+int sun_mx4_quantize(const void* w, int dtype, int rows, int cols, void* codes, void* scales, void* stream);
+int sun_mx4_dequantize(const void* codes, const void* scales, int rows, int cols, int dtype, void* out, void* stream);
+
+/* Bytes of device workspace sun_mx4_linear needs for a matrix [N, K] and up to `rows` rows, any types. */
+size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows);
+
+/*
+ * out[b, n] = sum_k W[n, k] x[b, k] with W [N, K] in the format above, from one row to a prefill block.  Enqueued on `stream`.
+ *   x    dev [rows, K], type x_dtype, row stride ld_x elements; out dev [rows, N], type out_dtype, row stride ld_out
+ * Weights and activations enter the matrix cores exactly (32-bit activations as three bf16 planes), sums are in 32 bits; values
+ * below the normal numbers of bf16 (2^-126) may count as zero.  A row's result depends on N, K, the row count and the types, not on
+ * the other rows' values.  out must not overlap x or the matrix.
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (N, rows < 1, K < 32 or no multiple of 32, a type, codes or x not 16-byte aligned, ld_x < K or no
+ * multiple of 16 bytes, ld_out < N, out not aligned to its type), SUN_ERR_WORKSPACE (too small or not 256-byte aligned).
+ */
+int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x,
+                   void* out, int out_dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ single operations */
 
 /*

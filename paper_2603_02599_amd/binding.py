@@ -36,6 +36,9 @@ EXPORTS = [
     "sun_prefill_workspace_bytes", "sun_prefill", "sun_serve_workspace_bytes", "sun_decode_serve",
     "sun_paged_attention", "sun_paged_attention_static", "sun_paged_attention_static_bytes",
     "sun_paged_attention_static_limit", "sun_linear",
+    "sun_kv8_pool_bytes", "sun_kv8_pool_create", "sun_kv8_pool_layout", "sun_kv8_pool_destroy", "sun_kv8_append",
+    "sun_kv8_attention", "sun_kv8_attention_workspace_bytes",
+    "sun_mx4_quantize", "sun_mx4_dequantize", "sun_mx4_linear", "sun_mx4_linear_workspace_bytes",
     "sun_hbm_read_probe", "sun_profile_read", "sun_profile_reset", "sun_last_error", "sun_version",
 ]
 
@@ -67,6 +70,13 @@ class KvLayout(C.Structure):
                 ("k_token", C.c_int64), ("k_dim", C.c_int64),
                 ("v_off", C.c_int64), ("v_layer", C.c_int64), ("v_page", C.c_int64), ("v_head", C.c_int64),
                 ("v_token", C.c_int64), ("v_dim", C.c_int64), ("total_elems", C.c_int64)]
+
+
+class Kv8Layout(C.Structure):
+    _fields_ = [("n_pages", C.c_int64), ("page_tokens", C.c_int32), ("reserved", C.c_int32)] + \
+               [(n, C.c_int64) for n in ("k_off", "k_layer", "k_page", "k_head", "k_token", "k_dim",
+                                         "v_off", "v_layer", "v_page", "v_head", "v_token", "v_dim",
+                                         "ks_off", "vs_off", "s_layer", "s_page", "s_head", "total_bytes")]
 
 
 class WeightPtrs(C.Structure):
@@ -104,7 +114,8 @@ def lib() -> C.CDLL:
         L.sun_version.restype = C.c_char_p
         for f in ("sun_kv_pool_bytes", "sun_weights_pack_bytes", "sun_qweights_pack_bytes", "sun_workspace_bytes",
                   "sun_prefill_workspace_bytes", "sun_serve_workspace_bytes", "sun_paged_attention_static_bytes",
-                  "sun_paged_attention_static_limit"):
+                  "sun_paged_attention_static_limit", "sun_kv8_pool_bytes", "sun_kv8_attention_workspace_bytes",
+                  "sun_mx4_linear_workspace_bytes"):
             getattr(L, f).restype = C.c_size_t
         L.sun_kv_pool_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int64, C.c_int]
         L.sun_kv_pool_create.argtypes = [C.POINTER(ModelCfg), C.c_void_p, C.c_size_t, C.c_int, C.c_int,
@@ -147,6 +158,22 @@ def lib() -> C.CDLL:
         L.sun_paged_attention_static_limit.argtypes = []
         L.sun_linear.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_size_t, C.c_void_p]
+        L.sun_kv8_pool_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int64, C.c_int]
+        L.sun_kv8_pool_create.argtypes = [C.POINTER(ModelCfg), C.c_void_p, C.c_size_t, C.c_int, C.POINTER(C.c_void_p)]
+        L.sun_kv8_pool_layout.argtypes = [C.c_void_p, C.POINTER(Kv8Layout)]
+        L.sun_kv8_pool_destroy.argtypes = [C.c_void_p]
+        L.sun_kv8_pool_destroy.restype = None
+        L.sun_kv8_append.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                     C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint]
+        L.sun_kv8_attention_workspace_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int, C.c_int]
+        L.sun_kv8_attention.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
+                                        C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint]
+        L.sun_mx4_quantize.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.sun_mx4_dequantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
+        L.sun_mx4_linear_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+        L.sun_mx4_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int64,
+                                     C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
         L.sun_hbm_read_probe.argtypes = [C.c_void_p, C.c_size_t, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
         L.sun_profile_read.argtypes = [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.sun_profile_reset.restype = None
@@ -472,6 +499,171 @@ def sun_paged_attention_static_limit() -> int:
 def sun_linear(weights, layer: int, mat: int, x, out, workspace, stream=None):
     _check(lib().sun_linear(weights.handle, layer, mat, x.shape[0], _p(x), _p(out), _p(workspace),
                             workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+# ------------------------------------------------------------------ 8-bit cache, microscaled 4-bit floats
+# Tensors of these calls live on one GPU, which need not be the current one: the work goes to that GPU's current stream unless
+# `stream` names another.  Wrong types, shapes and strides raise SunError (SUN_ERR_SHAPE) before anything is enqueued.
+_DTYPES = {torch.float32: SUN_F32, torch.bfloat16: SUN_BF16}
+
+
+def _refuse(message: str):
+    raise SunError(2, message)
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _DTYPES:
+        _refuse(f"{name} must be float32 or bfloat16, is {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _want(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape, rows: bool = False) -> int:
+    """The address of a tensor of this type and shape on the device of `like`: contiguous, or with rows any stride between rows."""
+    if t.dtype is not dtype or tuple(t.shape) != shape:
+        _refuse(f"{name} must be {dtype} {shape}, is {t.dtype} {tuple(t.shape)}")
+    if t.device != like.device:
+        _refuse(f"{name} is on {t.device}, not on {like.device}")
+    if not t.is_contiguous() and not (rows and t.stride(1) == 1):
+        _refuse(f"{name} must be contiguous" + (" within a row" if rows else ""))
+    return t.data_ptr()
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _call(like: torch.Tensor, stream, fn, *args):
+    """fn(*args, stream) with the GPU of `like` current."""
+    if like.device.type != "cuda":
+        _refuse(f"tensors must be on a GPU, are on {like.device}")
+    if like.device.index == torch.cuda.current_device():
+        return _check(fn(*args, _stream(stream)))
+    with torch.cuda.device(like.device):
+        return _check(fn(*args, _stream(stream)))
+
+
+def sun_kv8_pool_bytes(cfg: ModelCfg, n_pages: int, page_tokens: int = 16) -> int:
+    return int(lib().sun_kv8_pool_bytes(C.byref(cfg), n_pages, page_tokens))
+
+
+class Kv8Pool:
+    """Owner of the handle of an 8-bit pool; `mem` (a torch uint8 tensor on the GPU) is borrowed and kept alive."""
+
+    def __init__(self, handle: int, mem: torch.Tensor, cfg: ModelCfg):
+        self.handle, self.mem, self.cfg = handle, mem, cfg
+
+    def layout(self) -> Kv8Layout:
+        return sun_kv8_pool_layout(self)
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.sun_kv8_pool_destroy(self.handle)
+            self.handle = None
+
+
+def sun_kv8_pool_create(cfg: ModelCfg, mem: torch.Tensor, page_tokens: int = 16) -> Kv8Pool:
+    out = C.c_void_p()
+    nbytes = mem.numel() * mem.element_size() if isinstance(mem, torch.Tensor) else 0
+    _check(lib().sun_kv8_pool_create(C.byref(cfg), _p(mem), nbytes, page_tokens, C.byref(out)))
+    kept = ModelCfg()
+    C.pointer(kept)[0] = cfg
+    return Kv8Pool(out.value, mem, kept)
+
+
+def sun_kv8_pool_layout(pool: Kv8Pool) -> Kv8Layout:
+    lay = Kv8Layout()
+    _check(lib().sun_kv8_pool_layout(pool.handle, C.byref(lay)))
+    return lay
+
+
+def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page_tables, q_out, q_norm=None, k_norm=None,
+                   stream=None, flags: int = 0):
+    """k, v [rows, Hkv*d] (and q [rows, Hq*d], or None with q_out None), rows at any stride; positions, requests int32 [rows];
+    page_tables int32 [n_requests, max_pages]; gains [d] of the same type as q, k and v."""
+    c, like = pool.cfg, pool.mem
+    dt, rows = _dtype(k, "k"), k.shape[0]
+    kd, qd = c.n_kv_heads * c.head_dim, c.n_q_heads * c.head_dim
+    if page_tables.dim() != 2:
+        _refuse("page_tables must be [n_requests, max_pages]")
+    n_requests, max_pages = page_tables.shape
+    pk, pv = _want("k", k, like, k.dtype, (rows, kd), True), _want("v", v, like, k.dtype, (rows, kd), True)
+    pq = po = None
+    if q is not None:
+        pq = _want("q", q, like, k.dtype, (rows, qd), True)
+    if q_out is not None:
+        po = _want("q_out", q_out, like, k.dtype, (rows, qd))
+    gains = [None if g is None else _want(n, g, like, k.dtype, (c.head_dim,)) for n, g in (("q_norm", q_norm), ("k_norm", k_norm))]
+    i32 = torch.int32
+    at = (_want("positions", positions, like, i32, (rows,)), _want("requests", requests, like, i32, (rows,)),
+          _want("page_tables", page_tables, like, i32, (n_requests, max_pages)))
+    _call(like, stream, lambda st: lib().sun_kv8_append(
+        pool.handle, layer, rows, dt, pq, _row_stride(q) if q is not None else 0, pk, _row_stride(k), pv, _row_stride(v), *at,
+        n_requests, max_pages, *gains, po, st, flags))
+
+
+def sun_kv8_attention_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int) -> int:
+    return int(lib().sun_kv8_attention_workspace_bytes(C.byref(cfg), batch, max_pages))
+
+
+def _workspace(t: torch.Tensor, like: torch.Tensor):
+    if t.device != like.device or not t.is_contiguous():
+        _refuse(f"workspace must be contiguous and on {like.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, workspace, window: int = 0, stream=None,
+                      flags: int = 0):
+    """q, out [batch, Hq*d]; page_tables int32 [batch, max_pages]; n_tokens int32 [batch]."""
+    c, like = pool.cfg, pool.mem
+    dt, qd = _dtype(q, "q"), c.n_q_heads * c.head_dim
+    if page_tables.dim() != 2:
+        _refuse("page_tables must be [batch, max_pages]")
+    batch, max_pages = page_tables.shape
+    args = (pool.handle, layer, batch, dt, _want("q", q, like, q.dtype, (batch, qd)),
+            _want("page_tables", page_tables, like, torch.int32, (batch, max_pages)), max_pages,
+            _want("n_tokens", n_tokens, like, torch.int32, (batch,)), window, _want("out", out, like, q.dtype, (batch, qd)),
+            *_workspace(workspace, like))
+    _call(like, stream, lambda st: lib().sun_kv8_attention(*args, st, flags))
+
+
+def sun_mx4_quantize(w: torch.Tensor, stream=None):
+    """Returns (codes uint8 [rows, cols/2], scales uint8 [rows, cols/32])."""
+    if w.dim() != 2 or w.shape[1] % 32:
+        _refuse("w must be [rows, cols], cols a multiple of 32")
+    rows, cols = w.shape
+    dt, src = _dtype(w, "w"), _want("w", w, w, w.dtype, (rows, cols))
+    codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
+    scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
+    _call(w, stream, lib().sun_mx4_quantize, src, dt, rows, cols, codes.data_ptr(), scales.data_ptr())
+    return codes, scales
+
+
+def _mx4(codes: torch.Tensor, scales: torch.Tensor, like: torch.Tensor):
+    if codes.dim() != 2:
+        _refuse("codes must be [rows, cols/2]")
+    n, k = codes.shape[0], codes.shape[1] * 2
+    return (_want("codes", codes, like, torch.uint8, (n, k // 2)), _want("scales", scales, like, torch.uint8, (n, k // 32)), n, k)
+
+
+def sun_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
+    """The values [rows, cols], float32 or bfloat16."""
+    pc, ps, n, k = _mx4(codes, scales, codes)
+    out = torch.empty((n, k), dtype=dtype, device=codes.device)
+    _call(codes, stream, lib().sun_mx4_dequantize, pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr())
+    return out
+
+
+def sun_mx4_linear_workspace_bytes(N: int, K: int, rows: int) -> int:
+    return int(lib().sun_mx4_linear_workspace_bytes(N, K, rows))
+
+
+def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):
+    """out [rows, N] = x [rows, K] W^T; x and out float32 or bfloat16 each, rows at any stride."""
+    pc, ps, n, k = _mx4(codes, scales, codes)
+    rows = x.shape[0]
+    px, po = _want("x", x, codes, x.dtype, (rows, k), True), _want("out", out, codes, out.dtype, (rows, n), True)
+    _call(codes, stream, lib().sun_mx4_linear, pc, ps, n, k, rows, px, _dtype(x, "x"), _row_stride(x), po, _dtype(out, "out"),
+          _row_stride(out), *_workspace(workspace, codes))
 
 
 def sun_hbm_read_probe(src, block_bytes: int, perm, workgroups: int, sink, streaming_loads: bool = False, stream=None):

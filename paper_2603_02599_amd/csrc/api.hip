@@ -1436,4 +1436,202 @@ int sun_linear(const sun_weights* weights_, int layer, int mat, int batch, const
     return SUN_OK;
 }
 
+// ---------------------------------------------------------------- 8-bit cache
+static sun_kv8_layout make_kv8_layout(const sun_model_cfg& c, int64_t n_pages) {
+    sun_kv8_layout L{};
+    const int64_t blk = (int64_t)kPageTokens * c.head_dim;  // codes of one (page, head) block of K or of V
+    L.n_pages = n_pages;
+    L.page_tokens = kPageTokens;
+    L.k_page = L.v_page = 2 * c.n_kv_heads * blk;
+    L.k_layer = L.v_layer = n_pages * L.k_page;
+    L.k_head = L.v_head = blk;
+    L.k_token = c.head_dim;
+    L.k_dim = 1;
+    L.v_token = 1;
+    L.v_dim = kPageTokens;
+    L.v_off = c.n_kv_heads * blk;
+    L.ks_off = (int64_t)c.n_layers * L.k_layer;  // the scales of all layers behind all codes, which keeps the codes' blocks on cache lines
+    L.s_head = kPageTokens;
+    L.s_page = 2 * c.n_kv_heads * kPageTokens;
+    L.s_layer = n_pages * L.s_page;
+    L.vs_off = L.ks_off + c.n_kv_heads * kPageTokens;
+    L.total_bytes = L.ks_off + (int64_t)c.n_layers * L.s_layer;
+    return L;
+}
+
+constexpr int kKv8MaxPages = 1 << 26;  // table columns: positions fit 31 bits
+
+size_t sun_kv8_pool_bytes(const sun_model_cfg* cfg, int64_t n_pages, int page_tokens) {
+    if (!cfg || n_pages < 0 || page_tokens != kPageTokens) return 0;
+    return (size_t)make_kv8_layout(*cfg, n_pages).total_bytes;
+}
+
+int sun_kv8_pool_create(const sun_model_cfg* cfg, void* dev_mem, size_t bytes, int page_tokens, sun_kv8_pool** out) {
+    if (!out) return fail(SUN_ERR_NULL, "out is NULL");
+    *out = nullptr;
+    if (int rc = check_cfg(cfg)) return rc;
+    if (!dev_mem) return fail(SUN_ERR_NULL, "pool memory is NULL");
+    if (page_tokens != kPageTokens) return fail(SUN_ERR_SHAPE, "page_tokens must be %d", kPageTokens);
+    if ((uintptr_t)dev_mem % 256) return fail(SUN_ERR_POOL_SIZE, "pool memory must be 256-byte aligned");
+    const size_t page_bytes = sun_kv8_pool_bytes(cfg, 1, page_tokens);
+    const int64_t n_pages = (int64_t)(bytes / page_bytes);
+    if (n_pages < 1) return fail(SUN_ERR_POOL_SIZE, "pool of %zu bytes holds no page of %zu bytes", bytes, page_bytes);
+    if (n_pages > 0x7fffffff) return fail(SUN_ERR_POOL_SIZE, "too many pages");
+    Kv8Pool* p = new (std::nothrow) Kv8Pool();
+    if (!p) return fail(SUN_ERR_NULL, "out of host memory");
+    p->cfg = *cfg;
+    p->base = (uint8_t*)dev_mem;
+    p->lay = make_kv8_layout(*cfg, n_pages);
+    *out = (sun_kv8_pool*)p;
+    return SUN_OK;
+}
+
+int sun_kv8_pool_layout(const sun_kv8_pool* pool, sun_kv8_layout* out) {
+    if (!pool || !out) return fail(SUN_ERR_NULL, "NULL argument");
+    *out = ((const Kv8Pool*)pool)->lay;
+    return SUN_OK;
+}
+
+void sun_kv8_pool_destroy(sun_kv8_pool* pool) { delete (Kv8Pool*)pool; }
+
+static bool is_dtype(int dtype) { return dtype == SUN_F32 || dtype == SUN_BF16; }
+static int dtype_bytes(int dtype) { return dtype == SUN_F32 ? 4 : 2; }
+
+static int validate_kv8_rows(const Kv8Pool& pool, const Kv8Rows& r, hipStream_t st) {
+    std::vector<int32_t> pos((size_t)r.rows), req((size_t)r.rows), tab((size_t)r.n_requests * r.max_pages);
+    SUN_HIP_CHECK(hipMemcpyAsync(pos.data(), r.positions, pos.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipMemcpyAsync(req.data(), r.requests, req.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipMemcpyAsync(tab.data(), r.page_tables, tab.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipStreamSynchronize(st));
+    std::vector<int64_t> places;
+    for (int i = 0; i < r.rows; ++i) {
+        if (pos[i] < 0) continue;
+        if (req[i] < 0 || req[i] >= r.n_requests)
+            return fail(SUN_ERR_PAGE_RANGE, "row %d: request %d outside [0, %d)", i, req[i], r.n_requests);
+        if (pos[i] / kPageTokens >= r.max_pages)
+            return fail(SUN_ERR_SEQ_LEN, "row %d: position %d beyond the table's %d pages", i, pos[i], r.max_pages);
+        const int32_t page = tab[(size_t)req[i] * r.max_pages + pos[i] / kPageTokens];
+        if (page < 0 || page >= pool.lay.n_pages)
+            return fail(SUN_ERR_PAGE_RANGE, "row %d: page %d outside [0, %lld)", i, page, (long long)pool.lay.n_pages);
+        places.push_back((int64_t)page * kPageTokens + pos[i] % kPageTokens);
+    }
+    std::sort(places.begin(), places.end());
+    if (std::adjacent_find(places.begin(), places.end()) != places.end())
+        return fail(SUN_ERR_SEQ_LEN, "two rows write the same position of a page");
+    return SUN_OK;
+}
+
+int sun_kv8_append(sun_kv8_pool* pool_, int layer, int rows, int dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                   const void* v, int64_t ld_v, const int32_t* positions, const int32_t* requests,
+                   const int32_t* page_tables, int n_requests, int max_pages, const void* q_norm, const void* k_norm,
+                   void* q_out, void* stream, unsigned flags) {
+    if (!pool_ || !k || !v || !positions || !requests || !page_tables) return fail(SUN_ERR_NULL, "NULL argument");
+    const Kv8Pool& pool = *(const Kv8Pool*)pool_;
+    const sun_model_cfg& c = pool.cfg;
+    if ((q != nullptr) != (q_out != nullptr)) return fail(SUN_ERR_SHAPE, "q and q_out go together");
+    if (!is_dtype(dtype)) return fail(SUN_ERR_SHAPE, "dtype must be SUN_F32 or SUN_BF16");
+    if (layer < 0 || layer >= c.n_layers) return fail(SUN_ERR_SHAPE, "layer out of range");
+    if (rows < 1 || n_requests < 1 || max_pages < 1 || max_pages > kKv8MaxPages)
+        return fail(SUN_ERR_SHAPE, "rows and n_requests must be >= 1, max_pages in [1, %d]", kKv8MaxPages);
+    if (c.qk_norm && (!k_norm || (q && !q_norm))) return fail(SUN_ERR_NULL, "the head norm's gains are missing");
+    if ((!c.qk_norm && (k_norm || q_norm)) || (!q && q_norm)) return fail(SUN_ERR_SHAPE, "head-norm gains without a head norm, or without q");
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_norm | (uintptr_t)k_norm | (uintptr_t)q_out) % 16)
+        return fail(SUN_ERR_SHAPE, "q, k, v, gains and q_out must be 16-byte aligned");
+    const int64_t unit = 16 / dtype_bytes(dtype), qd = (int64_t)c.n_q_heads * c.head_dim, kd = (int64_t)c.n_kv_heads * c.head_dim;
+    if ((q && (ld_q < qd || ld_q % unit)) || ld_k < kd || ld_k % unit || ld_v < kd || ld_v % unit)
+        return fail(SUN_ERR_SHAPE, "row strides must be at least a row and multiples of 16 bytes");
+    if (q && q == q_out && ld_q != qd) return fail(SUN_ERR_SHAPE, "q_out may be q only where q is contiguous");
+    const Kv8Rows r{q, k, v, ld_q, ld_k, ld_v, positions, requests, page_tables, rows, n_requests, max_pages, q_norm, k_norm, q_out};
+    hipStream_t st = (hipStream_t)stream;
+    if (flags & SUN_VALIDATE)
+        if (int rc = guarded([&] { return validate_kv8_rows(pool, r, st); })) return rc;
+    SUN_HIP_CHECK(launch_kv8_append(pool, layer, r, dtype == SUN_F32, st));
+    return SUN_OK;
+}
+
+size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages) {
+    if (!cfg || batch < 1 || max_pages < 1 || max_pages > kKv8MaxPages || check_cfg(cfg) != SUN_OK) return 0;
+    return align_up(std::max<size_t>(kv8_partial_floats(*cfg, batch, kv8_max_chunks(*cfg, batch, max_pages, 0)) * 4, 1));
+}
+
+static int validate_kv8_requests(const Kv8Pool& pool, int batch, const int32_t* page_tables, int max_pages, const int32_t* n_tokens,
+                                 int window, hipStream_t st) {
+    std::vector<int32_t> n((size_t)batch), tab((size_t)batch * max_pages);
+    SUN_HIP_CHECK(hipMemcpyAsync(n.data(), n_tokens, n.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipMemcpyAsync(tab.data(), page_tables, tab.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipStreamSynchronize(st));
+    for (int i = 0; i < batch; ++i) {
+        if (n[i] < 0 || n[i] > (long long)max_pages * kPageTokens)
+            return fail(SUN_ERR_SEQ_LEN, "request %d: %d tokens, the table has %d pages", i, n[i], max_pages);
+        for (int p = (window > 0 ? std::max(0, n[i] - window) : 0) / kPageTokens; p * kPageTokens < n[i]; ++p) {
+            const int32_t page = tab[(size_t)i * max_pages + p];
+            if (page < 0 || page >= pool.lay.n_pages)
+                return fail(SUN_ERR_PAGE_RANGE, "request %d: page-table entry %d = %d outside [0, %lld)", i, p, page, (long long)pool.lay.n_pages);
+        }
+    }
+    return SUN_OK;
+}
+
+int sun_kv8_attention(const sun_kv8_pool* pool_, int layer, int batch, int dtype, const void* q, const int32_t* page_tables,
+                      int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace, size_t workspace_bytes,
+                      void* stream, unsigned flags) {
+    if (!pool_ || !q || !page_tables || !n_tokens || !out || !workspace) return fail(SUN_ERR_NULL, "NULL argument");
+    const Kv8Pool& pool = *(const Kv8Pool*)pool_;
+    const sun_model_cfg& c = pool.cfg;
+    if (!is_dtype(dtype)) return fail(SUN_ERR_SHAPE, "dtype must be SUN_F32 or SUN_BF16");
+    if (layer < 0 || layer >= c.n_layers) return fail(SUN_ERR_SHAPE, "layer out of range");
+    if (batch < 1 || batch > 1024 || max_pages < 1 || max_pages > kKv8MaxPages || window < 0)
+        return fail(SUN_ERR_SHAPE, "batch must be in [1,1024], max_pages in [1, %d], window >= 0", kKv8MaxPages);
+    if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(SUN_ERR_SHAPE, "q and out must be 16-byte aligned");
+    if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    const size_t need = kv8_partial_floats(c, batch, kv8_max_chunks(c, batch, max_pages, window)) * 4;
+    if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
+    hipStream_t st = (hipStream_t)stream;
+    if (flags & SUN_VALIDATE)
+        if (int rc = guarded([&] { return validate_kv8_requests(pool, batch, page_tables, max_pages, n_tokens, window, st); })) return rc;
+    SUN_HIP_CHECK(launch_kv8_attention(pool, layer, batch, q, dtype == SUN_F32, page_tables, max_pages, n_tokens, window, out, (float*)workspace, st));
+    return SUN_OK;
+}
+
+// ---------------------------------------------------------------- microscaled 4-bit floats
+static int check_mx4(const void* codes, const void* scales, int rows, int cols, const void* dense, int dtype) {
+    if (!codes || !scales || !dense) return fail(SUN_ERR_NULL, "NULL argument");
+    if (!is_dtype(dtype)) return fail(SUN_ERR_SHAPE, "dtype must be SUN_F32 or SUN_BF16");
+    if (rows < 1 || cols < 32 || cols % 32) return fail(SUN_ERR_SHAPE, "rows must be >= 1, cols a positive multiple of 32");
+    if (((uintptr_t)codes | (uintptr_t)dense) % 16) return fail(SUN_ERR_SHAPE, "codes and dense arrays must be 16-byte aligned");
+    return SUN_OK;
+}
+
+int sun_mx4_quantize(const void* w, int dtype, int rows, int cols, void* codes, void* scales, void* stream) {
+    if (int rc = check_mx4(codes, scales, rows, cols, w, dtype)) return rc;
+    SUN_HIP_CHECK(launch_mx4_quantize(w, dtype == SUN_F32, rows, cols, codes, scales, (hipStream_t)stream));
+    return SUN_OK;
+}
+
+int sun_mx4_dequantize(const void* codes, const void* scales, int rows, int cols, int dtype, void* out, void* stream) {
+    if (int rc = check_mx4(codes, scales, rows, cols, out, dtype)) return rc;
+    SUN_HIP_CHECK(launch_mx4_dequantize(codes, scales, dtype == SUN_F32, rows, cols, out, (hipStream_t)stream));
+    return SUN_OK;
+}
+
+size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows) {
+    if (N < 1 || rows < 1 || K < 32 || K % 32) return 0;
+    return align_up(std::max<size_t>(mx4_linear_workspace(N, K, rows, true), 1));
+}
+
+int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x,
+                   void* out, int out_dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (int rc = check_mx4(codes, scales, N, K, x, x_dtype)) return rc;
+    if (!out || !workspace) return fail(SUN_ERR_NULL, "NULL argument");
+    if (!is_dtype(out_dtype) || rows < 1) return fail(SUN_ERR_SHAPE, "out_dtype must be SUN_F32 or SUN_BF16, rows >= 1");
+    if (ld_x < K || ld_x % (16 / dtype_bytes(x_dtype)) || ld_out < N || (uintptr_t)out % dtype_bytes(out_dtype))
+        return fail(SUN_ERR_SHAPE, "ld_x must be >= K and a multiple of 16 bytes, ld_out >= N, out aligned to its type");
+    if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    const size_t need = mx4_linear_workspace(N, K, rows, x_dtype == SUN_F32);
+    if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
+    const Mx4Linear m{(const uint8_t*)codes, (const uint8_t*)scales, N, K, rows, x, ld_x, x_dtype == SUN_F32, out, ld_out, out_dtype == SUN_F32};
+    SUN_HIP_CHECK(launch_mx4_linear(m, workspace, (hipStream_t)stream));
+    return SUN_OK;
+}
+
 }  // extern "C"

@@ -96,6 +96,38 @@ hipError_t launch_attn_prefill(const KvPool& pool, int layer, const float* q, co
 // how many splits the block wants
 int attn_prefill_splits(const sun_model_cfg& c, int rows, int first);
 
+// ---------------- the 8-bit cache (kv8.hip) ----------------
+struct Kv8Rows {   // rows of an append, see sun_kv8_append
+    const void *q, *k, *v;
+    int64_t ld_q, ld_k, ld_v;
+    const int32_t *positions, *requests, *page_tables;
+    int rows, n_requests, max_pages;
+    const void *q_norm, *k_norm;
+    void* q_out;
+};
+hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, bool f32, hipStream_t st);
+// Chunks of a request at most, whatever its length, and the scratch that they take when there are several.
+int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window);
+size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks);
+hipError_t launch_kv8_attention(const Kv8Pool& pool, int layer, int batch, const void* q, bool f32, const int32_t* page_tables, int max_pages,
+                                const int32_t* n_tokens, int window, void* out, float* partial, hipStream_t st);
+
+// ---------------- microscaled 4-bit floats (mx4.hip) ----------------
+hipError_t launch_mx4_quantize(const void* w, bool f32, int64_t rows, int64_t cols, void* codes, void* scales, hipStream_t st);
+hipError_t launch_mx4_dequantize(const void* codes, const void* scales, bool f32, int64_t rows, int64_t cols, void* out, hipStream_t st);
+struct Mx4Linear {
+    const uint8_t *codes, *scales;
+    int N, K, rows;
+    const void* x;
+    int64_t ld_x;
+    bool x_f32;
+    void* out;
+    int64_t ld_out;
+    bool out_f32;
+};
+size_t mx4_linear_workspace(int N, int K, int rows, bool x_f32);
+hipError_t launch_mx4_linear(const Mx4Linear& a, void* workspace, hipStream_t st);
+
 // ---------------- all layers of a small batch in one launch (layers.hip) ----------------
 constexpr int kLayersRows = 16;    // rows of such a step at most; measured in layers.hip
 constexpr int kLayersRowsW4 = 8;   // with 4-bit weights

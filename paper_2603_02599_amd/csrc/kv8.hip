@@ -1,0 +1,648 @@
+// The 8-bit paged cache: keys and values rotated, rounded and appended, and attention of one new token over them.
+//
+// A cached vector y of head_dim values is stored as e4m3 codes and one power of two: with e the smallest integer >= -100 for
+// which the largest finite |y| is at most 448 * 2^e, code = e4m3(y * 2^-e) and the scale byte is e + 127.  Scaling by a power of
+// two is exact, so a value has one rounding (2^-4 of itself at most, above the format's subnormals), and the power can be applied behind a
+// product: to a key's score, and to a value's weight.
+#include <math.h>
+
+#include "kernels.hpp"
+#include "rows.hpp"
+
+namespace sun {
+
+constexpr int kHalfMax = 64;   // pairs of a head's rotation at most
+
+struct Kv8AppendArgs {
+    uint8_t *codes, *scales;   // the layer's
+    int64_t k_page, k_head, v_off, v_page, v_head, s_page, s_head, vs_off;
+    Kv8Rows r;
+    int n_pages, Hq, Hkv, heads_a_block, row_blocks, parts;
+    float eps;
+    double theta[kHalfMax];
+};
+
+template <class T>
+__device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(p);
+        x[0] = v[0], x[1] = v[1], x[2] = v[2], x[3] = v[3];
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
+    }
+}
+template <int O>
+__device__ __forceinline__ double lane_xor_f64(double v) {
+    const uint2 w = __builtin_bit_cast(uint2, v);
+    return __builtin_bit_cast(double, uint2{lane_xor<O>(w.x), lane_xor<O>(w.y)});
+}
+template <int LANES, class R>
+__device__ __forceinline__ R lanes_sum(R v) {
+    auto step = [](auto o, R a) {
+        if constexpr (sizeof(R) == 8) return a + lane_xor_f64<decltype(o)::value>(a);
+        else return a + lane_xor<decltype(o)::value>(a);
+    };
+    v = step(std::integral_constant<int, 1>{}, v);
+    v = step(std::integral_constant<int, 2>{}, v);
+    v = step(std::integral_constant<int, 4>{}, v);
+    if constexpr (LANES == 16) v = step(std::integral_constant<int, 8>{}, v);
+    return v;
+}
+// the magnitude that decides a vector's power: not-a-numbers and infinities do not count
+__device__ __forceinline__ float finite_abs(float y) {
+    const float a = fabsf(y);
+    return a < INFINITY ? a : 0.f;
+}
+// e + 127 for the largest magnitude top; 448 = 1.75 * 2^8
+__device__ __forceinline__ int entry_scale(float top) {
+    const uint32_t b = __float_as_uint(top);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);   // a subnormal top is far below 448 * 2^-100
+    return max(e, -100) + 127;
+}
+__device__ __forceinline__ uint32_t entry_codes(float a, float b, float c, float d, float inv) {
+    const float x[4] = {a, b, c, d};
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, w, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(fabsf(x[i]) < INFINITY)) w = (w & ~(255u << (8 * i))) | (0x7fu << (8 * i));
+    return w;
+}
+__device__ __forceinline__ float entry_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+
+// Where a row's key and value go: the page, or -1 for a padding row or a position without a page.
+__device__ __forceinline__ int row_page(const Kv8AppendArgs& a, int row, int pos) {
+    if (pos < 0) return -1;
+    const int req = a.r.requests[row], col = pos / kPageTokens;
+    if (req < 0 || req >= a.r.n_requests || col >= a.r.max_pages) return -1;
+    const int page = a.r.page_tables[(int64_t)req * a.r.max_pages + col];
+    return page >= 0 && page < a.n_pages ? page : -1;
+}
+
+// Workgroups [0, row_blocks * parts): q and k of RG rows, head_dim / 8 lanes a head with four pairs each.  The rest: v of 16 rows, a wave
+// a head.  Queries are computed in 32 bits; keys, which are rounded to few bits behind it, in 64 up to one rounding to 32, so that no
+// code depends on the order of operations.
+template <class T, int D, int RG>
+__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
+    constexpr int LPH = D / 8;   // lanes per head
+    __shared__ float2 turn[RG][D / 2];
+    __shared__ uint32_t vcode[4][16][D / 4 + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int rows = a.r.rows;
+    if ((int)blockIdx.x < a.row_blocks * a.parts) {
+        const int row0 = ((int)blockIdx.x / a.parts) * RG, part = (int)blockIdx.x % a.parts;
+        if (tid < RG * (D / 2)) {
+            const int r = tid / (D / 2), j = tid % (D / 2);
+            const int pos = row0 + r < rows ? a.r.positions[row0 + r] : -1;
+            if (pos >= 0) turn[r][j] = rope_pair(a.theta[j], pos);
+        }
+        __syncthreads();
+        const int nq = a.r.q ? a.Hq : 0, heads = nq + a.Hkv, total = heads * min(RG, rows - row0);
+        const int sub = lane % LPH, j0 = 4 * sub, group = tid / LPH;
+        constexpr int GROUPS = 256 / LPH;
+        for (int base = part * GROUPS; base < total; base += a.parts * GROUPS) {   // the same for all lanes, which read one another
+            const int at = base + group, r = min(at, total - 1) / heads, head = min(at, total - 1) % heads, row = row0 + r;
+            const int pos = a.r.positions[row];
+            const bool live = at < total && pos >= 0, is_q = head < nq;
+            const T* src = is_q ? (const T*)a.r.q + row * a.r.ld_q + head * D : (const T*)a.r.k + row * a.r.ld_k + (head - nq) * D;
+            float x[4], y[4];
+            load4(src + j0, x);
+            load4(src + D / 2 + j0, y);
+            const T* gain = (const T*)(is_q ? a.r.q_norm : a.r.k_norm);
+            float gx[4], gy[4];
+            if (gain) {
+                load4(gain + j0, gx);
+                load4(gain + D / 2 + j0, gy);
+            }
+            float2 cs[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cs[i] = turn[r][j0 + i];
+            float qa[4], qb[4], ka[4], kb[4];
+            if (__any(is_q)) {
+                float scale = 1.f;
+                if (gain) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ss += x[i] * x[i] + y[i] * y[i];
+                    scale = 1.f / sqrtf(lanes_sum<LPH>(ss) / (float)D + a.eps);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float u = gain ? x[i] * scale * gx[i] : x[i], w = gain ? y[i] * scale * gy[i] : y[i];
+                    qa[i] = u * cs[i].x - w * cs[i].y;
+                    qb[i] = w * cs[i].x + u * cs[i].y;
+                }
+            }
+            if (__any(!is_q)) {
+                double scale = 1.0;
+                if (gain) {
+                    double ss = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ss += (double)x[i] * (double)x[i] + (double)y[i] * (double)y[i];
+                    scale = 1.0 / sqrt(lanes_sum<LPH>(ss) / (double)D + (double)a.eps);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double u = gain ? x[i] * scale * gx[i] : (double)x[i], w = gain ? y[i] * scale * gy[i] : (double)y[i];
+                    ka[i] = (float)(u * cs[i].x - w * cs[i].y);
+                    kb[i] = (float)(w * cs[i].x + u * cs[i].y);
+                }
+            }
+            float top = 0.f;
+            if (!is_q) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(finite_abs(ka[i]), finite_abs(kb[i])));
+            }
+            top = fmaxf(top, lane_xor<1>(top));
+            top = fmaxf(top, lane_xor<2>(top));
+            top = fmaxf(top, lane_xor<4>(top));
+            if constexpr (LPH == 16) top = fmaxf(top, lane_xor<8>(top));
+            if (!live) continue;
+            if (is_q) {
+                T* dst = (T*)a.r.q_out + ((int64_t)row * a.Hq + head) * D + j0;
+                if constexpr (sizeof(T) == 4) {
+                    *reinterpret_cast<f32x4*>(dst) = f32x4{qa[0], qa[1], qa[2], qa[3]};
+                    *reinterpret_cast<f32x4*>(dst + D / 2) = f32x4{qb[0], qb[1], qb[2], qb[3]};
+                } else {
+                    *reinterpret_cast<uint2*>(dst) = uint2{pack_bf16(qa[0], qa[1]), pack_bf16(qa[2], qa[3])};
+                    *reinterpret_cast<uint2*>(dst + D / 2) = uint2{pack_bf16(qb[0], qb[1]), pack_bf16(qb[2], qb[3])};
+                }
+                continue;
+            }
+            const int page = row_page(a, row, pos);
+            if (page < 0) continue;
+            const int byte = entry_scale(top), slot = pos % kPageTokens, kvh = head - nq;
+            const float inv = entry_inverse(byte);
+            uint8_t* dst = a.codes + page * a.k_page + kvh * a.k_head + slot * D + j0;
+            *reinterpret_cast<uint32_t*>(dst) = entry_codes(ka[0], ka[1], ka[2], ka[3], inv);
+            *reinterpret_cast<uint32_t*>(dst + D / 2) = entry_codes(kb[0], kb[1], kb[2], kb[3], inv);
+            if (sub == 0) a.scales[page * a.s_page + kvh * a.s_head + slot] = (uint8_t)byte;
+        }
+        return;
+    }
+    // ---- v: lane (row lane / 4, quarter lane % 4) of 16 rows
+    const int blk = (int)blockIdx.x - a.row_blocks * a.parts, per = (a.Hkv + 3) / 4;
+    const int row0 = (blk / per) * 16, head = (blk % per) * 4 + wave;
+    if (head >= a.Hkv) return;   // a wave is by itself from here on
+    constexpr int E = 16 / (int)sizeof(T), NL = D / (4 * E);   // values of a load, loads of a lane
+    const int r = lane >> 2, quarter = lane & 3, row = min(row0 + r, rows - 1);
+    const int pos = row0 + r < rows ? a.r.positions[row] : -1;
+    const int page = row_page(a, row, pos);
+    const T* src = (const T*)a.r.v + row * a.r.ld_v + head * D + quarter * E;
+    float x[NL][E];
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int h = 0; h < E; h += 4) {
+            float v[4];
+            load4(src + i * 4 * E + h, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][h + e] = v[e];
+        }
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) top = fmaxf(top, finite_abs(x[i][e]));
+    top = fmaxf(top, lane_xor<1>(top));
+    top = fmaxf(top, lane_xor<2>(top));
+    const int byte = entry_scale(top);
+    const float inv = entry_inverse(byte);
+    uint8_t* vbase = a.codes + a.v_off + head * a.v_head;
+    if (page >= 0 && quarter == 0) a.scales[a.vs_off + page * a.s_page + head * a.s_head + pos % kPageTokens] = (uint8_t)byte;
+    // Sixteen rows that are consecutive positions of one request and have their pages leave in groups of four tokens; others byte by byte.
+    const int pos0 = __builtin_amdgcn_readfirstlane(pos), req = row0 + r < rows ? a.r.requests[row] : -1;
+    const int req0 = __builtin_amdgcn_readfirstlane(req), count = min(16, rows - row0);
+    const bool run = __all(r >= count || (page >= 0 && req == req0 && pos == pos0 + r));
+    uint32_t* mine = &vcode[wave][r][0];
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int h = 0; h < E; h += 4) {
+            const uint32_t w = entry_codes(x[i][h], x[i][h + 1], x[i][h + 2], x[i][h + 3], inv);
+            const int dim = i * 4 * E + quarter * E + h;
+            mine[dim / 4] = w;
+            if (!run && page >= 0) {
+                uint8_t* dst = vbase + page * a.v_page + dim * kPageTokens + pos % kPageTokens;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) dst[b * kPageTokens] = (uint8_t)(w >> (8 * b));
+            }
+        }
+    if (!run) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a wave's LDS operations are in order, and other waves use other places
+    const uint8_t* got = reinterpret_cast<const uint8_t*>(&vcode[wave][0][0]);
+    constexpr int LDR = (D / 4 + 1) * 4;
+    for (int quad = pos0 >> 2; quad <= (pos0 + count - 1) >> 2; ++quad) {
+        const int t0 = quad * 4 - pos0;   // row of the quad's first token
+        const int pg = __shfl(page, min(max(t0, 0), count - 1) * 4);
+        uint8_t* dst = vbase + pg * a.v_page + (quad & 3) * 4;
+        for (int dim = lane; dim < D; dim += 64) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) w |= (uint32_t)got[min(max(t0 + b, 0), count - 1) * LDR + dim] << (8 * b);
+            if (t0 >= 0 && t0 + 3 < count) {
+                *reinterpret_cast<uint32_t*>(dst + dim * kPageTokens) = w;
+            } else {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    if (t0 + b >= 0 && t0 + b < count) dst[dim * kPageTokens + b] = (uint8_t)(w >> (8 * b));
+            }
+        }
+    }
+}
+
+template <class T, int D>
+static hipError_t append(const Kv8AppendArgs& a0, hipStream_t st) {
+    Kv8AppendArgs a = a0;
+    const int rows = a.r.rows, v_blocks = (rows + 15) / 16 * ((a.Hkv + 3) / 4);
+    if (rows >= 1024) {
+        a.row_blocks = (rows + 3) / 4;
+        a.parts = 1;
+        hipLaunchKernelGGL((kv8_append_kernel<T, D, 4>), dim3(a.row_blocks * a.parts + v_blocks), dim3(256), 0, st, a);
+    } else {
+        a.row_blocks = rows;
+        a.parts = 1;
+        hipLaunchKernelGGL((kv8_append_kernel<T, D, 1>), dim3(a.row_blocks * a.parts + v_blocks), dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, bool f32, hipStream_t st) {
+    const sun_model_cfg& c = pool.cfg;
+    const sun_kv8_layout& L = pool.lay;
+    Kv8AppendArgs a{};
+    a.codes = pool.base + L.k_off + layer * L.k_layer;
+    a.scales = pool.base + L.ks_off + layer * L.s_layer;
+    a.k_page = L.k_page, a.k_head = L.k_head;
+    a.v_off = L.v_off - L.k_off, a.v_page = L.v_page, a.v_head = L.v_head;
+    a.s_page = L.s_page, a.s_head = L.s_head, a.vs_off = L.vs_off - L.ks_off;
+    a.r = r;
+    a.n_pages = (int)L.n_pages, a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads;
+    a.eps = c.rms_eps;
+    EmbedRope e{};
+    e.d = c.head_dim, e.base = c.rope_base;
+    e.rs = RopeScale{c.rope_scaling, c.rope_original_max_position, (double)c.rope_factor, (double)c.rope_low_freq_factor, (double)c.rope_high_freq_factor};
+    for (int j = 0; j < c.head_dim / 2; ++j) a.theta[j] = rope_theta(e, j);
+    if (f32) return c.head_dim == 128 ? append<float, 128>(a, st) : append<float, 64>(a, st);
+    return c.head_dim == 128 ? append<uint16_t, 128>(a, st) : append<uint16_t, 64>(a, st);
+}
+
+// ---------------------------------------------------------------- attention of one new token
+//
+// A wave takes a chunk of one request's tokens for one KV head and walks it 64 tokens (four pages) a step.  With lanes
+// (c = lane % 16, g = lane / 16):
+//   scores  S^T = K Q^T, 16 x 16 x 32: row m of tile t (0..3) is token 4 t + m % 4 of page m / 4, so that lane (c, g) gets the scores
+//           of head c and all sixteen tokens of page g: 4 t + i from register i of tile t.
+//   output  O = P V: the same lane is P's operand for the tokens of page g, and V [dim][token] gives lane (dim, g) those tokens in one load.
+// No value moves between lanes on the way.  Heads are at most eight, so the operands' sixteen places hold two of an operand's
+// planes: a weight p is carried as bf16(p) and bf16 of the rest (16 bits together, 24 with a third plane for 32-bit calls), and a 32-bit
+// query as three truncations of 8 bits, which are exact.  Codes become bf16 exactly.  Powers of two are applied to scores and weights.
+// The running maximum and sum are in 32 bits; the sum is over the weights before they are split.
+
+constexpr int kKv8Step = 64;
+constexpr int kKv8MaxChunk = 512;
+
+// Tokens of a chunk: a power of two that gives about 2048 of them over the batch if all requests were like this one.  It depends on the
+// request's own length, the batch size and the heads, so a request's result does not depend on its batch-mates.
+__host__ __device__ inline int kv8_chunk(int span, int batch, int Hkv) {
+    const long long target = (long long)span * Hkv * batch / 2048;
+    int ch = kKv8Step;
+    while (ch < kKv8MaxChunk && 2 * ch <= target) ch *= 2;
+    return ch;
+}
+
+struct Kv8AttnArgs {
+    const uint8_t *codes, *scales;
+    int64_t k_page, k_head, v_off, v_page, v_head, s_page, s_head, vs_off;
+    const void* q;
+    const int32_t *page_tables, *n_tokens;
+    void* out;
+    float* partial;     // [batch][chunks][Hq][D], behind them (maximum in powers of two, sum) pairs [batch][chunks][Hq]
+    int batch, max_pages, n_pages, Hq, Hkv, window, chunks;
+    float c;            // log2(e) / sqrt(D)
+};
+
+struct Kv8Span {
+    int first, n, chunk, chunks;   // first token of the first page, end, tokens of a chunk, chunks (0: nothing to attend to)
+    int lo;
+};
+__device__ __forceinline__ Kv8Span kv8_span(const Kv8AttnArgs& a, int b) {
+    Kv8Span s;
+    const long long cap = (long long)a.max_pages * kPageTokens;
+    s.n = (int)min((long long)max(a.n_tokens[b], 0), cap);
+    s.lo = a.window > 0 ? max(0, s.n - a.window) : 0;
+    s.first = s.lo / kPageTokens * kPageTokens;
+    const int span = s.n - s.first;
+    s.chunk = kv8_chunk(span, a.batch, a.Hkv);
+    s.chunks = (span + s.chunk - 1) / s.chunk;
+    return s;
+}
+
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w0, uint32_t w1) {
+    struct { bf16x2_t v[4]; } r;
+    r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false);
+    r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true);
+    r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false);
+    r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true);
+    return __builtin_bit_cast(bf16x8, r);
+}
+__device__ __forceinline__ float power(uint32_t word, int byte) { return __uint_as_float(((word >> (8 * byte)) & 255u) << 23); }
+// x with its lower 16 bits off; what is left of a finite x is exact
+__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ float below(float x) {
+    const float r = x - upper(x);
+    return fabsf(x) < INFINITY ? r : 0.f;
+}
+
+template <class T>
+__device__ __forceinline__ void store_as(T* p, float v) {
+    if constexpr (sizeof(T) == 4) *p = v;
+    else *p = f32_to_bf16_bits(v);
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int NH = D / 64, NB = D / 16;   // loads of a key's quarter, dim blocks of the output
+    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+    const long long item = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = (int)(item % a.Hkv);
+    const long long rest = item / a.Hkv;
+    const int b = (int)(rest % a.batch), ci = (int)(rest / a.batch);
+    if (ci >= a.chunks) return;
+    const Kv8Span s = kv8_span(a, b);
+    const int G = a.Hq / a.Hkv;
+    if (ci >= s.chunks) {
+        if (ci == 0 && s.chunks == 0)   // nothing to attend to
+            for (int i = lane; i < G * D; i += 64) store_as((T*)a.out + ((int64_t)b * a.Hq + head * G) * D + i, 0.f);
+        return;
+    }
+    const int begin = s.first + ci * s.chunk, end = min(s.n, begin + s.chunk);
+    const int32_t* table = a.page_tables + (int64_t)b * a.max_pages;
+
+    // queries: operand column c, dims 64 h + 16 g + 8 u .. + 7
+    bf16x8 q0[NH][2], q2[F32 ? NH : 1][2];
+    {
+        const int hd = c16 & 7;
+        const T* qp = (const T*)a.q + ((int64_t)b * a.Hq + head * G + min(hd, G - 1)) * D + 16 * g;
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (F32) {
+                    u32x4_s w0, w2;
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        uint32_t bits0 = 0, bits2 = 0;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float x = hd < G ? qp[64 * h + 8 * u + 2 * p + e] : 0.f;
+                            if (x != x) x = __uint_as_float(0x7fc00000u);   // one that its upper bits say
+                            const float r1 = below(x), r2 = below(r1);
+                            const float mine = c16 < 8 ? x : r1;
+                            bits0 |= (__float_as_uint(mine) >> 16) << (16 * e);
+                            bits2 |= (c16 < 8 ? __float_as_uint(r2) >> 16 : 0u) << (16 * e);
+                        }
+                        w0[p] = bits0;
+                        w2[p] = bits2;
+                    }
+                    q0[h][u] = __builtin_bit_cast(bf16x8, w0);
+                    q2[h][u] = __builtin_bit_cast(bf16x8, w2);
+                } else {
+                    u32x4_s w = *reinterpret_cast<const u32x4_s*>(qp + 64 * h + 8 * u);
+                    if (hd >= G) w = u32x4_s{0, 0, 0, 0};
+                    q0[h][u] = __builtin_bit_cast(bf16x8, w);
+                }
+            }
+    }
+    f32x4 o[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    const uint8_t* kb = a.codes + head * a.k_head;
+    const uint8_t* vb = a.codes + a.v_off + head * a.v_head;
+    const uint8_t* sb = a.scales + head * a.s_head;
+    auto page_at = [&](int tok, int idx) { return table[min(tok / kPageTokens + idx, a.max_pages - 1)]; };
+    auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
+    for (int tok = begin; tok < end; tok += kKv8Step) {
+        const int pk = page_at(tok, c16 >> 2), pv = page_at(tok, g);
+        const uint8_t* kp = kb + (int64_t)(usable(pk) ? pk : 0) * a.k_page + (c16 & 3) * D + 16 * g;
+        const int64_t pvc = usable(pv) ? pv : 0;
+        const uint8_t* vp = vb + pvc * a.v_page + c16 * kPageTokens;
+        u32x4_s kr[4][NH], vr[NB];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) kr[t][h] = *reinterpret_cast<const u32x4_s*>(kp + 4 * t * D + 64 * h);
+        const u32x4_s ks = *reinterpret_cast<const u32x4_s*>(sb + pvc * a.s_page);
+        const u32x4_s vs = *reinterpret_cast<const u32x4_s*>(sb + a.vs_off + pvc * a.s_page);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) vr[i] = *reinterpret_cast<const u32x4_s*>(vp + i * 16 * kPageTokens);
+
+        float p[16];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < NH; ++h)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bf16x8 k = codes_to_bf16(kr[t][h][2 * u], kr[t][h][2 * u + 1]);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q0[h][u], acc, 0, 0, 0);
+                    if constexpr (F32) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q2[h][u], acc, 0, 0, 0);
+                }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v = acc[i];
+                if constexpr (F32) v += lane_xor<8>(v);
+                p[4 * t + i] = v * power(ks[t], i);
+            }
+        }
+        // tokens outside [lo, end) and of pages that are not there: no weight, and codes and powers that nobody wrote are not used
+        const int at = tok + kPageTokens * g;
+        float w[16];
+        const bool whole = __all(usable(pv) && at >= s.lo && at + kPageTokens <= end);
+        if (!whole) {
+            uint32_t live = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool on = usable(pv) && at + i >= s.lo && at + i < end;
+                live |= (uint32_t)on << i;
+                if (!on) p[i] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t mask = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mask |= (live >> (4 * j + e) & 1) ? 255u << (8 * e) : 0u;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) vr[i][j] &= mask;
+            }
+        }
+        float top = p[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+        {
+            float x = top, y = top;
+            swap_rows<16>(x, y);
+            top = fmaxf(x, y);
+            x = y = top;
+            swap_rows<32>(x, y);
+            top = fmaxf(x, y);
+        }
+        if (__any(top > m)) {
+            const float grown = fmaxf(top, m);
+            const float scale = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - grown) * a.c);
+            l *= scale;
+            m = grown;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = __shfl(scale, (4 * g + i) & 7);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) o[j][i] *= f;
+            }
+        }
+        const float mc = m == -INFINITY ? 0.f : m * a.c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], a.c, -mc));
+            l += e;
+            w[i] = e == 0.f ? 0.f : e * power(vs[i >> 2], i & 3);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            u32x4_s w0, w2;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = w[8 * u + 2 * j], y = w[8 * u + 2 * j + 1];
+                const uint32_t hi = pack_bf16(x, y);
+                const float rx = x - bf16_lo(hi), ry = y - bf16_hi(hi);
+                const uint32_t lo = pack_bf16(rx, ry);
+                w0[j] = c16 < 8 ? hi : lo;
+                if constexpr (F32) w2[j] = c16 < 8 ? pack_bf16(rx - bf16_lo(lo), ry - bf16_hi(lo)) : 0u;
+            }
+            const bf16x8 p0 = __builtin_bit_cast(bf16x8, w0);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const bf16x8 v = codes_to_bf16(vr[i][2 * u], vr[i][2 * u + 1]);
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p0, v, o[i], 0, 0, 0);
+                if constexpr (F32) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w2), v, o[i], 0, 0, 0);
+            }
+        }
+    }
+    // sums of the four pages' lanes, planes of the output, and both to the lanes of heads 4 g + i
+    {
+        float x = l, y = l;
+        swap_rows<16>(x, y);
+        l = x + y;
+        x = y = l;
+        swap_rows<32>(x, y);
+        l = x + y;
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] += lane_xor<32>(o[j][i]);
+    const bool one = s.chunks == 1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int hd = 4 * g + i;
+        const float sum = __shfl(l, hd & 7), top = __shfl(m, hd & 7);
+        if (g >= 2 || hd >= G) continue;
+        const int64_t h = head * G + hd;
+        if (one) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            T* dst = (T*)a.out + ((int64_t)b * a.Hq + h) * D + c16;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) store_as(dst + 16 * j, o[j][i] * inv);
+        } else {
+            const int64_t at = ((int64_t)b * a.chunks + ci) * a.Hq + h;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) a.partial[at * D + 16 * j + c16] = o[j][i];
+            float* ml = a.partial + (int64_t)a.batch * a.chunks * a.Hq * D + at * 2;
+            if (c16 == 0) ml[0] = top * a.c, ml[1] = sum;
+        }
+    }
+}
+
+// out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over a request's chunks; a wave a head
+template <class T, int D>
+__global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnArgs a) {
+    const int lane = threadIdx.x & 63;
+    const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (item >= (long long)a.batch * a.Hq) return;
+    const int b = (int)(item / a.Hq), h = (int)(item % a.Hq);
+    const Kv8Span s = kv8_span(a, b);
+    if (s.chunks < 2) return;
+    const int64_t at0 = (int64_t)b * a.chunks * a.Hq + h;
+    const float2* ml = reinterpret_cast<const float2*>(a.partial + (int64_t)a.batch * a.chunks * a.Hq * D);
+    float top = -INFINITY;
+    for (int c = lane; c < s.chunks; c += 64) top = fmaxf(top, ml[at0 + (int64_t)c * a.Hq].x);
+    top = wave_max(top);
+    if (top == -INFINITY) top = 0.f;
+    float sum = 0.f, o[D / 64];
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) o[j] = 0.f;
+    for (int c = 0; c < s.chunks; ++c) {
+        const int64_t at = at0 + (int64_t)c * a.Hq;
+        const float2 p = ml[at];
+        const float w = __builtin_amdgcn_exp2f(p.x - top);
+        sum += w * p.y;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) o[j] += w * a.partial[at * D + 64 * j + lane];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + 64 * j + lane, o[j] * inv);
+}
+
+int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window) {
+    long long most = (long long)max_pages * kPageTokens;
+    if (window > 0) most = std::min(most, (long long)window + kPageTokens - 1);
+    most = std::min(most, 0x7fffffffll);
+    // within one length of chunk the longest request has the most of them
+    long long chunks = 1;
+    const long long per = (long long)c.n_kv_heads * batch;
+    for (int ch = kKv8Step; ch <= kKv8MaxChunk; ch *= 2) {
+        const long long last = ch == kKv8MaxChunk ? most : std::min(most, (2ll * ch * 2048 - 1) / per);   // the longest with chunks of at most ch
+        if (last > 0) chunks = std::max(chunks, (last + ch - 1) / ch);
+    }
+    return (int)std::min(chunks, 0x7fffffffll);
+}
+size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks) {
+    return chunks < 2 ? 0 : (size_t)batch * chunks * c.n_q_heads * (c.head_dim + 2);
+}
+
+template <class T, int D>
+static hipError_t attend(const Kv8AttnArgs& a, hipStream_t st) {
+    const long long items = (long long)a.batch * a.Hkv * a.chunks;
+    hipLaunchKernelGGL((kv8_attn_kernel<T, D>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.chunks > 1)
+        hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)(((long long)a.batch * a.Hq + 3) / 4)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_attention(const Kv8Pool& pool, int layer, int batch, const void* q, bool f32, const int32_t* page_tables, int max_pages,
+                                const int32_t* n_tokens, int window, void* out, float* partial, hipStream_t st) {
+    const sun_model_cfg& c = pool.cfg;
+    const sun_kv8_layout& L = pool.lay;
+    Kv8AttnArgs a{};
+    a.codes = pool.base + L.k_off + layer * L.k_layer;
+    a.scales = pool.base + L.ks_off + layer * L.s_layer;
+    a.k_page = L.k_page, a.k_head = L.k_head;
+    a.v_off = L.v_off - L.k_off, a.v_page = L.v_page, a.v_head = L.v_head;
+    a.s_page = L.s_page, a.s_head = L.s_head, a.vs_off = L.vs_off - L.ks_off;
+    a.q = q, a.page_tables = page_tables, a.n_tokens = n_tokens, a.out = out, a.partial = partial;
+    a.batch = batch, a.max_pages = max_pages, a.n_pages = (int)L.n_pages;
+    a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads, a.window = window;
+    a.chunks = kv8_max_chunks(c, batch, max_pages, window);
+    a.c = 1.4426950408889634f / sqrtf((float)c.head_dim);
+    if (f32) return c.head_dim == 128 ? attend<float, 128>(a, st) : attend<float, 64>(a, st);
+    return c.head_dim == 128 ? attend<uint16_t, 128>(a, st) : attend<uint16_t, 64>(a, st);
+}
+
+}  // namespace sun

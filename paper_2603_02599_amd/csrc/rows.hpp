@@ -32,7 +32,7 @@ inline EmbedRope make_embed_rope(const sun_model_cfg& cfg, const void* embed, co
                                (double)cfg.rope_low_freq_factor, (double)cfg.rope_high_freq_factor}};
 }
 
-__device__ __forceinline__ double rope_theta(const EmbedRope& e, int j) {
+__host__ __device__ __forceinline__ double rope_theta(const EmbedRope& e, int j) {
     double theta = pow(e.base, -2.0 * (double)j / (double)e.d);
     if (e.rs.scaling == 1) {
         const double wavelen = 2.0 * 3.14159265358979323846 / theta, orig = (double)e.rs.orig_max;
