@@ -1616,7 +1616,7 @@ int sun_mx4_dequantize(const void* codes, const void* scales, int rows, int cols
 
 size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows) {
     if (N < 1 || rows < 1 || K < 32 || K % 32) return 0;
-    return align_up(std::max<size_t>(mx4_linear_workspace(N, K, rows, true), 1));
+    return align_up(std::max<size_t>(mx4_linear_workspace_up_to(N, K, rows), 1));
 }
 
 int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x,

@@ -126,6 +126,7 @@ struct Mx4Linear {
     bool out_f32;
 };
 size_t mx4_linear_workspace(int N, int K, int rows, bool x_f32);
+size_t mx4_linear_workspace_up_to(int N, int K, int rows);
 hipError_t launch_mx4_linear(const Mx4Linear& a, void* workspace, hipStream_t st);
 
 // ---------------- all layers of a small batch in one launch (layers.hip) ----------------

@@ -110,6 +110,8 @@ struct Mx4Args {
     int64_t ld_x, plane, ld_out;
     int N, K, rows;
     void* out;
+    float* part;           // [splits][rows][N], where k is split
+    bool wide;             // four columns of out may be stored at once
 };
 
 // 32-bit activations as their three planes; a lane takes eight
@@ -159,69 +161,368 @@ __device__ __forceinline__ void store_as(T* p, float v) {
     else *p = f32_to_bf16_bits(v);
 }
 
-// Sixteen columns and 16 * RB rows a workgroup, the blocks of k dealt to its four waves, whose sums meet in LDS.  Lane (c = lane % 16,
+__device__ u32x4_s g_mx4_zeros = {0, 0, 0, 0};   // what lanes behind the last column are given
+
+// Requests from memory straight into LDS, the address a lane's own: 16 bytes a lane (lane i's land at lds_byte + 16 i), or a byte, which
+// lands as a word (at lds_byte + 4 i).  Whoever reads the place waits for vmcnt and the barrier by hand.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is a reserved register, see lds_dma16
+__device__ __forceinline__ void lds_fetch16(const void* p, uint32_t lds_byte) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_fetch1(const void* p, uint32_t lds_byte) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// Four consecutive columns of one row
+template <class T>
+__device__ __forceinline__ void store_quad(const Mx4Args& a, T* out, int64_t ld, bool wide, int64_t row, int n, const f32x4& v) {
+    T* p = out + row * ld + n;
+    if (wide && n + 3 < a.N) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = v;
+        else *reinterpret_cast<uint2*>(p) = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n + i < a.N) store_as(p + i, v[i]);
+}
+
+// Up to sixteen rows: sixteen columns a workgroup, chunks of 128 k dealt to its eight waves, whose sums meet in LDS.  Lane (c = lane % 16,
 // g = lane / 16) holds column c's block 4 i + g of codes, one 16-byte load, which are four 16 x 16 x 32 products.
-template <class T, int P, int RB>
-__global__ __launch_bounds__(256) void mx4_linear_kernel(Mx4Args a) {
-    __shared__ float sums[4][16 * RB][17];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16, row0 = blockIdx.y * (16 * RB);
+constexpr int kFewWaves = 8;
+template <class T, int P>
+__global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
+    __shared__ float sums[kFewWaves][16][17];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16;
     const int64_t n = min(n0 + c16, a.N - 1);
-    const int blocks = a.K / kMxBlock;
-    f32x4 acc[RB];
+    const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
+    const uint16_t* xr = a.x + (int64_t)min(c16, a.rows - 1) * a.ld_x;
+    constexpr int U = 4;
+    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int i0 = wave; i0 < chunks; i0 += kFewWaves * U) {
+        u32x4_s code[U];
+        uint32_t power[U];
+        int at[U];
 #pragma unroll
-    for (int r = 0; r < RB; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = wave; i * 4 < blocks; i += 4) {
-        const int blk = i * 4 + g, at = min(blk, blocks - 1);
-        u32x4_s code = *reinterpret_cast<const u32x4_s*>(a.codes + (n * blocks + at) * 16);
-        float scale = mx4_scale(a.scales[n * blocks + at]);
-        if (blk >= blocks) code = u32x4_s{0, 0, 0, 0}, scale = 1.f;
+        for (int u = 0; u < U; ++u) {
+            const int blk = (i0 + u * kFewWaves) * 4 + g;
+            at[u] = min(blk, blocks - 1);
+            code[u] = *reinterpret_cast<const u32x4_s*>(a.codes + (n * blocks + at[u]) * 16);
+            power[u] = a.scales[n * blocks + at[u]];
+            if (blk >= blocks) at[u] = -1;
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const bf16x8 w = mx4_values(code[j], scale);
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * kFewWaves >= chunks) break;
+            const bool on = at[u] >= 0;
+            const float scale = on ? mx4_scale(power[u]) : 1.f;
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const int64_t row = min(row0 + 16 * r + c16, a.rows - 1);
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 w = mx4_values(on ? code[u][j] : 0u, scale);
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    u32x4_s x = *reinterpret_cast<const u32x4_s*>(a.x + p * a.plane + row * a.ld_x + at * 32 + j * 8);
-                    if (blk >= blocks) x = u32x4_s{0, 0, 0, 0};
-                    acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, x), acc[r], 0, 0, 0);
+                    const u32x4_s* src = on ? reinterpret_cast<const u32x4_s*>(xr + p * a.plane + at[u] * 32 + j * 8) : &g_mx4_zeros;
+                    acc[j & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, *src), acc[j & 1], 0, 0, 0);
                 }
             }
         }
     }
     // register i: column 4 g + i, row c
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sums[wave][16 * r + c16][4 * g + i] = acc[r][i];
+    for (int i = 0; i < 4; ++i) sums[wave][c16][4 * g + i] = acc[0][i] + acc[1][i];
     __syncthreads();
-    for (int u = threadIdx.x; u < 16 * RB * 16; u += 256) {
-        const int r = u >> 4, c = u & 15;
-        if (row0 + r < a.rows && n0 + c < a.N)
-            store_as((T*)a.out + (row0 + r) * a.ld_out + n0 + c, ((sums[0][r][c] + sums[1][r][c]) + sums[2][r][c]) + sums[3][r][c]);
+    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
+    if (r < a.rows && r < 16 && n0 + c < a.N) {
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) v += sums[w][r][c];
+        store_as((T*)a.out + r * a.ld_out + n0 + c, v);
     }
 }
 
+// Some dozen rows, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Codes, powers and activations of
+// ST - 1 steps of 128 k are under way into LDS while one is computed on; every request takes the place in LDS that the lane reads its operand
+// from, so there are no bank conflicts.  A step is a chunk of k of one plane of the activations.
+template <class T, int P, int RT, int NT, int WN, int ST>
+__global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
+    constexpr int XF = RT * 4, CF = NT * WN;                    // operand fragments (1 KiB) of a step: activations, codes
+    constexpr int C0 = XF * 1024, S0 = C0 + CF * 1024, STAGE = S0 + CF * 256;
+    constexpr int XW = XF / WN, OPS = XW + 2 * NT;              // a wave's requests of activations, all of its requests
+    static_assert(XF % WN == 0 && OPS * (ST - 2) < 64 && ST * STAGE <= 160 * 1024, "");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ST * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * (16 * NT * WN) + wave * 16 * NT, row0 = blockIdx.y * (16 * RT);
+    const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
+    const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, steps = (min(chunks, c0 + per) - c0) * P;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const uint8_t *code[NT], *power[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t at = (int64_t)min(n0 + 16 * t + c16, a.N - 1) * blocks + g;
+        code[t] = a.codes + at * 16;
+        power[t] = a.scales + at;
+    }
+    const uint16_t* x[XW];
+#pragma unroll
+    for (int i = 0; i < XW; ++i) {
+        const int f = wave * XW + i;   // row tile f / 4, block f % 4 of the chunk; lane (row c, eighth of 64 bytes g)
+        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + c16, a.rows - 1) * a.ld_x + (f & 3) * 32 + g * 8;
+    }
+    int chunk = c0, plane = 0, fill = 0;   // what is requested next, and its place in the ring
+    auto request = [&]() {
+        const uint32_t to = lds0 + fill * STAGE;
+#pragma unroll
+        for (int i = 0; i < XW; ++i) {
+            const int f = wave * XW + i;
+            const void* src = x[i] + plane * a.plane + (int64_t)chunk * 128;
+            if (chunk * 4 + (f & 3) >= blocks) src = &g_mx4_zeros;
+            lds_fetch16(src, to + f * 1024);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const bool on = chunk * 4 + g < blocks;
+            lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, to + C0 + (wave * NT + t) * 1024);
+            lds_fetch1(on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, to + S0 + (wave * NT + t) * 256);
+        }
+        if (++plane == P) plane = 0, ++chunk;
+        if (++fill == ST) fill = 0;
+    };
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < min(ST - 1, steps); ++s) request();
+    int at = 0;
+    for (int s = 0; s < steps; ++s) {
+        // The oldest step has landed for every wave, and every wave is done with the one before, whose place may be written again.
+        __builtin_amdgcn_sched_barrier(0);
+        if (s + ST - 1 <= steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(OPS * (ST - 2)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (s + ST - 1 < steps) request();
+        __builtin_amdgcn_sched_barrier(0);
+        const uint8_t* from = lds + at * STAGE;
+        u32x4_s w[NT];
+        float scale[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            w[t] = *reinterpret_cast<const u32x4_s*>(from + C0 + (wave * NT + t) * 1024 + lane * 16);
+            scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(from + S0 + (wave * NT + t) * 256 + lane * 4));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x8 v[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) v[t] = mx4_values(w[t][j], scale[t]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (j * 16 + c16) * 16);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
+            }
+        }
+        if (++at == ST) at = 0;
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = row0 + 16 * r + c16;
+        if (row >= a.rows) continue;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int n = n0 + 16 * t + 4 * g;
+            if (gridDim.z > 1) store_quad<float>(a, a.part + (int64_t)blockIdx.z * a.rows * a.N, a.N, a.N % 4 == 0, row, n, acc[r][t]);
+            else store_quad<T>(a, (T*)a.out, a.ld_out, a.wide, row, n, acc[r][t]);
+        }
+    }
+}
+
+// Many rows, where the matrix cores are what is short: 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations go
+// through LDS (two steps of 128 k, the next on its way while one is computed on), a wave's codes and powers straight into registers: they are an
+// eighth of what the activations are, and two waves share them through the cache.
+template <class T, int P, int RT, int NT, int WR, int WN>
+__global__ __launch_bounds__(64 * WR * WN) void mx4_tile_kernel(Mx4Args a) {
+    constexpr int XF = RT * WR * 4, XW = XF / (WR * WN);
+    static_assert(XF % (WR * WN) == 0 && 2 * XF * 1024 <= 160 * 1024, "");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * XF * 1024];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    // Workgroups are dealt to the eight XCDs in turn.  Each gets the row tiles of one column tile side by side, whose codes it then reads once.
+    const int col_tiles = (a.N + 16 * NT * WN - 1) / (16 * NT * WN), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR);
+    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    const int col_tile = local / row_tiles * 8 + xcd, row_tile = local % row_tiles;
+    if (col_tile >= col_tiles) return;
+    const int n0 = col_tile * (16 * NT * WN) + (wave % WN) * 16 * NT, row0 = row_tile * (16 * RT * WR), wr = wave / WN;
+    const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
+    const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, steps = (min(chunks, c0 + per) - c0) * P;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const uint8_t *code[NT], *power[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t at = (int64_t)min(n0 + 16 * t + c16, a.N - 1) * blocks + g;
+        code[t] = a.codes + at * 16;
+        power[t] = a.scales + at;
+    }
+    const uint16_t* x[XW];
+#pragma unroll
+    for (int i = 0; i < XW; ++i) {
+        const int f = wave * XW + i;
+        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + c16, a.rows - 1) * a.ld_x + (f & 3) * 32 + g * 8;
+    }
+    int chunk = c0, plane = 0, fill = 0;
+    u32x4_s w[NT];
+    uint32_t pw[NT];
+    auto request = [&]() {
+        const uint32_t to = lds0 + fill * (XF * 1024);
+#pragma unroll
+        for (int i = 0; i < XW; ++i) {
+            const int f = wave * XW + i;
+            const void* src = x[i] + plane * a.plane + (int64_t)chunk * 128;
+            if (chunk * 4 + (f & 3) >= blocks) src = &g_mx4_zeros;
+            lds_fetch16(src, to + f * 1024);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const bool on = chunk * 4 + g < blocks;
+            w[t] = *(on ? reinterpret_cast<const u32x4_s*>(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros);
+            pw[t] = *(on ? power[t] + chunk * 4 : reinterpret_cast<const uint8_t*>(&g_mx4_zeros));
+        }
+        if (++plane == P) plane = 0, ++chunk;
+        fill ^= 1;
+    };
+    f32x4 acc[RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    request();
+    for (int s = 0; s < steps; ++s) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        u32x4_s now[NT];
+        float scale[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            now[t] = w[t];
+            scale[t] = mx4_scale(pw[t]);
+            asm volatile("" : "+v"(now[t]), "+v"(scale[t]));   // what has landed is taken here, in front of the next requests, for which nobody waits yet
+        }
+        if (s + 1 < steps) request();
+        __builtin_amdgcn_sched_barrier(0);
+        const uint8_t* from = lds + (s & 1) * (XF * 1024) + (wr * RT * 4 + g) * 1024 + c16 * 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x8 v[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) v[t] = mx4_values(now[t][j], scale[t]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + r * 4096 + j * 256);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = row0 + 16 * (wr * RT + r) + c16;
+        if (row >= a.rows) continue;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int n = n0 + 16 * t + 4 * g;
+            if (gridDim.z > 1) store_quad<float>(a, a.part + (int64_t)blockIdx.z * a.rows * a.N, a.N, a.N % 4 == 0, row, n, acc[r][t]);
+            else store_quad<T>(a, (T*)a.out, a.ld_out, a.wide, row, n, acc[r][t]);
+        }
+    }
+}
+
+// out = sum of the parts along k, in their order
+template <class T>
+__global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
+    const int64_t total = (int64_t)a.rows * a.N, stride = (int64_t)gridDim.x * 256;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += stride) {
+        float v = a.part[u];
+        for (int z = 1; z < splits; ++z) v += a.part[z * total + u];
+        store_as((T*)a.out + u / a.N * a.ld_out + u % a.N, v);
+    }
+}
+
+struct Mx4Plan {
+    enum { FEW, STREAM, TILE } kind;
+    int rt;        // row tiles of a wave
+    int splits;    // along k
+};
+static Mx4Plan mx4_plan(int N, int K, int rows) {
+    const int chunks = (K + 127) / 128;
+    if (rows <= 16) return Mx4Plan{Mx4Plan::FEW, 1, 1};
+    auto split = [&](long long tiles, int least) {   // parts of at least `least` steps while the chip is not full
+        int s = (int)std::max<long long>(1, std::min<long long>(256 / tiles, chunks / least));
+        s = std::min(s, 16);
+        const int per = (chunks + s - 1) / s;
+        return (chunks + per - 1) / per;   // none of them empty
+    };
+    if (rows <= 128) {
+        const int rt = rows <= 32 ? 2 : rows <= 64 ? 4 : 8, cols = rt == 8 ? 256 : 128;
+        return Mx4Plan{Mx4Plan::STREAM, rt, split((N + cols - 1) / cols, 4)};
+    }
+    const long long tiles = (long long)((N + 255) / 256) * ((rows + 255) / 256);
+    if (tiles >= 192) return Mx4Plan{Mx4Plan::TILE, 8, 1};
+    const long long small = (long long)((N + 127) / 128) * ((rows + 127) / 128);
+    return Mx4Plan{Mx4Plan::TILE, 4, split((small + 1) / 2, 4)};   // two workgroups share a compute unit
+}
+static size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 size_t mx4_linear_workspace(int N, int K, int rows, bool x_f32) {
-    return x_f32 ? (size_t)3 * rows * K * 2 : 0;   // planes of 32-bit activations
+    const int s = mx4_plan(N, K, rows).splits;
+    return (x_f32 ? align256((size_t)3 * rows * K * 2) : 0) + (s > 1 ? (size_t)s * rows * N * 4 : 0);
+}
+// The most that any number of rows up to this takes: within a class of rows that is the largest, and past 128 rows the splits only fall.
+size_t mx4_linear_workspace_up_to(int N, int K, int rows) {
+    size_t most = mx4_linear_workspace(N, K, rows, true);
+    for (int r : {32, 64, 128})
+        if (r < rows) most = std::max(most, mx4_linear_workspace(N, K, r, true));
+    for (int64_t r = 256; r < rows; r += 128) {
+        most = std::max(most, mx4_linear_workspace(N, K, (int)r, true));
+        if (mx4_plan(N, K, (int)r).splits == 1) break;
+    }
+    return most;
 }
 
 template <class T, int P>
-static hipError_t multiply(const Mx4Args& a, hipStream_t st) {
-    const dim3 grid((a.N + 15) / 16, (a.rows + 63) / 64);
-    if (a.rows <= 16) hipLaunchKernelGGL((mx4_linear_kernel<T, P, 1>), dim3(grid.x, 1), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((mx4_linear_kernel<T, P, 4>), grid, dim3(256), 0, st, a);
+static hipError_t multiply(Mx4Args a, hipStream_t st) {
+    const Mx4Plan p = mx4_plan(a.N, a.K, a.rows);
+    a.wide = (uintptr_t)a.out % (4 * sizeof(T)) == 0 && a.ld_out % 4 == 0;
+    if (p.kind == Mx4Plan::FEW) {
+        hipLaunchKernelGGL((mx4_few_kernel<T, P>), dim3((a.N + 15) / 16), dim3(64 * kFewWaves), 0, st, a);
+        return hipGetLastError();
+    }
+    if (p.kind == Mx4Plan::STREAM) {
+        const dim3 grid((a.N + 127) / 128, 1, p.splits), grid8((a.N + 255) / 256, 1, p.splits);
+        if (p.rt == 2) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 2, 2, 4, 6>), grid, dim3(256), 0, st, a);
+        else if (p.rt == 4) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 4, 2, 4, 5>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 2, 8, 3>), grid8, dim3(512), 0, st, a);
+    } else if (p.rt == 8) {
+        const unsigned cols = ((a.N + 255) / 256 + 7) / 8 * 8, rows = (a.rows + 255) / 256;
+        hipLaunchKernelGGL((mx4_tile_kernel<T, P, 8, 4, 2, 4>), dim3(cols * rows, 1, p.splits), dim3(512), 0, st, a);
+    } else {
+        const unsigned cols = ((a.N + 127) / 128 + 7) / 8 * 8, rows = (a.rows + 127) / 128;
+        hipLaunchKernelGGL((mx4_tile_kernel<T, P, 4, 4, 2, 2>), dim3(cols * rows, 1, p.splits), dim3(256), 0, st, a);
+    }
+    if (hipError_t e = hipGetLastError()) return e;
+    if (p.splits > 1) {
+        const int64_t total = (int64_t)a.rows * a.N;
+        hipLaunchKernelGGL(mx4_join_kernel<T>, dim3((unsigned)std::min<int64_t>((total + 255) / 256, 8192)), dim3(256), 0, st, a, p.splits);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_mx4_linear(const Mx4Linear& m, void* workspace, hipStream_t st) {
-    Mx4Args a{m.codes, m.scales, (const uint16_t*)m.x, m.ld_x, 0, m.ld_out, m.N, m.K, m.rows, m.out};
+    Mx4Args a{m.codes, m.scales, (const uint16_t*)m.x, m.ld_x, 0, m.ld_out, m.N, m.K, m.rows, m.out, (float*)workspace, false};
     if (m.x_f32) {
         a.x = (const uint16_t*)workspace;
         a.ld_x = m.K;
         a.plane = (int64_t)m.rows * m.K;
+        a.part = (float*)((char*)workspace + align256((size_t)3 * m.rows * m.K * 2));
         hipLaunchKernelGGL(mx4_planes_kernel, dim3(octet_grid((int64_t)m.rows * (m.K / 8))), dim3(256), 0, st, (const float*)m.x, m.ld_x, m.rows, m.K,
                            (uint16_t*)workspace, a.plane);
         if (hipError_t e = hipGetLastError()) return e;
