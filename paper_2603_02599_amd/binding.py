@@ -517,13 +517,13 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     return _DTYPES[t.dtype]
 
 
-def _want(name: str, t: torch.Tensor, like: torch.Tensor, dtype, shape, rows: bool = False) -> int:
-    """The address of a tensor of this type and shape on the device of `like`: contiguous, or with rows any stride between rows."""
-    if t.dtype is not dtype or tuple(t.shape) != shape:
+def _want(name: str, t: torch.Tensor, device: int, dtype, shape, rows: bool = False) -> int:
+    """The address of a tensor of this type and shape on GPU `device`: contiguous, or with rows any stride between rows."""
+    if t.dtype is not dtype or t.shape != shape:
         _refuse(f"{name} must be {dtype} {shape}, is {t.dtype} {tuple(t.shape)}")
-    if t.device != like.device:
-        _refuse(f"{name} is on {t.device}, not on {like.device}")
-    if not t.is_contiguous() and not (rows and t.stride(1) == 1):
+    if t.get_device() != device:
+        _refuse(f"{name} is on {t.device}, not on GPU {device}")
+    if not (t.is_contiguous() or (rows and t.stride(1) == 1)):
         _refuse(f"{name} must be contiguous" + (" within a row" if rows else ""))
     return t.data_ptr()
 
@@ -532,14 +532,38 @@ def _row_stride(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _call(like: torch.Tensor, stream, fn, *args):
-    """fn(*args, stream) with the GPU of `like` current."""
-    if like.device.type != "cuda":
-        _refuse(f"tensors must be on a GPU, are on {like.device}")
-    if like.device.index == torch.cuda.current_device():
-        return _check(fn(*args, _stream(stream)))
-    with torch.cuda.device(like.device):
-        return _check(fn(*args, _stream(stream)))
+def _workspace(t: torch.Tensor, device: int):
+    if t.get_device() != device or not t.is_contiguous():
+        _refuse(f"workspace must be contiguous and on GPU {device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _gpu(t: torch.Tensor) -> int:
+    device = t.get_device()
+    if device < 0:
+        _refuse(f"tensors must be on a GPU, are on {t.device}")
+    return device
+
+
+def _table(page_tables: torch.Tensor):
+    if page_tables.dim() != 2:
+        _refuse("page_tables must be [requests, max_pages]")
+    return page_tables.shape
+
+
+def _with_flags(fn, flags: int):
+    return lambda *args: fn(*args, flags)
+
+
+def _call(device: int, stream, fn, *args):
+    """fn(*args, stream) with GPU `device` current."""
+    if device == torch._C._cuda_getDevice():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def sun_kv8_pool_bytes(cfg: ModelCfg, n_pages: int, page_tokens: int = 16) -> int:
@@ -551,6 +575,7 @@ class Kv8Pool:
 
     def __init__(self, handle: int, mem: torch.Tensor, cfg: ModelCfg):
         self.handle, self.mem, self.cfg = handle, mem, cfg
+        self.head_dim, self.q_dim, self.kv_dim = cfg.head_dim, cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
 
     def layout(self) -> Kv8Layout:
         return sun_kv8_pool_layout(self)
@@ -580,76 +605,56 @@ def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page
                    stream=None, flags: int = 0):
     """k, v [rows, Hkv*d] (and q [rows, Hq*d], or None with q_out None), rows at any stride; positions, requests int32 [rows];
     page_tables int32 [n_requests, max_pages]; gains [d] of the same type as q, k and v."""
-    c, like = pool.cfg, pool.mem
-    dt, rows = _dtype(k, "k"), k.shape[0]
-    kd, qd = c.n_kv_heads * c.head_dim, c.n_q_heads * c.head_dim
-    if page_tables.dim() != 2:
-        _refuse("page_tables must be [n_requests, max_pages]")
-    n_requests, max_pages = page_tables.shape
-    pk, pv = _want("k", k, like, k.dtype, (rows, kd), True), _want("v", v, like, k.dtype, (rows, kd), True)
-    pq = po = None
-    if q is not None:
-        pq = _want("q", q, like, k.dtype, (rows, qd), True)
-    if q_out is not None:
-        po = _want("q_out", q_out, like, k.dtype, (rows, qd))
-    gains = [None if g is None else _want(n, g, like, k.dtype, (c.head_dim,)) for n, g in (("q_norm", q_norm), ("k_norm", k_norm))]
-    i32 = torch.int32
-    at = (_want("positions", positions, like, i32, (rows,)), _want("requests", requests, like, i32, (rows,)),
-          _want("page_tables", page_tables, like, i32, (n_requests, max_pages)))
-    _call(like, stream, lambda st: lib().sun_kv8_append(
-        pool.handle, layer, rows, dt, pq, _row_stride(q) if q is not None else 0, pk, _row_stride(k), pv, _row_stride(v), *at,
-        n_requests, max_pages, *gains, po, st, flags))
+    dev, dt, t, i32 = _gpu(pool.mem), _dtype(k, "k"), k.dtype, torch.int32
+    rows, (n_requests, max_pages) = k.shape[0], _table(page_tables)
+    _call(dev, stream, _with_flags(lib().sun_kv8_append, flags), pool.handle, layer, rows, dt,
+          None if q is None else _want("q", q, dev, t, (rows, pool.q_dim), True), 0 if q is None else _row_stride(q),
+          _want("k", k, dev, t, (rows, pool.kv_dim), True), _row_stride(k), _want("v", v, dev, t, (rows, pool.kv_dim), True), _row_stride(v),
+          _want("positions", positions, dev, i32, (rows,)), _want("requests", requests, dev, i32, (rows,)),
+          _want("page_tables", page_tables, dev, i32, (n_requests, max_pages)), n_requests, max_pages,
+          None if q_norm is None else _want("q_norm", q_norm, dev, t, (pool.head_dim,)),
+          None if k_norm is None else _want("k_norm", k_norm, dev, t, (pool.head_dim,)),
+          None if q_out is None else _want("q_out", q_out, dev, t, (rows, pool.q_dim)))
 
 
 def sun_kv8_attention_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int) -> int:
     return int(lib().sun_kv8_attention_workspace_bytes(C.byref(cfg), batch, max_pages))
 
 
-def _workspace(t: torch.Tensor, like: torch.Tensor):
-    if t.device != like.device or not t.is_contiguous():
-        _refuse(f"workspace must be contiguous and on {like.device}")
-    return t.data_ptr(), t.numel() * t.element_size()
-
-
 def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, workspace, window: int = 0, stream=None,
                       flags: int = 0):
     """q, out [batch, Hq*d]; page_tables int32 [batch, max_pages]; n_tokens int32 [batch]."""
-    c, like = pool.cfg, pool.mem
-    dt, qd = _dtype(q, "q"), c.n_q_heads * c.head_dim
-    if page_tables.dim() != 2:
-        _refuse("page_tables must be [batch, max_pages]")
-    batch, max_pages = page_tables.shape
-    args = (pool.handle, layer, batch, dt, _want("q", q, like, q.dtype, (batch, qd)),
-            _want("page_tables", page_tables, like, torch.int32, (batch, max_pages)), max_pages,
-            _want("n_tokens", n_tokens, like, torch.int32, (batch,)), window, _want("out", out, like, q.dtype, (batch, qd)),
-            *_workspace(workspace, like))
-    _call(like, stream, lambda st: lib().sun_kv8_attention(*args, st, flags))
+    dev, dt, (batch, max_pages) = _gpu(pool.mem), _dtype(q, "q"), _table(page_tables)
+    _call(dev, stream, _with_flags(lib().sun_kv8_attention, flags), pool.handle, layer, batch, dt,
+          _want("q", q, dev, q.dtype, (batch, pool.q_dim)), _want("page_tables", page_tables, dev, torch.int32, (batch, max_pages)), max_pages,
+          _want("n_tokens", n_tokens, dev, torch.int32, (batch,)), window, _want("out", out, dev, q.dtype, (batch, pool.q_dim)),
+          *_workspace(workspace, dev))
 
 
 def sun_mx4_quantize(w: torch.Tensor, stream=None):
     """Returns (codes uint8 [rows, cols/2], scales uint8 [rows, cols/32])."""
     if w.dim() != 2 or w.shape[1] % 32:
         _refuse("w must be [rows, cols], cols a multiple of 32")
-    rows, cols = w.shape
-    dt, src = _dtype(w, "w"), _want("w", w, w, w.dtype, (rows, cols))
-    codes = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
-    scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=w.device)
-    _call(w, stream, lib().sun_mx4_quantize, src, dt, rows, cols, codes.data_ptr(), scales.data_ptr())
+    (rows, cols), dev = w.shape, _gpu(w)
+    dt, src = _dtype(w, "w"), _want("w", w, dev, w.dtype, w.shape)
+    codes, scales = w.new_empty((rows, cols // 2), dtype=torch.uint8), w.new_empty((rows, cols // 32), dtype=torch.uint8)
+    _call(dev, stream, lib().sun_mx4_quantize, src, dt, rows, cols, codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
-def _mx4(codes: torch.Tensor, scales: torch.Tensor, like: torch.Tensor):
+def _mx4(codes: torch.Tensor, scales: torch.Tensor, device: int):
     if codes.dim() != 2:
         _refuse("codes must be [rows, cols/2]")
-    n, k = codes.shape[0], codes.shape[1] * 2
-    return (_want("codes", codes, like, torch.uint8, (n, k // 2)), _want("scales", scales, like, torch.uint8, (n, k // 32)), n, k)
+    n, half = codes.shape
+    return (_want("codes", codes, device, torch.uint8, (n, half)), _want("scales", scales, device, torch.uint8, (n, half // 16)), n, 2 * half)
 
 
 def sun_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
     """The values [rows, cols], float32 or bfloat16."""
-    pc, ps, n, k = _mx4(codes, scales, codes)
-    out = torch.empty((n, k), dtype=dtype, device=codes.device)
-    _call(codes, stream, lib().sun_mx4_dequantize, pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr())
+    dev = _gpu(codes)
+    pc, ps, n, k = _mx4(codes, scales, dev)
+    out = codes.new_empty((n, k), dtype=dtype)
+    _call(dev, stream, lib().sun_mx4_dequantize, pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr())
     return out
 
 
@@ -659,11 +664,11 @@ def sun_mx4_linear_workspace_bytes(N: int, K: int, rows: int) -> int:
 
 def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):
     """out [rows, N] = x [rows, K] W^T; x and out float32 or bfloat16 each, rows at any stride."""
-    pc, ps, n, k = _mx4(codes, scales, codes)
+    dev = _gpu(codes)
+    pc, ps, n, k = _mx4(codes, scales, dev)
     rows = x.shape[0]
-    px, po = _want("x", x, codes, x.dtype, (rows, k), True), _want("out", out, codes, out.dtype, (rows, n), True)
-    _call(codes, stream, lib().sun_mx4_linear, pc, ps, n, k, rows, px, _dtype(x, "x"), _row_stride(x), po, _dtype(out, "out"),
-          _row_stride(out), *_workspace(workspace, codes))
+    _call(dev, stream, lib().sun_mx4_linear, pc, ps, n, k, rows, _want("x", x, dev, x.dtype, (rows, k), True), _dtype(x, "x"), _row_stride(x),
+          _want("out", out, dev, out.dtype, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev))
 
 
 def sun_hbm_read_probe(src, block_bytes: int, perm, workgroups: int, sink, streaming_loads: bool = False, stream=None):

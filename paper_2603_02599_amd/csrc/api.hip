@@ -1482,6 +1482,7 @@ int sun_kv8_pool_create(const sun_model_cfg* cfg, void* dev_mem, size_t bytes, i
     p->cfg = *cfg;
     p->base = (uint8_t*)dev_mem;
     p->lay = make_kv8_layout(*cfg, n_pages);
+    kv8_thetas(*cfg, p->theta);
     *out = (sun_kv8_pool*)p;
     return SUN_OK;
 }

@@ -274,10 +274,12 @@ struct KvPool {
     std::vector<int64_t> ingested;  // tokens ingested per source model (host side)
 };
 
+constexpr int kKv8Half = 64;   // pairs of a head's rotation at most
 struct Kv8Pool {
     sun_model_cfg cfg;
     uint8_t* base;
     sun_kv8_layout lay;
+    double theta[kKv8Half];    // the rotation's frequencies
 };
 
 enum MatKind { MAT_NONE = 0, MAT_F32 = 1, MAT_BF16_PACKED = 2, MAT_W4_PACKED = 3, MAT_W4_LOGICAL = 4 };

@@ -97,6 +97,7 @@ hipError_t launch_attn_prefill(const KvPool& pool, int layer, const float* q, co
 int attn_prefill_splits(const sun_model_cfg& c, int rows, int first);
 
 // ---------------- the 8-bit cache (kv8.hip) ----------------
+void kv8_thetas(const sun_model_cfg& c, double* theta);
 struct Kv8Rows {   // rows of an append, see sun_kv8_append
     const void *q, *k, *v;
     int64_t ld_q, ld_k, ld_v;

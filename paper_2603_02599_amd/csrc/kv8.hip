@@ -11,7 +11,12 @@
 
 namespace sun {
 
-constexpr int kHalfMax = 64;   // pairs of a head's rotation at most
+void kv8_thetas(const sun_model_cfg& c, double* theta) {
+    EmbedRope e{};
+    e.d = c.head_dim, e.base = c.rope_base;
+    e.rs = RopeScale{c.rope_scaling, c.rope_original_max_position, (double)c.rope_factor, (double)c.rope_low_freq_factor, (double)c.rope_high_freq_factor};
+    for (int j = 0; j < c.head_dim / 2; ++j) theta[j] = rope_theta(e, j);
+}
 
 struct Kv8AppendArgs {
     uint8_t *codes, *scales;   // the layer's
@@ -19,7 +24,7 @@ struct Kv8AppendArgs {
     Kv8Rows r;
     int n_pages, Hq, Hkv, heads_a_block, row_blocks, parts;
     float eps;
-    double theta[kHalfMax];
+    double theta[kKv8Half];
 };
 
 template <class T>
@@ -281,18 +286,15 @@ hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, b
     a.r = r;
     a.n_pages = (int)L.n_pages, a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads;
     a.eps = c.rms_eps;
-    EmbedRope e{};
-    e.d = c.head_dim, e.base = c.rope_base;
-    e.rs = RopeScale{c.rope_scaling, c.rope_original_max_position, (double)c.rope_factor, (double)c.rope_low_freq_factor, (double)c.rope_high_freq_factor};
-    for (int j = 0; j < c.head_dim / 2; ++j) a.theta[j] = rope_theta(e, j);
+    for (int j = 0; j < c.head_dim / 2; ++j) a.theta[j] = pool.theta[j];
     if (f32) return c.head_dim == 128 ? append<float, 128>(a, st) : append<float, 64>(a, st);
     return c.head_dim == 128 ? append<uint16_t, 128>(a, st) : append<uint16_t, 64>(a, st);
 }
 
 // ---------------------------------------------------------------- attention of one new token
 //
-// A wave takes a chunk of one request's tokens for one KV head and walks it 64 tokens (four pages) a step.  With lanes
-// (c = lane % 16, g = lane / 16):
+// A workgroup takes a chunk of one request's tokens for one KV head; its four waves walk it 64 tokens (four pages) a step, in turn, and
+// their results meet in LDS.  With lanes (c = lane % 16, g = lane / 16):
 //   scores  S^T = K Q^T, 16 x 16 x 32: row m of tile t (0..3) is token 4 t + m % 4 of page m / 4, so that lane (c, g) gets the scores
 //           of head c and all sixteen tokens of page g: 4 t + i from register i of tile t.
 //   output  O = P V: the same lane is P's operand for the tokens of page g, and V [dim][token] gives lane (dim, g) those tokens in one load.
@@ -300,15 +302,18 @@ hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, b
 // planes: a weight p is carried as bf16(p) and bf16 of the rest (16 bits together, 24 with a third plane for 32-bit calls), and a 32-bit
 // query as three truncations of 8 bits, which are exact.  Codes become bf16 exactly.  Powers of two are applied to scores and weights.
 // The running maximum and sum are in 32 bits; the sum is over the weights before they are split.
+// A step's keys are requested when the step before has its scores, its values when that has its output, page numbers a step ahead of both.
 
 constexpr int kKv8Step = 64;
-constexpr int kKv8MaxChunk = 512;
+constexpr int kKv8Waves = 4;
+constexpr int kKv8MinChunk = kKv8Step * kKv8Waves, kKv8MaxChunk = 1024;
 
-// Tokens of a chunk: a power of two that gives about 2048 of them over the batch if all requests were like this one.  It depends on the
+// Tokens of a chunk: a power of two that gives about 512 of them over the batch if all requests were like this one.  It depends on the
 // request's own length, the batch size and the heads, so a request's result does not depend on its batch-mates.
+constexpr int kKv8Chunks = 512;
 __host__ __device__ inline int kv8_chunk(int span, int batch, int Hkv) {
-    const long long target = (long long)span * Hkv * batch / 2048;
-    int ch = kKv8Step;
+    const long long target = (long long)span * Hkv * batch / kKv8Chunks;
+    int ch = kKv8MinChunk;
     while (ch < kKv8MaxChunk && 2 * ch <= target) ch *= 2;
     return ch;
 }
@@ -363,28 +368,54 @@ __device__ __forceinline__ void store_as(T* p, float v) {
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
+__global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NH = D / 64, NB = D / 16;   // loads of a key's quarter, dim blocks of the output
-    const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
-    const long long item = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = (int)(item % a.Hkv);
-    const long long rest = item / a.Hkv;
-    const int b = (int)(rest % a.batch), ci = (int)(rest / a.batch);
-    if (ci >= a.chunks) return;
+    __shared__ float part_o[kKv8Waves][kMaxGroup][D];
+    __shared__ float2 part_ml[kKv8Waves][kMaxGroup];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
+    const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.batch, ci = rest / a.batch;
     const Kv8Span s = kv8_span(a, b);
     const int G = a.Hq / a.Hkv;
     if (ci >= s.chunks) {
-        if (ci == 0 && s.chunks == 0)   // nothing to attend to
-            for (int i = lane; i < G * D; i += 64) store_as((T*)a.out + ((int64_t)b * a.Hq + head * G) * D + i, 0.f);
+        if (ci == 0)   // nothing to attend to
+            for (int i = threadIdx.x; i < G * D; i += 64 * kKv8Waves) store_as((T*)a.out + ((int64_t)b * a.Hq + head * G) * D + i, 0.f);
         return;
     }
-    const int begin = s.first + ci * s.chunk, end = min(s.n, begin + s.chunk);
+    const int begin = s.first + ci * s.chunk + wave * kKv8Step, end = min(s.n, s.first + (ci + 1) * s.chunk);
     const int32_t* table = a.page_tables + (int64_t)b * a.max_pages;
 
-    // queries: operand column c, dims 64 h + 16 g + 8 u .. + 7
+    const uint8_t* kb = a.codes + head * a.k_head + (c16 & 3) * D + 16 * g;
+    const uint8_t* vb = a.codes + a.v_off + head * a.v_head + c16 * kPageTokens;
+    const uint8_t* sb = a.scales + head * a.s_head;
+    // Pages of a step: of the lane's key row and of the lane's sixteen tokens.  One that is not there is read as page 0, and left out.
+    struct Pages { int k, v; };
+    auto pages_at = [&](int tok) {
+        const int col = tok / kPageTokens;
+        return Pages{table[min(col + (c16 >> 2), a.max_pages - 1)], table[min(col + g, a.max_pages - 1)]};
+    };
+    auto usable = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+    u32x4_s kr[4][NH], vr[NB], ks, vs;
+    bool there;                           // whether the lane's page of tokens is
+    auto request_k = [&](Pages p) {
+        const uint8_t* kp = kb + (int64_t)(usable(p.k) ? p.k : 0) * a.k_page;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) kr[t][h] = *reinterpret_cast<const u32x4_s*>(kp + 4 * t * D + 64 * h);
+        there = usable(p.v);
+        ks = *reinterpret_cast<const u32x4_s*>(sb + (int64_t)(there ? p.v : 0) * a.s_page);
+    };
+    auto request_v = [&](Pages p) {
+        const int64_t page = usable(p.v) ? p.v : 0;
+        vs = *reinterpret_cast<const u32x4_s*>(sb + a.vs_off + page * a.s_page);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) vr[i] = *reinterpret_cast<const u32x4_s*>(vb + page * a.v_page + i * 16 * kPageTokens);
+    };
+
+    constexpr int STRIDE = kKv8Step * kKv8Waves;
     bf16x8 q0[NH][2], q2[F32 ? NH : 1][2];
-    {
+    auto load_q = [&]() {   // operand column c, dims 64 h + 16 g + 8 u .. + 7
         const int hd = c16 & 7;
         const T* qp = (const T*)a.q + ((int64_t)b * a.Hq + head * G + min(hd, G - 1)) * D + 16 * g;
 #pragma unroll
@@ -416,32 +447,13 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
                     q0[h][u] = __builtin_bit_cast(bf16x8, w);
                 }
             }
-    }
+    };
     f32x4 o[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    const uint8_t* kb = a.codes + head * a.k_head;
-    const uint8_t* vb = a.codes + a.v_off + head * a.v_head;
-    const uint8_t* sb = a.scales + head * a.s_head;
-    auto page_at = [&](int tok, int idx) { return table[min(tok / kPageTokens + idx, a.max_pages - 1)]; };
-    auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
-    for (int tok = begin; tok < end; tok += kKv8Step) {
-        const int pk = page_at(tok, c16 >> 2), pv = page_at(tok, g);
-        const uint8_t* kp = kb + (int64_t)(usable(pk) ? pk : 0) * a.k_page + (c16 & 3) * D + 16 * g;
-        const int64_t pvc = usable(pv) ? pv : 0;
-        const uint8_t* vp = vb + pvc * a.v_page + c16 * kPageTokens;
-        u32x4_s kr[4][NH], vr[NB];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int h = 0; h < NH; ++h) kr[t][h] = *reinterpret_cast<const u32x4_s*>(kp + 4 * t * D + 64 * h);
-        const u32x4_s ks = *reinterpret_cast<const u32x4_s*>(sb + pvc * a.s_page);
-        const u32x4_s vs = *reinterpret_cast<const u32x4_s*>(sb + a.vs_off + pvc * a.s_page);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) vr[i] = *reinterpret_cast<const u32x4_s*>(vp + i * 16 * kPageTokens);
-
+    auto step = [&](int tok, auto more, Pages here) {   // more: a step at `here` follows
         float p[16];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -463,25 +475,18 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
         }
         // tokens outside [lo, end) and of pages that are not there: no weight, and codes and powers that nobody wrote are not used
         const int at = tok + kPageTokens * g;
-        float w[16];
-        const bool whole = __all(usable(pv) && at >= s.lo && at + kPageTokens <= end);
+        const bool whole = __all(there && at >= s.lo && at + kPageTokens <= end);
+        uint32_t live = 0xffff;
         if (!whole) {
-            uint32_t live = 0;
+            live = 0;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const bool on = usable(pv) && at + i >= s.lo && at + i < end;
+                const bool on = there && at + i >= s.lo && at + i < end;
                 live |= (uint32_t)on << i;
                 if (!on) p[i] = -INFINITY;
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t mask = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mask |= (live >> (4 * j + e) & 1) ? 255u << (8 * e) : 0u;
-#pragma unroll
-                for (int i = 0; i < NB; ++i) vr[i][j] &= mask;
-            }
         }
+        if constexpr (decltype(more)::value) request_k(here);
         float top = p[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
@@ -506,11 +511,25 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
             }
         }
         const float mc = m == -INFINITY ? 0.f : m * a.c;
+        float w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], a.c, -mc));
             l += e;
-            w[i] = e == 0.f ? 0.f : e * power(vs[i >> 2], i & 3);
+            w[i] = e * power(vs[i >> 2], i & 3);
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(live >> i & 1)) w[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t mask = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mask |= (live >> (4 * j + e) & 1) ? 255u << (8 * e) : 0u;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) vr[i][j] &= mask;
+            }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -532,8 +551,23 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
                 if constexpr (F32) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w2), v, o[i], 0, 0, 0);
             }
         }
+        if constexpr (decltype(more)::value) request_v(here);
+    };
+    if (begin < end) {   // the last step apart: no register is asked for that is not used
+        Pages next = pages_at(begin);
+        request_k(next);
+        request_v(next);
+        next = pages_at(begin + STRIDE);
+        load_q();
+        int tok = begin;
+        for (; tok + STRIDE < end; tok += STRIDE) {
+            const Pages here = next;
+            next = pages_at(tok + 2 * STRIDE);
+            step(tok, std::true_type{}, here);
+        }
+        step(tok, std::false_type{}, next);
     }
-    // sums of the four pages' lanes, planes of the output, and both to the lanes of heads 4 g + i
+    // sums of the four pages' lanes, planes of the output, and both to LDS by the lanes of heads 4 g + i
     {
         float x = l, y = l;
         swap_rows<16>(x, y);
@@ -542,28 +576,34 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(Kv8AttnArgs a) {
         swap_rows<32>(x, y);
         l = x + y;
     }
+    if (lane < kMaxGroup) part_ml[wave][lane] = float2{m == -INFINITY ? -INFINITY : m * a.c, l};
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] += lane_xor<32>(o[j][i]);
-    const bool one = s.chunks == 1;
+        for (int i = 0; i < 4; ++i) {
+            const float v = o[j][i] + lane_xor<32>(o[j][i]);
+            if (g < 2) part_o[wave][4 * g + i][16 * j + c16] = v;
+        }
+    __syncthreads();
+    const int64_t at0 = ((int64_t)b * a.chunks + ci) * a.Hq + head * G;
+    for (int e = threadIdx.x; e < G * D; e += 64 * kKv8Waves) {
+        const int hd = e / D, dim = e % D;
+        float top = -INFINITY, sum = 0.f, v = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int hd = 4 * g + i;
-        const float sum = __shfl(l, hd & 7), top = __shfl(m, hd & 7);
-        if (g >= 2 || hd >= G) continue;
-        const int64_t h = head * G + hd;
-        if (one) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            T* dst = (T*)a.out + ((int64_t)b * a.Hq + h) * D + c16;
+        for (int w = 0; w < kKv8Waves; ++w) top = fmaxf(top, part_ml[w][hd].x);
+        const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int j = 0; j < NB; ++j) store_as(dst + 16 * j, o[j][i] * inv);
+        for (int w = 0; w < kKv8Waves; ++w) {
+            const float2 ml = part_ml[w][hd];
+            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+            sum += f * ml.y;
+            v += f * part_o[w][hd][dim];
+        }
+        if (s.chunks == 1) {
+            store_as((T*)a.out + ((int64_t)b * a.Hq + head * G) * D + e, sum == 0.f ? 0.f : v / sum);
         } else {
-            const int64_t at = ((int64_t)b * a.chunks + ci) * a.Hq + h;
-#pragma unroll
-            for (int j = 0; j < NB; ++j) a.partial[at * D + 16 * j + c16] = o[j][i];
-            float* ml = a.partial + (int64_t)a.batch * a.chunks * a.Hq * D + at * 2;
-            if (c16 == 0) ml[0] = top * a.c, ml[1] = sum;
+            a.partial[at0 * D + e] = v;
+            if (dim == 0) reinterpret_cast<float2*>(a.partial + (int64_t)a.batch * a.chunks * a.Hq * D)[at0 + hd] = float2{top, sum};
         }
     }
 }
@@ -583,20 +623,31 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnArgs a) {
     for (int c = lane; c < s.chunks; c += 64) top = fmaxf(top, ml[at0 + (int64_t)c * a.Hq].x);
     top = wave_max(top);
     if (top == -INFINITY) top = 0.f;
+    constexpr int U = 8;   // chunks under way at a time
     float sum = 0.f, o[D / 64];
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) o[j] = 0.f;
-    for (int c = 0; c < s.chunks; ++c) {
-        const int64_t at = at0 + (int64_t)c * a.Hq;
-        const float2 p = ml[at];
-        const float w = __builtin_amdgcn_exp2f(p.x - top);
-        sum += w * p.y;
+    for (int c0 = 0; c0 < s.chunks; c0 += U) {
+        float2 p[U];
+        float v[U][D / 64];
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) o[j] += w * a.partial[at * D + 64 * j + lane];
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = at0 + (int64_t)min(c0 + u, s.chunks - 1) * a.Hq;
+            p[u] = ml[at];
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) v[u][j] = a.partial[at * D + 64 * j + lane];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c0 + u >= s.chunks) break;
+            const float w = __builtin_amdgcn_exp2f(p[u].x - top);
+            sum += w * p[u].y;
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) o[j] += w * v[u][j];
+        }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + 64 * j + lane, o[j] * inv);
+    for (int j = 0; j < D / 64; ++j) store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + 64 * j + lane, sum == 0.f ? 0.f : o[j] / sum);
 }
 
 int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window) {
@@ -606,8 +657,8 @@ int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window)
     // within one length of chunk the longest request has the most of them
     long long chunks = 1;
     const long long per = (long long)c.n_kv_heads * batch;
-    for (int ch = kKv8Step; ch <= kKv8MaxChunk; ch *= 2) {
-        const long long last = ch == kKv8MaxChunk ? most : std::min(most, (2ll * ch * 2048 - 1) / per);   // the longest with chunks of at most ch
+    for (int ch = kKv8MinChunk; ch <= kKv8MaxChunk; ch *= 2) {
+        const long long last = ch == kKv8MaxChunk ? most : std::min(most, (2ll * ch * kKv8Chunks - 1) / per);   // the longest with chunks of at most ch
         if (last > 0) chunks = std::max(chunks, (last + ch - 1) / ch);
     }
     return (int)std::min(chunks, 0x7fffffffll);
@@ -618,8 +669,7 @@ size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks) {
 
 template <class T, int D>
 static hipError_t attend(const Kv8AttnArgs& a, hipStream_t st) {
-    const long long items = (long long)a.batch * a.Hkv * a.chunks;
-    hipLaunchKernelGGL((kv8_attn_kernel<T, D>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kv8_attn_kernel<T, D>), dim3((unsigned)((long long)a.batch * a.Hkv * a.chunks)), dim3(64 * kKv8Waves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.chunks > 1)
         hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)(((long long)a.batch * a.Hq + 3) / 4)), dim3(256), 0, st, a);

@@ -152,8 +152,8 @@ def test_attention_refusals(lib, change, status):
 
 
 def chunk(span, batch, hkv):
-    ch = 64
-    while ch < 512 and 2 * ch <= span * hkv * batch // 2048:
+    ch = 256
+    while ch < 1024 and 2 * ch <= span * hkv * batch // 512:
         ch *= 2
     return ch
 
