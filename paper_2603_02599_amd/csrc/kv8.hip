@@ -306,7 +306,7 @@ hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, b
 
 constexpr int kKv8Step = 64;
 constexpr int kKv8Waves = 4;
-constexpr int kKv8MinChunk = kKv8Step * kKv8Waves, kKv8MaxChunk = 1024;
+constexpr int kKv8MinChunk = kKv8Step * kKv8Waves, kKv8MaxChunk = 2048;
 
 // Tokens of a chunk: a power of two that gives about 512 of them over the batch if all requests were like this one.  It depends on the
 // request's own length, the batch size and the heads, so a request's result does not depend on its batch-mates.
@@ -368,7 +368,7 @@ __device__ __forceinline__ void store_as(T* p, float v) {
 }
 
 template <class T, int D>
-__global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a) {
+__global__ __launch_bounds__(64 * kKv8Waves, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NH = D / 64, NB = D / 16;   // loads of a key's quarter, dim blocks of the output
     __shared__ float part_o[kKv8Waves][kMaxGroup][D];
@@ -385,7 +385,11 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
     const int begin = s.first + ci * s.chunk + wave * kKv8Step, end = min(s.n, s.first + (ci + 1) * s.chunk);
     const int32_t* table = a.page_tables + (int64_t)b * a.max_pages;
 
-    const uint8_t* kb = a.codes + head * a.k_head + (c16 & 3) * D + 16 * g;
+    // Keys of 128 dims are read in whole token rows, 128 bytes by a pair of lanes c, c ^ 1 and the four g: register h of both is token 2 (c / 2) + h,
+    // the even lane has dims 16 g .. of it and the odd one 64 + 16 g .., and they exchange before the scores.  Half rows (each lane its own token) cannot be streamed
+    // past the caches without loss.  Keys of 64 dims are whole rows as they are.
+    const bool odd = c16 & 1;
+    const uint8_t* kb = a.codes + head * a.k_head + 16 * g + (NH == 2 ? (c16 & 2) * D + (odd ? 64 : 0) : (c16 & 3) * D);
     const uint8_t* vb = a.codes + a.v_off + head * a.v_head + c16 * kPageTokens;
     const uint8_t* sb = a.scales + head * a.s_head;
     // Pages of a step: of the lane's key row and of the lane's sixteen tokens.  One that is not there is read as page 0, and left out.
@@ -402,7 +406,7 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int h = 0; h < NH; ++h) kr[t][h] = *reinterpret_cast<const u32x4_s*>(kp + 4 * t * D + 64 * h);
+            for (int h = 0; h < NH; ++h) kr[t][h] = load_stream(reinterpret_cast<const u32x4_s*>(kp + (4 * t + (NH == 2 ? h : 0)) * D));
         there = usable(p.v);
         ks = *reinterpret_cast<const u32x4_s*>(sb + (int64_t)(there ? p.v : 0) * a.s_page);
     };
@@ -410,7 +414,7 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
         const int64_t page = usable(p.v) ? p.v : 0;
         vs = *reinterpret_cast<const u32x4_s*>(sb + a.vs_off + page * a.s_page);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) vr[i] = *reinterpret_cast<const u32x4_s*>(vb + page * a.v_page + i * 16 * kPageTokens);
+        for (int i = 0; i < NB; ++i) vr[i] = load_stream(reinterpret_cast<const u32x4_s*>(vb + page * a.v_page + i * 16 * kPageTokens));
     };
 
     constexpr int STRIDE = kKv8Step * kKv8Waves;
@@ -457,7 +461,16 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
         float p[16];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
+            __builtin_amdgcn_sched_barrier(0);   // codes are converted where they are used: all at once they take twice the registers
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (NH == 2) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t r0 = kr[t][0][e], r1 = kr[t][1][e], got = lane_xor<1>(odd ? r0 : r1);
+                    kr[t][0][e] = odd ? got : r0;
+                    kr[t][1][e] = odd ? r1 : got;
+                }
+            }
 #pragma unroll
             for (int h = 0; h < NH; ++h)
 #pragma unroll
@@ -486,7 +499,9 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
                 if (!on) p[i] = -INFINITY;
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) request_k(here);
+        __builtin_amdgcn_sched_barrier(0);
         float top = p[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
@@ -533,6 +548,7 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            __builtin_amdgcn_sched_barrier(0);
             u32x4_s w0, w2;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -551,7 +567,9 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
                 if constexpr (F32) o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w2), v, o[i], 0, 0, 0);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(more)::value) request_v(here);
+        __builtin_amdgcn_sched_barrier(0);
     };
     if (begin < end) {   // the last step apart: no register is asked for that is not used
         Pages next = pages_at(begin);
@@ -608,46 +626,58 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_attn_kernel(Kv8AttnArgs a)
     }
 }
 
-// out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over a request's chunks; a wave a head
+// out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over a request's chunks, a workgroup a head: chunk c is wave c % 4's.  The first
+// partials are requested before their weights are known.
 template <class T, int D>
 __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnArgs a) {
-    const int lane = threadIdx.x & 63;
-    const long long item = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= (long long)a.batch * a.Hq) return;
-    const int b = (int)(item / a.Hq), h = (int)(item % a.Hq);
+    constexpr int W = 4, U = 8, E = D / 64;   // waves, a wave's partials under way at a time, dims of a lane
+    __shared__ float part[W][D];
+    __shared__ float sums[W];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
     const Kv8Span s = kv8_span(a, b);
     if (s.chunks < 2) return;
     const int64_t at0 = (int64_t)b * a.chunks * a.Hq + h;
     const float2* ml = reinterpret_cast<const float2*>(a.partial + (int64_t)a.batch * a.chunks * a.Hq * D);
+    float2 p[U];
+    float v[U][E];
+    auto request = [&](int c0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = at0 + (int64_t)min(c0 + u * W, s.chunks - 1) * a.Hq;
+            p[u] = ml[at];
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[u][j] = a.partial[at * D + 64 * j + lane];
+        }
+    };
+    request(wave);
     float top = -INFINITY;
     for (int c = lane; c < s.chunks; c += 64) top = fmaxf(top, ml[at0 + (int64_t)c * a.Hq].x);
     top = wave_max(top);
     if (top == -INFINITY) top = 0.f;
-    constexpr int U = 8;   // chunks under way at a time
-    float sum = 0.f, o[D / 64];
+    float sum = 0.f, o[E];
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) o[j] = 0.f;
-    for (int c0 = 0; c0 < s.chunks; c0 += U) {
-        float2 p[U];
-        float v[U][D / 64];
+    for (int j = 0; j < E; ++j) o[j] = 0.f;
+    for (int c0 = wave; c0 < s.chunks; c0 += U * W) {
+        if (c0 != wave) request(c0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = at0 + (int64_t)min(c0 + u, s.chunks - 1) * a.Hq;
-            p[u] = ml[at];
-#pragma unroll
-            for (int j = 0; j < D / 64; ++j) v[u][j] = a.partial[at * D + 64 * j + lane];
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (c0 + u >= s.chunks) break;
+            if (c0 + u * W >= s.chunks) break;
             const float w = __builtin_amdgcn_exp2f(p[u].x - top);
             sum += w * p[u].y;
 #pragma unroll
-            for (int j = 0; j < D / 64; ++j) o[j] += w * v[u][j];
+            for (int j = 0; j < E; ++j) o[j] += w * v[u][j];
         }
     }
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + 64 * j + lane, sum == 0.f ? 0.f : o[j] / sum);
+    for (int j = 0; j < E; ++j) part[wave][64 * j + lane] = o[j];
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    const int dim = threadIdx.x;
+    if (dim >= D) return;
+    const float l = ((sums[0] + sums[1]) + sums[2]) + sums[3];
+    const float r = ((part[0][dim] + part[1][dim]) + part[2][dim]) + part[3][dim];
+    store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + dim, l == 0.f ? 0.f : r / l);
 }
 
 int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window) {
@@ -672,7 +702,7 @@ static hipError_t attend(const Kv8AttnArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((kv8_attn_kernel<T, D>), dim3((unsigned)((long long)a.batch * a.Hkv * a.chunks)), dim3(64 * kKv8Waves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.chunks > 1)
-        hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)(((long long)a.batch * a.Hq + 3) / 4)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)(a.batch * a.Hq)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

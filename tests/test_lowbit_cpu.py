@@ -153,7 +153,7 @@ def test_attention_refusals(lib, change, status):
 
 def chunk(span, batch, hkv):
     ch = 256
-    while ch < 1024 and 2 * ch <= span * hkv * batch // 512:
+    while ch < 2048 and 2 * ch <= span * hkv * batch // 512:
         ch *= 2
     return ch
 
