@@ -244,8 +244,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
 }
 
 // Some dozen rows, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Codes, powers and activations of
-// ST - 1 steps of 128 k are under way into LDS while one is computed on; every request takes the place in LDS that the lane reads its operand
-// from, so there are no bank conflicts.  A step is a chunk of k of one plane of the activations.
+// ST - 1 steps of 128 k are under way into LDS while one is computed on.  A step is a chunk of k of one plane of the activations.
+//
+// A request reads 64 bytes of each of sixteen rows, four lanes side by side on a row (the address unit takes four neighbouring lanes on one line
+// at a time; lanes on rows of their own take it four times as long).  In LDS the four pieces of row r are exchanged by r / 4, so that
+// sixteen rows' pieces j, which is what an operand reads, lie on different banks.
 template <class T, int P, int RT, int NT, int WN, int ST>
 __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
     constexpr int XF = RT * 4, CF = NT * WN;                    // operand fragments (1 KiB) of a step: activations, codes
@@ -258,18 +261,19 @@ __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
     const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, steps = (min(chunks, c0 + per) - c0) * P;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const int row16 = lane >> 2, piece = (lane & 3) ^ (lane >> 4);   // what the lane requests of sixteen rows
     const uint8_t *code[NT], *power[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int64_t at = (int64_t)min(n0 + 16 * t + c16, a.N - 1) * blocks + g;
-        code[t] = a.codes + at * 16;
-        power[t] = a.scales + at;
+        const int64_t at = (int64_t)min(n0 + 16 * t + row16, a.N - 1) * blocks;
+        code[t] = a.codes + (at + piece) * 16;
+        power[t] = a.scales + at + (lane & 3);
     }
     const uint16_t* x[XW];
 #pragma unroll
     for (int i = 0; i < XW; ++i) {
-        const int f = wave * XW + i;   // row tile f / 4, block f % 4 of the chunk; lane (row c, eighth of 64 bytes g)
-        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + c16, a.rows - 1) * a.ld_x + (f & 3) * 32 + g * 8;
+        const int f = wave * XW + i;   // row tile f / 4, block f % 4 of the chunk
+        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
     }
     int chunk = c0, plane = 0, fill = 0;   // what is requested next, and its place in the ring
     auto request = [&]() {
@@ -281,11 +285,11 @@ __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
             if (chunk * 4 + (f & 3) >= blocks) src = &g_mx4_zeros;
             lds_fetch16(src, to + f * 1024);
         }
+        const bool on = chunk * 4 + piece < blocks, power_on = chunk * 4 + (lane & 3) < blocks;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const bool on = chunk * 4 + g < blocks;
             lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, to + C0 + (wave * NT + t) * 1024);
-            lds_fetch1(on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, to + S0 + (wave * NT + t) * 256);
+            lds_fetch1(power_on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, to + S0 + (wave * NT + t) * 256);
         }
         if (++plane == P) plane = 0, ++chunk;
         if (++fill == ST) fill = 0;
@@ -309,8 +313,8 @@ __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
         float scale[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            w[t] = *reinterpret_cast<const u32x4_s*>(from + C0 + (wave * NT + t) * 1024 + lane * 16);
-            scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(from + S0 + (wave * NT + t) * 256 + lane * 4));
+            w[t] = *reinterpret_cast<const u32x4_s*>(from + C0 + (wave * NT + t) * 1024 + (c16 * 4 + (g ^ (c16 >> 2))) * 16);
+            scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(from + S0 + (wave * NT + t) * 256 + (c16 * 4 + g) * 4));
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
             for (int t = 0; t < NT; ++t) v[t] = mx4_values(w[t][j], scale[t]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (j * 16 + c16) * 16);
+                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (c16 * 4 + (j ^ (c16 >> 2))) * 16);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
             }
@@ -339,54 +343,54 @@ __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
     }
 }
 
-// Many rows, where the matrix cores are what is short: 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations go
-// through LDS (two steps of 128 k, the next on its way while one is computed on), a wave's codes and powers straight into registers: they are an
-// eighth of what the activations are, and two waves share them through the cache.
+// Many rows, where the matrix cores are what is short: 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations,
+// codes and powers go through LDS as above, the next step's on their way while one is computed on.  Two places for the activations; codes and powers,
+// which a wave takes into registers when it enters the step, have one.
 template <class T, int P, int RT, int NT, int WR, int WN>
-__global__ __launch_bounds__(64 * WR * WN) void mx4_tile_kernel(Mx4Args a) {
-    constexpr int XF = RT * WR * 4, XW = XF / (WR * WN);
-    static_assert(XF % (WR * WN) == 0 && 2 * XF * 1024 <= 160 * 1024, "");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * XF * 1024];
+__global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
+    constexpr int WAVES = WR * WN, XF = RT * WR * 4, XW = XF / WAVES, CF = NT * WN, CW = CF / WAVES;
+    constexpr int C0 = 2 * XF * 1024, S0 = C0 + CF * 1024;
+    static_assert(XF % WAVES == 0 && CF % WAVES == 0 && S0 + CF * 256 <= 160 * 1024, "");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[S0 + CF * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
     // Workgroups are dealt to the eight XCDs in turn.  Each gets the row tiles of one column tile side by side, whose codes it then reads once.
-    const int col_tiles = (a.N + 16 * NT * WN - 1) / (16 * NT * WN), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR);
+    const int col_tiles = (a.N + 16 * CF - 1) / (16 * CF), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR);
     const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
     const int col_tile = local / row_tiles * 8 + xcd, row_tile = local % row_tiles;
     if (col_tile >= col_tiles) return;
-    const int n0 = col_tile * (16 * NT * WN) + (wave % WN) * 16 * NT, row0 = row_tile * (16 * RT * WR), wr = wave / WN;
+    const int n0 = col_tile * (16 * CF), row0 = row_tile * (16 * RT * WR), wr = wave / WN, wn = wave % WN;
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
     const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, steps = (min(chunks, c0 + per) - c0) * P;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    const uint8_t *code[NT], *power[NT];
+    const int row16 = lane >> 2, piece = (lane & 3) ^ (lane >> 4);
+    const uint8_t *code[CW], *power[CW];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t at = (int64_t)min(n0 + 16 * t + c16, a.N - 1) * blocks + g;
-        code[t] = a.codes + at * 16;
-        power[t] = a.scales + at;
+    for (int t = 0; t < CW; ++t) {
+        const int64_t at = (int64_t)min(n0 + 16 * (wave * CW + t) + row16, a.N - 1) * blocks;
+        code[t] = a.codes + (at + piece) * 16;
+        power[t] = a.scales + at + (lane & 3);
     }
     const uint16_t* x[XW];
 #pragma unroll
     for (int i = 0; i < XW; ++i) {
         const int f = wave * XW + i;
-        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + c16, a.rows - 1) * a.ld_x + (f & 3) * 32 + g * 8;
+        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
     }
     int chunk = c0, plane = 0, fill = 0;
-    u32x4_s w[NT];
-    uint32_t pw[NT];
     auto request = [&]() {
         const uint32_t to = lds0 + fill * (XF * 1024);
+        const bool on = chunk * 4 + piece < blocks, power_on = chunk * 4 + (lane & 3) < blocks;
+#pragma unroll
+        for (int t = 0; t < CW; ++t) {
+            lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, lds0 + C0 + (wave * CW + t) * 1024);
+            lds_fetch1(power_on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, lds0 + S0 + (wave * CW + t) * 256);
+        }
 #pragma unroll
         for (int i = 0; i < XW; ++i) {
             const int f = wave * XW + i;
             const void* src = x[i] + plane * a.plane + (int64_t)chunk * 128;
             if (chunk * 4 + (f & 3) >= blocks) src = &g_mx4_zeros;
             lds_fetch16(src, to + f * 1024);
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const bool on = chunk * 4 + g < blocks;
-            w[t] = *(on ? reinterpret_cast<const u32x4_s*>(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros);
-            pw[t] = *(on ? power[t] + chunk * 4 : reinterpret_cast<const uint8_t*>(&g_mx4_zeros));
         }
         if (++plane == P) plane = 0, ++chunk;
         fill ^= 1;
@@ -399,26 +403,27 @@ __global__ __launch_bounds__(64 * WR * WN) void mx4_tile_kernel(Mx4Args a) {
     request();
     for (int s = 0; s < steps; ++s) {
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        u32x4_s now[NT];
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the step has landed for every wave
+        u32x4_s w[NT];
         float scale[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            now[t] = w[t];
-            scale[t] = mx4_scale(pw[t]);
-            asm volatile("" : "+v"(now[t]), "+v"(scale[t]));   // what has landed is taken here, in front of the next requests, for which nobody waits yet
+            w[t] = *reinterpret_cast<const u32x4_s*>(lds + C0 + (wn * NT + t) * 1024 + (c16 * 4 + (g ^ (c16 >> 2))) * 16);
+            scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(lds + S0 + (wn * NT + t) * 256 + (c16 * 4 + g) * 4));
         }
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");            // every wave has its codes, whose place is written next
         if (s + 1 < steps) request();
         __builtin_amdgcn_sched_barrier(0);
-        const uint8_t* from = lds + (s & 1) * (XF * 1024) + (wr * RT * 4 + g) * 1024 + c16 * 16;
+        const uint8_t* from = lds + (s & 1) * (XF * 1024) + (wr * RT * 4 + g) * 1024 + c16 * 64;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             bf16x8 v[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) v[t] = mx4_values(now[t][j], scale[t]);
+            for (int t = 0; t < NT; ++t) v[t] = mx4_values(w[t][j], scale[t]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + r * 4096 + j * 256);
+                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + r * 4096 + (j ^ (c16 >> 2)) * 16);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
             }
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(64 * WR * WN) void mx4_tile_kernel(Mx4Args a) {
         if (row >= a.rows) continue;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int n = n0 + 16 * t + 4 * g;
+            const int n = n0 + 16 * (wn * NT + t) + 4 * g;
             if (gridDim.z > 1) store_quad<float>(a, a.part + (int64_t)blockIdx.z * a.rows * a.N, a.N, a.N % 4 == 0, row, n, acc[r][t]);
             else store_quad<T>(a, (T*)a.out, a.ld_out, a.wide, row, n, acc[r][t]);
         }
