@@ -249,49 +249,52 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
 // A request reads 64 bytes of each of sixteen rows, four lanes side by side on a row (the address unit takes four neighbouring lanes on one line
 // at a time; lanes on rows of their own take it four times as long).  In LDS the four pieces of row r are exchanged by r / 4, so that
 // sixteen rows' pieces j, which is what an operand reads, lie on different banks.
-template <class T, int P, int RT, int NT, int WN, int ST>
-__global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
-    constexpr int XF = RT * 4, CF = NT * WN;                    // operand fragments (1 KiB) of a step: activations, codes
-    constexpr int C0 = XF * 1024, S0 = C0 + CF * 1024, STAGE = S0 + CF * 256;
-    constexpr int XW = XF / WN, OPS = XW + 2 * NT;              // a wave's requests of activations, all of its requests
-    static_assert(XF % WN == 0 && OPS * (ST - 2) < 64 && ST * STAGE <= 160 * 1024, "");
+template <class T, int P, int RT, int NT, int WN, int WK, int WJ, int ST>
+__global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a) {
+    constexpr int XF = RT * 4, CF = NT * WN;                    // operand fragments (1 KiB) of a chunk: activations, codes
+    constexpr int C0 = XF * 1024, S0 = C0 + CF * 1024, CHUNK = S0 + CF * 256, STAGE = WK * CHUNK;
+    constexpr int WC = WN * WJ, XW = XF / WC, CW = CF / WC;     // waves of a chunk, and what one requests of it
+    constexpr int OPS = XW + 2 * CW, J = 4 / WJ;
+    static_assert(XF % WC == 0 && CF % WC == 0 && OPS * (ST - 2) < 64 && ST * STAGE <= 160 * 1024 && WN * RT * NT * 1024 <= ST * STAGE, "");
     __shared__ __attribute__((aligned(16))) uint8_t lds[ST * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * (16 * NT * WN) + wave * 16 * NT, row0 = blockIdx.y * (16 * RT);
+    const int wn = wave % WN, wj = wave / WN % WJ, wk = wave / WC, wq = wave % WC;
+    const int nb = blockIdx.x * (16 * CF), n0 = nb + wn * 16 * NT, row0 = blockIdx.y * (16 * RT);
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
-    const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, steps = (min(chunks, c0 + per) - c0) * P;
+    const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, c1 = min(chunks, c0 + per), steps = (c1 - c0 + WK - 1) / WK * P;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int row16 = lane >> 2, piece = (lane & 3) ^ (lane >> 4);   // what the lane requests of sixteen rows
-    const uint8_t *code[NT], *power[NT];
+    const uint8_t *code[CW], *power[CW];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t at = (int64_t)min(n0 + 16 * t + row16, a.N - 1) * blocks;
+    for (int t = 0; t < CW; ++t) {
+        const int64_t at = (int64_t)min(nb + 16 * (wq * CW + t) + row16, a.N - 1) * blocks;
         code[t] = a.codes + (at + piece) * 16;
         power[t] = a.scales + at + (lane & 3);
     }
     const uint16_t* x[XW];
 #pragma unroll
     for (int i = 0; i < XW; ++i) {
-        const int f = wave * XW + i;   // row tile f / 4, block f % 4 of the chunk
+        const int f = wq * XW + i;   // row tile f / 4, block f % 4 of the chunk
         x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
     }
-    int chunk = c0, plane = 0, fill = 0;   // what is requested next, and its place in the ring
+    int chunk = c0 + wk, plane = 0, fill = 0;   // what is requested next, and its place in the ring
     auto request = [&]() {
-        const uint32_t to = lds0 + fill * STAGE;
+        const uint32_t to = lds0 + fill * STAGE + wk * CHUNK;
+        const int end = chunk < c1 ? blocks : 0;   // behind the last chunk there is nothing
 #pragma unroll
         for (int i = 0; i < XW; ++i) {
-            const int f = wave * XW + i;
+            const int f = wq * XW + i;
             const void* src = x[i] + plane * a.plane + (int64_t)chunk * 128;
-            if (chunk * 4 + (f & 3) >= blocks) src = &g_mx4_zeros;
+            if (chunk * 4 + (f & 3) >= end) src = &g_mx4_zeros;
             lds_fetch16(src, to + f * 1024);
         }
-        const bool on = chunk * 4 + piece < blocks, power_on = chunk * 4 + (lane & 3) < blocks;
+        const bool on = chunk * 4 + piece < end, power_on = chunk * 4 + (lane & 3) < end;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, to + C0 + (wave * NT + t) * 1024);
-            lds_fetch1(power_on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, to + S0 + (wave * NT + t) * 256);
+        for (int t = 0; t < CW; ++t) {
+            lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, to + C0 + (wq * CW + t) * 1024);
+            lds_fetch1(power_on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, to + S0 + (wq * CW + t) * 256);
         }
-        if (++plane == P) plane = 0, ++chunk;
+        if (++plane == P) plane = 0, chunk += WK;
         if (++fill == ST) fill = 0;
     };
     f32x4 acc[RT][NT];
@@ -308,27 +311,60 @@ __global__ __launch_bounds__(64 * WN) void mx4_stream_kernel(Mx4Args a) {
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (s + ST - 1 < steps) request();
         __builtin_amdgcn_sched_barrier(0);
-        const uint8_t* from = lds + at * STAGE;
-        u32x4_s w[NT];
+        const uint8_t* from = lds + at * STAGE + wk * CHUNK;
+        uint32_t w[NT][J];
         float scale[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            w[t] = *reinterpret_cast<const u32x4_s*>(from + C0 + (wave * NT + t) * 1024 + (c16 * 4 + (g ^ (c16 >> 2))) * 16);
-            scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(from + S0 + (wave * NT + t) * 256 + (c16 * 4 + g) * 4));
+            const uint8_t* p = from + C0 + (wn * NT + t) * 1024 + (c16 * 4 + (g ^ (c16 >> 2))) * 16 + wj * J * 4;
+            typedef uint32_t Words __attribute__((ext_vector_type(J == 1 ? 2 : J)));
+            if constexpr (J == 1) {
+                w[t][0] = *reinterpret_cast<const uint32_t*>(p);
+            } else {
+                const Words v = *reinterpret_cast<const Words*>(p);
+#pragma unroll
+                for (int j = 0; j < J; ++j) w[t][j] = v[j];
+            }
+            scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(from + S0 + (wn * NT + t) * 256 + (c16 * 4 + g) * 4));
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < J; ++j) {
             bf16x8 v[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) v[t] = mx4_values(w[t][j], scale[t]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (c16 * 4 + (j ^ (c16 >> 2))) * 16);
+                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (c16 * 4 + ((wj * J + j) ^ (c16 >> 2))) * 16);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
             }
         }
         if (++at == ST) at = 0;
+    }
+    if constexpr (WK * WJ > 1) {   // the sums of the waves that had other parts of k, in their order
+        f32x4* sums = reinterpret_cast<f32x4*>(lds);
+        const int part = wk * WJ + wj;
+        for (int q = 1; q < WK * WJ; ++q) {
+            __syncthreads();
+            if (part == q) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) sums[((wn * RT + r) * NT + t) * 64 + lane] = acc[r][t];
+            }
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const f32x4 v = sums[((wn * RT + r) * NT + t) * 64 + lane];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[r][t][i] += v[i];
+                    }
+            }
+        }
+        if (part > 0) return;
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -468,8 +504,8 @@ static Mx4Plan mx4_plan(int N, int K, int rows) {
         return (chunks + per - 1) / per;   // none of them empty
     };
     if (rows <= 128) {
-        const int rt = rows <= 32 ? 2 : rows <= 64 ? 4 : 8, cols = rt == 8 ? 256 : 128;
-        return Mx4Plan{Mx4Plan::STREAM, rt, split((N + cols - 1) / cols, 4)};
+        const int rt = rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
+        return Mx4Plan{Mx4Plan::STREAM, rt, split((N + 127) / 128, 4)};
     }
     const long long tiles = (long long)((N + 255) / 256) * ((rows + 255) / 256);
     if (tiles >= 192) return Mx4Plan{Mx4Plan::TILE, 8, 1};
@@ -502,10 +538,10 @@ static hipError_t multiply(Mx4Args a, hipStream_t st) {
         return hipGetLastError();
     }
     if (p.kind == Mx4Plan::STREAM) {
-        const dim3 grid((a.N + 127) / 128, 1, p.splits), grid8((a.N + 255) / 256, 1, p.splits);
-        if (p.rt == 2) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 2, 2, 4, 6>), grid, dim3(256), 0, st, a);
-        else if (p.rt == 4) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 4, 2, 4, 5>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 2, 8, 3>), grid8, dim3(512), 0, st, a);
+        const dim3 grid((a.N + 127) / 128, 1, p.splits);
+        if (p.rt == 2) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 2, 4, 2, 2, 2, 4>), grid, dim3(512), 0, st, a);
+        else if (p.rt == 4) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 4, 4, 2, 2, 2, 3>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 4, 2, 1, 4, 3>), grid, dim3(512), 0, st, a);
     } else if (p.rt == 8) {
         const unsigned cols = ((a.N + 255) / 256 + 7) / 8 * 8, rows = (a.rows + 255) / 256;
         hipLaunchKernelGGL((mx4_tile_kernel<T, P, 8, 4, 2, 4>), dim3(cols * rows, 1, p.splits), dim3(512), 0, st, a);
