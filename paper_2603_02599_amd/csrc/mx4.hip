@@ -278,22 +278,28 @@ __global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a
         x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
     }
     int chunk = c0 + wk, plane = 0, fill = 0;   // what is requested next, and its place in the ring
-    auto request = [&]() {
+    // Request i of OPS.  Behind the last chunk zeros are requested, so that every step has the same number of requests under way.
+    auto request = [&](int i) {
         const uint32_t to = lds0 + fill * STAGE + wk * CHUNK;
-        const int end = chunk < c1 ? blocks : 0;   // behind the last chunk there is nothing
-#pragma unroll
-        for (int i = 0; i < XW; ++i) {
+        const int end = chunk < c1 ? blocks : 0;
+        const bool full = chunk * 4 + 4 <= end;
+        const void* src;
+        if (i < XW) {
             const int f = wq * XW + i;
-            const void* src = x[i] + plane * a.plane + (int64_t)chunk * 128;
-            if (chunk * 4 + (f & 3) >= end) src = &g_mx4_zeros;
+            src = x[i] + (plane * a.plane + (int64_t)chunk * 128);
+            if (!full && chunk * 4 + (f & 3) >= end) src = &g_mx4_zeros;
             lds_fetch16(src, to + f * 1024);
+        } else if (i < XW + CW) {
+            src = code[i - XW] + (int64_t)chunk * 64;
+            if (!full && chunk * 4 + piece >= end) src = &g_mx4_zeros;
+            lds_fetch16(src, to + C0 + (wq * CW + i - XW) * 1024);
+        } else {
+            src = power[i - XW - CW] + chunk * 4;
+            if (!full && chunk * 4 + (lane & 3) >= end) src = &g_mx4_zeros;
+            lds_fetch1(src, to + S0 + (wq * CW + i - XW - CW) * 256);
         }
-        const bool on = chunk * 4 + piece < end, power_on = chunk * 4 + (lane & 3) < end;
-#pragma unroll
-        for (int t = 0; t < CW; ++t) {
-            lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, to + C0 + (wq * CW + t) * 1024);
-            lds_fetch1(power_on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, to + S0 + (wq * CW + t) * 256);
-        }
+    };
+    auto requested = [&]() {
         if (++plane == P) plane = 0, chunk += WK;
         if (++fill == ST) fill = 0;
     };
@@ -302,31 +308,36 @@ __global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < min(ST - 1, steps); ++s) request();
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) {
+#pragma unroll
+        for (int i = 0; i < OPS; ++i) request(i);
+        requested();
+    }
     int at = 0;
     for (int s = 0; s < steps; ++s) {
         // The oldest step has landed for every wave, and every wave is done with the one before, whose place may be written again.
         __builtin_amdgcn_sched_barrier(0);
-        if (s + ST - 1 <= steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(OPS * (ST - 2)) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + ST - 1 < steps) request();
-        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(OPS * (ST - 2)) : "memory");
         const uint8_t* from = lds + at * STAGE + wk * CHUNK;
         uint32_t w[NT][J];
         float scale[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const uint8_t* p = from + C0 + (wn * NT + t) * 1024 + (c16 * 4 + (g ^ (c16 >> 2))) * 16 + wj * J * 4;
-            typedef uint32_t Words __attribute__((ext_vector_type(J == 1 ? 2 : J)));
             if constexpr (J == 1) {
                 w[t][0] = *reinterpret_cast<const uint32_t*>(p);
             } else {
+                typedef uint32_t Words __attribute__((ext_vector_type(J)));
                 const Words v = *reinterpret_cast<const Words*>(p);
 #pragma unroll
                 for (int j = 0; j < J; ++j) w[t][j] = v[j];
             }
             scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(from + S0 + (wn * NT + t) * 256 + (c16 * 4 + g) * 4));
         }
+        // The requests of the step that takes the place of the one before stand between the products: all in front of them, they keep the
+        // address unit busy while the matrix cores wait.
+        constexpr int GROUPS = J * RT, EACH = (OPS + GROUPS - 1) / GROUPS;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             bf16x8 v[NT];
@@ -337,10 +348,14 @@ __global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a
                 const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (c16 * 4 + ((wj * J + j) ^ (c16 >> 2))) * 16);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
+#pragma unroll
+                for (int i = (j * RT + r) * EACH; i < min(OPS, (j * RT + r + 1) * EACH); ++i) request(i);
             }
         }
+        requested();
         if (++at == ST) at = 0;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way into LDS any more
     if constexpr (WK * WJ > 1) {   // the sums of the waves that had other parts of k, in their order
         f32x4* sums = reinterpret_cast<f32x4*>(lds);
         const int part = wk * WJ + wj;
@@ -386,7 +401,7 @@ template <class T, int P, int RT, int NT, int WR, int WN>
 __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
     constexpr int WAVES = WR * WN, XF = RT * WR * 4, XW = XF / WAVES, CF = NT * WN, CW = CF / WAVES;
     constexpr int C0 = 2 * XF * 1024, S0 = C0 + CF * 1024;
-    static_assert(XF % WAVES == 0 && CF % WAVES == 0 && S0 + CF * 256 <= 160 * 1024, "");
+    static_assert(2 * CF / WAVES + XF / WAVES <= 4 * RT && XF % WAVES == 0 && CF % WAVES == 0 && S0 + CF * 256 <= 160 * 1024, "");
     __shared__ __attribute__((aligned(16))) uint8_t lds[S0 + CF * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
     // Workgroups are dealt to the eight XCDs in turn.  Each gets the row tiles of one column tile side by side, whose codes it then reads once.
@@ -412,22 +427,29 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
         const int f = wave * XW + i;
         x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
     }
+    const int c1 = min(chunks, c0 + per);
+    constexpr int OPS = 2 * CW + XW;
     int chunk = c0, plane = 0, fill = 0;
-    auto request = [&]() {
-        const uint32_t to = lds0 + fill * (XF * 1024);
-        const bool on = chunk * 4 + piece < blocks, power_on = chunk * 4 + (lane & 3) < blocks;
-#pragma unroll
-        for (int t = 0; t < CW; ++t) {
-            lds_fetch16(on ? (const void*)(code[t] + (int64_t)chunk * 64) : &g_mx4_zeros, lds0 + C0 + (wave * CW + t) * 1024);
-            lds_fetch1(power_on ? (const void*)(power[t] + chunk * 4) : &g_mx4_zeros, lds0 + S0 + (wave * CW + t) * 256);
+    auto request = [&](int i) {
+        const int end = chunk < c1 ? blocks : 0;
+        const bool full = chunk * 4 + 4 <= end;
+        const void* src;
+        if (i < CW) {
+            src = code[i] + (int64_t)chunk * 64;
+            if (!full && chunk * 4 + piece >= end) src = &g_mx4_zeros;
+            lds_fetch16(src, lds0 + C0 + (wave * CW + i) * 1024);
+        } else if (i < 2 * CW) {
+            src = power[i - CW] + chunk * 4;
+            if (!full && chunk * 4 + (lane & 3) >= end) src = &g_mx4_zeros;
+            lds_fetch1(src, lds0 + S0 + (wave * CW + i - CW) * 256);
+        } else {
+            const int f = wave * XW + i - 2 * CW;
+            src = x[i - 2 * CW] + (plane * a.plane + (int64_t)chunk * 128);
+            if (!full && chunk * 4 + (f & 3) >= end) src = &g_mx4_zeros;
+            lds_fetch16(src, lds0 + fill * (XF * 1024) + f * 1024);
         }
-#pragma unroll
-        for (int i = 0; i < XW; ++i) {
-            const int f = wave * XW + i;
-            const void* src = x[i] + plane * a.plane + (int64_t)chunk * 128;
-            if (chunk * 4 + (f & 3) >= blocks) src = &g_mx4_zeros;
-            lds_fetch16(src, to + f * 1024);
-        }
+    };
+    auto requested = [&]() {
         if (++plane == P) plane = 0, ++chunk;
         fill ^= 1;
     };
@@ -436,7 +458,9 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    request();
+#pragma unroll
+    for (int i = 0; i < OPS; ++i) request(i);
+    requested();
     for (int s = 0; s < steps; ++s) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the step has landed for every wave
@@ -449,8 +473,6 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
         }
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");            // every wave has its codes, whose place is written next
-        if (s + 1 < steps) request();
-        __builtin_amdgcn_sched_barrier(0);
         const uint8_t* from = lds + (s & 1) * (XF * 1024) + (wr * RT * 4 + g) * 1024 + c16 * 64;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -462,9 +484,12 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
                 const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + r * 4096 + (j ^ (c16 >> 2)) * 16);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
+                if (j * RT + r < OPS) request(j * RT + r);   // between the products, and early in the step
             }
         }
+        requested();
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing is on its way into LDS any more
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = row0 + 16 * (wr * RT + r) + c16;
