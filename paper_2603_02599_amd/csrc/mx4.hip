@@ -338,19 +338,28 @@ __global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a
         // The requests of the step that takes the place of the one before stand between the products: all in front of them, they keep the
         // address unit busy while the matrix cores wait.
         constexpr int GROUPS = J * RT, EACH = (OPS + GROUPS - 1) / GROUPS;
+        auto rows_at = [&](int q) {   // operand of group q: row tile q % RT, eighth wj * J + q / RT of the blocks
+            return *reinterpret_cast<const bf16x8*>(from + (q % RT * 4 + g) * 1024 + (c16 * 4 + ((wj * J + q / RT) ^ (c16 >> 2))) * 16);
+        };
+        bf16x8 b[GROUPS], v[J][NT];
+        constexpr int AHEAD = 2;       // operands on their way from LDS
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            bf16x8 v[NT];
+        for (int t = 0; t < NT; ++t) v[0][t] = mx4_values(w[t][0], scale[t]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) v[t] = mx4_values(w[t][j], scale[t]);
+        for (int q = 0; q < min(AHEAD, GROUPS); ++q) b[q] = rows_at(q);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + (r * 4 + g) * 1024 + (c16 * 4 + ((wj * J + j) ^ (c16 >> 2))) * 16);
+        for (int q = 0; q < GROUPS; ++q) {
+            if (q + AHEAD < GROUPS) b[q + AHEAD] = rows_at(q + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);   // left to itself the compiler reads an operand in front of its products and waits
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
+            for (int t = 0; t < NT; ++t) acc[q % RT][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q / RT][t], b[q], acc[q % RT][t], 0, 0, 0);
+            // the weights of the next eighth, a column tile at a time
 #pragma unroll
-                for (int i = (j * RT + r) * EACH; i < min(OPS, (j * RT + r + 1) * EACH); ++i) request(i);
-            }
+            for (int t = 0; t < NT; ++t)
+                if (q / RT + 1 < GROUPS / RT && t * RT / NT == q % RT) v[q / RT + 1][t] = mx4_values(w[t][q / RT + 1], scale[t]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = q * EACH; i < min(OPS, (q + 1) * EACH); ++i) request(i);
         }
         requested();
         if (++at == ST) at = 0;
@@ -474,18 +483,26 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");            // every wave has its codes, whose place is written next
         const uint8_t* from = lds + (s & 1) * (XF * 1024) + (wr * RT * 4 + g) * 1024 + c16 * 64;
+        auto rows_at = [&](int q) { return *reinterpret_cast<const bf16x8*>(from + q % RT * 4096 + ((q / RT) ^ (c16 >> 2)) * 16); };
+        constexpr int GROUPS = 4 * RT, AHEAD = 2, EACH = (2 * OPS + GROUPS - 1) / GROUPS;
+        bf16x8 b[GROUPS], v[4][NT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            bf16x8 v[NT];
+        for (int t = 0; t < NT; ++t) v[0][t] = mx4_values(w[t][0], scale[t]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) v[t] = mx4_values(w[t][j], scale[t]);
+        for (int q = 0; q < AHEAD; ++q) b[q] = rows_at(q);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const bf16x8 b = *reinterpret_cast<const bf16x8*>(from + r * 4096 + (j ^ (c16 >> 2)) * 16);
+        for (int q = 0; q < GROUPS; ++q) {
+            if (q + AHEAD < GROUPS) b[q + AHEAD] = rows_at(q + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);   // left to itself the compiler reads an operand in front of its products and waits
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], b, acc[r][t], 0, 0, 0);
-                if (j * RT + r < OPS) request(j * RT + r);   // between the products, and early in the step
-            }
+            for (int t = 0; t < NT; ++t) acc[q % RT][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[q / RT][t], b[q], acc[q % RT][t], 0, 0, 0);
+            // the weights of the next eighth, a column tile at a time
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                if (q / RT + 1 < GROUPS / RT && t * RT / NT == q % RT) v[q / RT + 1][t] = mx4_values(w[t][q / RT + 1], scale[t]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = q * EACH; i < min(OPS, (q + 1) * EACH); ++i) request(i);   // between the products, and early in the step
         }
         requested();
     }
