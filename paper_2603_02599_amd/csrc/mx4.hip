@@ -112,35 +112,56 @@ struct Mx4Args {
     void* out;
     float* part;           // [splits][rows][N], where k is split
     bool wide;             // four columns of out may be stored at once
+    int splits;
 };
 
-// 32-bit activations as their three planes; a lane takes eight
+// Eight 32-bit activations as their three planes.  What is not finite has its value in the first plane and zeros in the others.
+__device__ __forceinline__ void mx4_planes(const float (&v)[8], bf16x8 (&planes)[3]) {
+    u32x4_s w[3];
+    float r[8];
+    bool finite = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        r[i] = v[i];
+        finite &= fabsf(v[i]) < INFINITY;
+    }
+    auto cut = [](float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+    auto plane = [&](int p) {   // the upper halves of two values a word
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[p][j] = __builtin_amdgcn_perm(__float_as_uint(r[2 * j + 1]), __float_as_uint(r[2 * j]), 0x07060302u);
+    };
+    if (!finite) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (v[i] != v[i]) r[i] = __uint_as_float(0x7fc00000u);   // a not-a-number that its upper half says
+    }
+    plane(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = cut(r[i]);
+    if (!finite) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(fabsf(v[i]) < INFINITY)) r[i] = 0.f;
+    }
+    plane(1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = cut(r[i]);
+    plane(2);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) planes[p] = __builtin_bit_cast(bf16x8, w[p]);
+}
+
+// a lane takes eight
 __global__ __launch_bounds__(256) void mx4_planes_kernel(const float* x, int64_t ld_x, int rows, int K, uint16_t* planes, int64_t plane) {
     const int64_t octets = (int64_t)rows * (K / 8), stride = (int64_t)gridDim.x * 256;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < octets; u += stride) {
         const int64_t row = u / (K / 8), k = u % (K / 8) * 8;
         float v[8];
         load8(x + row * ld_x + k, v);
-        u32x4_s w[3];
+        bf16x8 w[3];
+        mx4_planes(v, w);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t word[3] = {0, 0, 0};
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float r = v[2 * j + e];
-                if (r != r) r = __uint_as_float(0x7fc00000u);   // a not-a-number that its upper bits say
-#pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    const uint32_t top = __float_as_uint(r) & 0xffff0000u;
-                    word[p] |= e ? top : top >> 16;
-                    r = fabsf(r) < INFINITY ? r - __uint_as_float(top) : 0.f;
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < 3; ++p) w[p][j] = word[p];
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4_s*>(planes + p * plane + row * K + k) = w[p];
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(planes + p * plane + row * K + k) = w[p];
     }
 }
 
@@ -189,56 +210,94 @@ __device__ __forceinline__ void store_quad(const Mx4Args& a, T* out, int64_t ld,
         if (n + i < a.N) store_as(p + i, v[i]);
 }
 
-// Up to sixteen rows: sixteen columns a workgroup, chunks of 128 k dealt to its eight waves, whose sums meet in LDS.  Lane (c = lane % 16,
-// g = lane / 16) holds column c's block 4 i + g of codes, one 16-byte load, which are four 16 x 16 x 32 products.
+// Up to sixteen rows: 16 * NT columns a workgroup, the chunks of 128 k dealt to its eight waves, whose sums meet in LDS.  A wave has U chunks under
+// way at a time: their codes and powers go into LDS (see the next kernel for the order), its activations straight into the operand's registers: a
+// row that is not there is not asked for.  32-bit activations are cut into their planes here.
 constexpr int kFewWaves = 8;
-template <class T, int P>
+template <class T, class X, int NT, int U>
 __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
-    __shared__ float sums[kFewWaves][16][17];
+    constexpr int P = sizeof(X) == 4 ? 3 : 1, WAVE = U * NT * 1280, SUMS = 16 * (16 * NT + 1) * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kFewWaves * (WAVE > SUMS ? WAVE : SUMS)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16;
-    const int64_t n = min(n0 + c16, a.N - 1);
+    const int n0 = blockIdx.x * (16 * NT), row16 = lane >> 2, piece = (lane & 3) ^ (lane >> 4);
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
-    const uint16_t* xr = a.x + (int64_t)min(c16, a.rows - 1) * a.ld_x;
-    constexpr int U = 4;
-    f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    const uint8_t* mine = lds + wave * WAVE;
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * WAVE;
+    const X* xr = (const X*)a.x + (int64_t)min(c16, a.rows - 1) * a.ld_x;
+    f32x4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int i0 = wave; i0 < chunks; i0 += kFewWaves * U) {
-        u32x4_s code[U];
-        uint32_t power[U];
-        int at[U];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the last chunks' operands were read from is written again
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int chunk = i0 + u * kFewWaves;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int64_t at = (int64_t)min(n0 + 16 * t + row16, a.N - 1) * blocks + chunk * 4;
+                lds_fetch16(chunk * 4 + piece < blocks ? (const void*)(a.codes + (at + piece) * 16) : &g_mx4_zeros, to + (u * NT + t) * 1024);
+                lds_fetch1(chunk * 4 + (lane & 3) < blocks ? (const void*)(a.scales + at + (lane & 3)) : &g_mx4_zeros, to + U * NT * 1024 + (u * NT + t) * 256);
+            }
+        }
+        u32x4_s x[U][4][P == 3 ? 2 : 1];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int blk = (i0 + u * kFewWaves) * 4 + g;
-            at[u] = min(blk, blocks - 1);
-            code[u] = *reinterpret_cast<const u32x4_s*>(a.codes + (n * blocks + at[u]) * 16);
-            power[u] = a.scales[n * blocks + at[u]];
-            if (blk >= blocks) at[u] = -1;
+            const bool on = c16 < a.rows && blk < blocks;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int h = 0; h < (P == 3 ? 2 : 1); ++h) {
+                    x[u][j][h] = u32x4_s{0, 0, 0, 0};
+                    if (on) x[u][j][h] = *reinterpret_cast<const u32x4_s*>(xr + blk * 32 + j * 8 + h * 4);
+                }
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the wave's codes and powers have landed; no other wave reads them
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (i0 + u * kFewWaves >= chunks) break;
-            const bool on = at[u] >= 0;
-            const float scale = on ? mx4_scale(power[u]) : 1.f;
+            u32x4_s w[NT];
+            float scale[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                w[t] = *reinterpret_cast<const u32x4_s*>(mine + (u * NT + t) * 1024 + (c16 * 4 + (g ^ (c16 >> 2))) * 16);
+                scale[t] = mx4_scale(*reinterpret_cast<const uint32_t*>(mine + U * NT * 1024 + (u * NT + t) * 256 + (c16 * 4 + g) * 4));
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bf16x8 w = mx4_values(on ? code[u][j] : 0u, scale);
+                bf16x8 planes[P];
+                if constexpr (P == 3) {
+                    float v[8];
 #pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    const u32x4_s* src = on ? reinterpret_cast<const u32x4_s*>(xr + p * a.plane + at[u] * 32 + j * 8) : &g_mx4_zeros;
-                    acc[j & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, *src), acc[j & 1], 0, 0, 0);
+                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x[u][j][e >> 2][e & 3]);
+                    mx4_planes(v, planes);
+                } else {
+                    planes[0] = __builtin_bit_cast(bf16x8, x[u][j][0]);
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const bf16x8 v = mx4_values(w[t][j], scale[t]);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, planes[p], acc[t], 0, 0, 0);
                 }
             }
         }
     }
-    // register i: column 4 g + i, row c
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sums[wave][c16][4 * g + i] = acc[0][i] + acc[1][i];
+    // register i of tile t: column 16 t + 4 g + i, row c
     __syncthreads();
-    const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
-    if (r < a.rows && r < 16 && n0 + c < a.N) {
+    float* sums = reinterpret_cast<float*>(lds);
+    constexpr int LD = 16 * NT + 1;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[(wave * 16 + c16) * LD + 16 * t + 4 * g + i] = acc[t][i];
+    __syncthreads();
+    for (int u = threadIdx.x; u < a.rows * 16 * NT; u += 64 * kFewWaves) {
+        const int r = u / (16 * NT), c = u % (16 * NT);
+        if (n0 + c >= a.N) continue;
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) v += sums[w][r][c];
+        for (int w = 0; w < kFewWaves; ++w) v += sums[(w * 16 + r) * LD + c];
         store_as((T*)a.out + r * a.ld_out + n0 + c, v);
     }
 }
@@ -403,6 +462,9 @@ __global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a
     }
 }
 
+template <int RT, int NT, int WN, int WK, int WJ, int ST>
+constexpr int mx4_threads() { return 64 * WN * WK * WJ; }
+
 // Many rows, where the matrix cores are what is short: 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations,
 // codes and powers go through LDS as above, the next step's on their way while one is computed on.  Two places for the activations; codes and powers,
 // which a wave takes into registers when it enters the step, have one.
@@ -413,14 +475,15 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
     static_assert(2 * CF / WAVES + XF / WAVES <= 4 * RT && XF % WAVES == 0 && CF % WAVES == 0 && S0 + CF * 256 <= 160 * 1024, "");
     __shared__ __attribute__((aligned(16))) uint8_t lds[S0 + CF * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    // Workgroups are dealt to the eight XCDs in turn.  Each gets the row tiles of one column tile side by side, whose codes it then reads once.
-    const int col_tiles = (a.N + 16 * CF - 1) / (16 * CF), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR);
-    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
-    const int col_tile = local / row_tiles * 8 + xcd, row_tile = local % row_tiles;
-    if (col_tile >= col_tiles) return;
+    // Workgroups are dealt to the eight XCDs in turn.  Each XCD gets an equal run of the tiles with the row tiles of one column tile side by side,
+    // whose codes it then reads once.
+    const int col_tiles = (a.N + 16 * CF - 1) / (16 * CF), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR), tiles = col_tiles * row_tiles;
+    const int at = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (at >= tiles * a.splits) return;
+    const int split = at / tiles, col_tile = at % tiles / row_tiles, row_tile = at % row_tiles;
     const int n0 = col_tile * (16 * CF), row0 = row_tile * (16 * RT * WR), wr = wave / WN, wn = wave % WN;
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
-    const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, steps = (min(chunks, c0 + per) - c0) * P;
+    const int per = (chunks + a.splits - 1) / a.splits, c0 = split * per, steps = (min(chunks, c0 + per) - c0) * P;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     const int row16 = lane >> 2, piece = (lane & 3) ^ (lane >> 4);
     const uint8_t *code[CW], *power[CW];
@@ -514,7 +577,7 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int n = n0 + 16 * (wn * NT + t) + 4 * g;
-            if (gridDim.z > 1) store_quad<float>(a, a.part + (int64_t)blockIdx.z * a.rows * a.N, a.N, a.N % 4 == 0, row, n, acc[r][t]);
+            if (a.splits > 1) store_quad<float>(a, a.part + (int64_t)split * a.rows * a.N, a.N, a.N % 4 == 0, row, n, acc[r][t]);
             else store_quad<T>(a, (T*)a.out, a.ld_out, a.wide, row, n, acc[r][t]);
         }
     }
@@ -531,65 +594,90 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
     }
 }
 
+// How a product is dealt to workgroups.  Times in microseconds, measured on the 8B and 14B shapes' matrices with one plane of activations:
+// a workgroup of the streaming kernel asks for a KiB in 20 cycles and does little else; a step of 128 k of a 256 x 256 tile takes 3.1, of
+// one or two 128 x 128 tiles on a compute unit 1.1 and 1.7; a joining launch 4 and its parts' bytes at 4 TB/s.
+constexpr int kMx4SplitRows = 1 << 17;   // more rows are never split along k
 struct Mx4Plan {
     enum { FEW, STREAM, TILE } kind;
     int rt;        // row tiles of a wave
+    int cols;      // columns of a workgroup
     int splits;    // along k
 };
-static Mx4Plan mx4_plan(int N, int K, int rows) {
+static Mx4Plan mx4_plan(int N, int K, int rows, int planes) {
     const int chunks = (K + 127) / 128;
-    if (rows <= 16) return Mx4Plan{Mx4Plan::FEW, 1, 1};
-    auto split = [&](long long tiles, int least) {   // parts of at least `least` steps while the chip is not full
-        int s = (int)std::max<long long>(1, std::min<long long>(256 / tiles, chunks / least));
-        s = std::min(s, 16);
-        const int per = (chunks + s - 1) / s;
-        return (chunks + per - 1) / per;   // none of them empty
+    if (rows <= 16) return Mx4Plan{Mx4Plan::FEW, 1, N >= 64 * 256 ? 64 : N >= 32 * 256 ? 32 : 16, 1};
+    Mx4Plan best{};
+    double least = 1e30;
+    auto consider = [&](auto kind, int rt, int cols, long long tiles, double step, double step2) {
+        for (int want : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (want > 1 && (want > chunks / 4 || tiles >= 512 || rows > kMx4SplitRows)) break;
+            const int per = (chunks + want - 1) / want, splits = (chunks + per - 1) / per;   // none of them empty
+            if (splits != want) continue;
+            const long long n = (tiles * splits + 255) / 256;   // workgroups of the busiest compute unit
+            double t = (step2 > 0 ? n / 2 * step2 + n % 2 * step : n * step) * per * planes;
+            if (splits > 1) t += 4 + (splits + 1) * (double)rows * N * 4 / 4e6;
+            if (t < least) least = t, best = Mx4Plan{kind, rt, cols, splits};
+        }
     };
     if (rows <= 128) {
         const int rt = rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
-        return Mx4Plan{Mx4Plan::STREAM, rt, split((N + 127) / 128, 4)};
+        for (int cols : {128, 64, 32}) consider(Mx4Plan::STREAM, rt, cols, (N + cols - 1) / cols, (rt * 4 + cols / 8) * 20 / 2400.0, 0);
+    } else {
+        consider(Mx4Plan::TILE, 8, 256, (long long)((N + 255) / 256) * ((rows + 255) / 256), 3.1, 0);
+        consider(Mx4Plan::TILE, 4, 128, (long long)((N + 127) / 128) * ((rows + 127) / 128), 1.1, 1.7);
     }
-    const long long tiles = (long long)((N + 255) / 256) * ((rows + 255) / 256);
-    if (tiles >= 192) return Mx4Plan{Mx4Plan::TILE, 8, 1};
-    const long long small = (long long)((N + 127) / 128) * ((rows + 127) / 128);
-    return Mx4Plan{Mx4Plan::TILE, 4, split((small + 1) / 2, 4)};   // two workgroups share a compute unit
+    return best;
 }
 static size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 size_t mx4_linear_workspace(int N, int K, int rows, bool x_f32) {
-    const int s = mx4_plan(N, K, rows).splits;
-    return (x_f32 ? align256((size_t)3 * rows * K * 2) : 0) + (s > 1 ? (size_t)s * rows * N * 4 : 0);
+    const Mx4Plan p = mx4_plan(N, K, rows, x_f32 ? 3 : 1);
+    if (p.kind == Mx4Plan::FEW) return 0;
+    return (x_f32 ? align256((size_t)3 * rows * K * 2) : 0) + (p.splits > 1 ? (size_t)p.splits * rows * N * 4 : 0);
 }
-// The most that any number of rows up to this takes: within a class of rows that is the largest, and past 128 rows the splits only fall.
+// No less than what any number of rows up to this takes.  Between two of the numbers at which tiles are added, more rows never ask for more parts (what
+// joining costs grows with them), so the parts of the fewest of them and the size of the most are enough.
 size_t mx4_linear_workspace_up_to(int N, int K, int rows) {
-    size_t most = mx4_linear_workspace(N, K, rows, true);
-    for (int r : {32, 64, 128})
-        if (r < rows) most = std::max(most, mx4_linear_workspace(N, K, r, true));
-    for (int64_t r = 256; r < rows; r += 128) {
-        most = std::max(most, mx4_linear_workspace(N, K, (int)r, true));
-        if (mx4_plan(N, K, (int)r).splits == 1) break;
-    }
-    return most;
+    size_t parts = 0;
+    int from = 17;
+    for (int64_t to = 32; from <= std::min(rows, kMx4SplitRows); from = (int)to + 1, to += to < 128 ? to : 128)
+        for (int planes : {1, 3}) {
+            const int s = mx4_plan(N, K, from, planes).splits;
+            if (s > 1) parts = std::max(parts, (size_t)s * (size_t)std::min<int64_t>(to, rows) * N * 4);
+        }
+    return (rows > 16 ? align256((size_t)3 * rows * K * 2) : 0) + parts;
+}
+
+template <class T, class X>
+static hipError_t multiply_few(const Mx4Args& a, int cols, hipStream_t st) {
+    const dim3 grid((a.N + cols - 1) / cols), block(64 * kFewWaves);
+    if (cols == 64) hipLaunchKernelGGL((mx4_few_kernel<T, X, 4, 2>), grid, block, 0, st, a);
+    else if (cols == 32) hipLaunchKernelGGL((mx4_few_kernel<T, X, 2, 2>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((mx4_few_kernel<T, X, 1, 4>), grid, block, 0, st, a);
+    return hipGetLastError();
 }
 
 template <class T, int P>
-static hipError_t multiply(Mx4Args a, hipStream_t st) {
-    const Mx4Plan p = mx4_plan(a.N, a.K, a.rows);
-    a.wide = (uintptr_t)a.out % (4 * sizeof(T)) == 0 && a.ld_out % 4 == 0;
-    if (p.kind == Mx4Plan::FEW) {
-        hipLaunchKernelGGL((mx4_few_kernel<T, P>), dim3((a.N + 15) / 16), dim3(64 * kFewWaves), 0, st, a);
-        return hipGetLastError();
-    }
+static hipError_t multiply(const Mx4Args& a, const Mx4Plan& p, hipStream_t st) {
     if (p.kind == Mx4Plan::STREAM) {
-        const dim3 grid((a.N + 127) / 128, 1, p.splits);
-        if (p.rt == 2) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 2, 4, 2, 2, 2, 4>), grid, dim3(512), 0, st, a);
-        else if (p.rt == 4) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 4, 4, 2, 2, 2, 3>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 4, 2, 1, 4, 3>), grid, dim3(512), 0, st, a);
-    } else if (p.rt == 8) {
-        const unsigned cols = ((a.N + 255) / 256 + 7) / 8 * 8, rows = (a.rows + 255) / 256;
-        hipLaunchKernelGGL((mx4_tile_kernel<T, P, 8, 4, 2, 4>), dim3(cols * rows, 1, p.splits), dim3(512), 0, st, a);
+        const dim3 grid((a.N + p.cols - 1) / p.cols, 1, p.splits);
+        // RT, NT, WN, WK, WJ, ST
+#define SUN_STREAM(...) hipLaunchKernelGGL((mx4_stream_kernel<T, P, __VA_ARGS__>), grid, dim3(mx4_threads<__VA_ARGS__>()), 0, st, a)
+        if (p.rt == 2 && p.cols == 128) SUN_STREAM(2, 4, 2, 2, 2, 4);
+        else if (p.rt == 2 && p.cols == 64) SUN_STREAM(2, 4, 1, 2, 4, 4);
+        else if (p.rt == 2) SUN_STREAM(2, 2, 1, 4, 2, 3);
+        else if (p.rt == 4 && p.cols == 128) SUN_STREAM(4, 4, 2, 2, 2, 3);
+        else if (p.rt == 4 && p.cols == 64) SUN_STREAM(4, 4, 1, 2, 4, 3);
+        else if (p.rt == 4) SUN_STREAM(4, 2, 1, 4, 2, 2);
+        else if (p.cols == 128) SUN_STREAM(8, 4, 2, 1, 4, 3);
+        else if (p.cols == 64) SUN_STREAM(8, 4, 1, 2, 4, 2);
+        else SUN_STREAM(8, 2, 1, 2, 2, 2);
+#undef SUN_STREAM
     } else {
-        const unsigned cols = ((a.N + 127) / 128 + 7) / 8 * 8, rows = (a.rows + 127) / 128;
-        hipLaunchKernelGGL((mx4_tile_kernel<T, P, 4, 4, 2, 2>), dim3(cols * rows, 1, p.splits), dim3(256), 0, st, a);
+        const long long tiles = (long long)((a.N + p.cols - 1) / p.cols) * ((a.rows + p.cols - 1) / p.cols) * p.splits;
+        const dim3 grid((unsigned)((tiles + 7) / 8 * 8));
+        if (p.rt == 8) hipLaunchKernelGGL((mx4_tile_kernel<T, P, 8, 4, 2, 4>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((mx4_tile_kernel<T, P, 4, 4, 2, 2>), grid, dim3(256), 0, st, a);
     }
     if (hipError_t e = hipGetLastError()) return e;
     if (p.splits > 1) {
@@ -600,7 +688,14 @@ static hipError_t multiply(Mx4Args a, hipStream_t st) {
 }
 
 hipError_t launch_mx4_linear(const Mx4Linear& m, void* workspace, hipStream_t st) {
-    Mx4Args a{m.codes, m.scales, (const uint16_t*)m.x, m.ld_x, 0, m.ld_out, m.N, m.K, m.rows, m.out, (float*)workspace, false};
+    const Mx4Plan p = mx4_plan(m.N, m.K, m.rows, m.x_f32 ? 3 : 1);
+    const size_t out_size = m.out_f32 ? 4 : 2;
+    Mx4Args a{m.codes, m.scales, (const uint16_t*)m.x, m.ld_x, 0, m.ld_out, m.N, m.K, m.rows, m.out, (float*)workspace,
+              (uintptr_t)m.out % (4 * out_size) == 0 && m.ld_out % 4 == 0, p.splits};
+    if (p.kind == Mx4Plan::FEW) {
+        if (m.x_f32) return m.out_f32 ? multiply_few<float, float>(a, p.cols, st) : multiply_few<uint16_t, float>(a, p.cols, st);
+        return m.out_f32 ? multiply_few<float, uint16_t>(a, p.cols, st) : multiply_few<uint16_t, uint16_t>(a, p.cols, st);
+    }
     if (m.x_f32) {
         a.x = (const uint16_t*)workspace;
         a.ld_x = m.K;
@@ -609,9 +704,9 @@ hipError_t launch_mx4_linear(const Mx4Linear& m, void* workspace, hipStream_t st
         hipLaunchKernelGGL(mx4_planes_kernel, dim3(octet_grid((int64_t)m.rows * (m.K / 8))), dim3(256), 0, st, (const float*)m.x, m.ld_x, m.rows, m.K,
                            (uint16_t*)workspace, a.plane);
         if (hipError_t e = hipGetLastError()) return e;
-        return m.out_f32 ? multiply<float, 3>(a, st) : multiply<uint16_t, 3>(a, st);
+        return m.out_f32 ? multiply<float, 3>(a, p, st) : multiply<uint16_t, 3>(a, p, st);
     }
-    return m.out_f32 ? multiply<float, 1>(a, st) : multiply<uint16_t, 1>(a, st);
+    return m.out_f32 ? multiply<float, 1>(a, p, st) : multiply<uint16_t, 1>(a, p, st);
 }
 
 }  // namespace sun

@@ -188,8 +188,8 @@ def test_quantize_refusals(lib, args, status):
     (dict(K=63), 2), (dict(rows=0), 2), (dict(x_dtype=2), 2), (dict(out_dtype=-1), 2), (dict(codes=FAKE + 8), 2), (dict(x=FAKE + 4), 2), (dict(ld_x=60), 2),
     (dict(ld_x=66), 2), (dict(x_dtype=1, ld_x=68), 2), (dict(ld_out=99), 2), (dict(out=FAKE + 2), 2), (dict(ws=FAKE + 64), 4), (dict(ws_bytes=8), 4)])
 def test_linear_refusals(lib, change, status):
-    a = dict(codes=FAKE, scales=FAKE, N=100, K=64, rows=5, x=FAKE, x_dtype=0, ld_x=64, out=FAKE, out_dtype=0, ld_out=100, ws=FAKE,
-             ws_bytes=lib.sun_mx4_linear_workspace_bytes(100, 64, 5), stream=None)
+    a = dict(codes=FAKE, scales=FAKE, N=100, K=64, rows=40, x=FAKE, x_dtype=0, ld_x=64, out=FAKE, out_dtype=0, ld_out=100, ws=FAKE,
+             ws_bytes=lib.sun_mx4_linear_workspace_bytes(100, 64, 40), stream=None)
     assert set(change) <= set(a)
     a.update(change)
     assert lib.sun_mx4_linear(*a.values()) == status
@@ -198,6 +198,13 @@ def test_linear_refusals(lib, change, status):
 def test_linear_workspace_sizes(lib):
     assert lib.sun_mx4_linear_workspace_bytes(0, 64, 1) == lib.sun_mx4_linear_workspace_bytes(8, 48, 1) == lib.sun_mx4_linear_workspace_bytes(8, 64, 0) == 0
     assert lib.sun_mx4_linear_workspace_bytes(128256, 16384, 4096) >= 3 * 2 * 16384 * 4096   # sizes past 32 bits
+
+
+@pytest.mark.parametrize("N, K", [(17, 5120), (1000, 4096), (6144, 13824), (28672, 4096)])
+def test_linear_workspace_holds_fewer_rows_too(lib, N, K):
+    """A call with any number of rows finds enough in a workspace made for more: the size never falls as rows are added."""
+    sizes = [lib.sun_mx4_linear_workspace_bytes(N, K, r) for r in range(1, 1200)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
 
 
 def test_binding_refuses_what_does_not_fit():
