@@ -475,12 +475,14 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
     static_assert(2 * CF / WAVES + XF / WAVES <= 4 * RT && XF % WAVES == 0 && CF % WAVES == 0 && S0 + CF * 256 <= 160 * 1024, "");
     __shared__ __attribute__((aligned(16))) uint8_t lds[S0 + CF * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    // Workgroups are dealt to the eight XCDs in turn.  Each XCD gets an equal run of the tiles with the row tiles of one column tile side by side,
-    // whose codes it then reads once.
-    const int col_tiles = (a.N + 16 * CF - 1) / (16 * CF), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR), tiles = col_tiles * row_tiles;
-    const int at = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-    if (at >= tiles * a.splits) return;
-    const int split = at / tiles, col_tile = at % tiles / row_tiles, row_tile = at % row_tiles;
+    // Workgroups are dealt to the eight XCDs in turn.  An XCD gets the row tiles of every eighth column tile, whose codes it then reads once; those of the
+    // last few column tiles are dealt evenly.
+    const int col_tiles = (a.N + 16 * CF - 1) / (16 * CF), row_tiles = (a.rows + 16 * RT * WR - 1) / (16 * RT * WR);
+    const int groups = col_tiles * a.splits, even = groups / 8 * row_tiles, rest = groups % 8 * row_tiles;
+    const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3, late = xcd * ((rest + 7) / 8) + local - even;
+    if (local >= even && late >= min(rest, (xcd + 1) * ((rest + 7) / 8))) return;
+    const int group = local < even ? local / row_tiles * 8 + xcd : groups / 8 * 8 + late / row_tiles;
+    const int row_tile = local < even ? local % row_tiles : late % row_tiles, col_tile = group % col_tiles, split = group / col_tiles;
     const int n0 = col_tile * (16 * CF), row0 = row_tile * (16 * RT * WR), wr = wave / WN, wn = wave % WN;
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
     const int per = (chunks + a.splits - 1) / a.splits, c0 = split * per, steps = (min(chunks, c0 + per) - c0) * P;
@@ -596,7 +598,7 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
 
 // How a product is dealt to workgroups.  Times in microseconds, measured on the 8B and 14B shapes' matrices with one plane of activations:
 // a workgroup of the streaming kernel asks for a KiB in 20 cycles and does little else; a step of 128 k of a 256 x 256 tile takes 3.1, of
-// one or two 128 x 128 tiles on a compute unit 1.1 and 1.7; a joining launch 4 and its parts' bytes at 4 TB/s.
+// one or two 128 x 128 tiles on a compute unit 1.2 and 2.0; a joining launch 4 and its parts' bytes at 4 TB/s.
 constexpr int kMx4SplitRows = 1 << 17;   // more rows are never split along k
 struct Mx4Plan {
     enum { FEW, STREAM, TILE } kind;
@@ -625,7 +627,7 @@ static Mx4Plan mx4_plan(int N, int K, int rows, int planes) {
         for (int cols : {128, 64, 32}) consider(Mx4Plan::STREAM, rt, cols, (N + cols - 1) / cols, (rt * 4 + cols / 8) * 20 / 2400.0, 0);
     } else {
         consider(Mx4Plan::TILE, 8, 256, (long long)((N + 255) / 256) * ((rows + 255) / 256), 3.1, 0);
-        consider(Mx4Plan::TILE, 4, 128, (long long)((N + 127) / 128) * ((rows + 127) / 128), 1.1, 1.7);
+        consider(Mx4Plan::TILE, 4, 128, (long long)((N + 127) / 128) * ((rows + 127) / 128), 1.2, 2.0);
     }
     return best;
 }
@@ -674,8 +676,8 @@ static hipError_t multiply(const Mx4Args& a, const Mx4Plan& p, hipStream_t st) {
         else SUN_STREAM(8, 2, 1, 2, 2, 2);
 #undef SUN_STREAM
     } else {
-        const long long tiles = (long long)((a.N + p.cols - 1) / p.cols) * ((a.rows + p.cols - 1) / p.cols) * p.splits;
-        const dim3 grid((unsigned)((tiles + 7) / 8 * 8));
+        const long long groups = (long long)((a.N + p.cols - 1) / p.cols) * p.splits, rows = (a.rows + p.cols - 1) / p.cols;
+        const dim3 grid((unsigned)(8 * (groups / 8 * rows + (groups % 8 * rows + 7) / 8)));
         if (p.rt == 8) hipLaunchKernelGGL((mx4_tile_kernel<T, P, 8, 4, 2, 4>), grid, dim3(512), 0, st, a);
         else hipLaunchKernelGGL((mx4_tile_kernel<T, P, 4, 4, 2, 2>), grid, dim3(256), 0, st, a);
     }
