@@ -596,9 +596,10 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
     }
 }
 
-// How a product is dealt to workgroups.  Times in microseconds, measured on the 8B and 14B shapes' matrices with one plane of activations:
-// a workgroup of the streaming kernel asks for a KiB in 20 cycles and does little else; a step of 128 k of a 256 x 256 tile takes 3.1, of
-// one or two 128 x 128 tiles on a compute unit 1.2 and 2.0; a joining launch 4 and its parts' bytes at 4 TB/s.
+// How a product is dealt to workgroups.  Times in microseconds, measured on the 8B and 14B shapes' matrices with one plane of activations: a chunk
+// of 128 k takes a streaming workgroup of 128 (64) columns 0.40 (0.28) with 32 rows, 0.60 (0.45) with 64, 0.90 (0.80) with 128; narrower ones were
+// never faster.  A step of 128 k of a 256 x 256 tile takes 3.1, of one or two 128 x 128 tiles on a compute unit 1.2 and 2.0.  A joining
+// launch takes 4 and its parts' bytes at 4 TB/s.
 constexpr int kMx4SplitRows = 1 << 17;   // more rows are never split along k
 struct Mx4Plan {
     enum { FEW, STREAM, TILE } kind;
@@ -624,7 +625,8 @@ static Mx4Plan mx4_plan(int N, int K, int rows, int planes) {
     };
     if (rows <= 128) {
         const int rt = rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
-        for (int cols : {128, 64, 32}) consider(Mx4Plan::STREAM, rt, cols, (N + cols - 1) / cols, (rt * 4 + cols / 8) * 20 / 2400.0, 0);
+        consider(Mx4Plan::STREAM, rt, 128, (N + 127) / 128, rt == 2 ? 0.40 : rt == 4 ? 0.60 : 0.90, 0);
+        consider(Mx4Plan::STREAM, rt, 64, (N + 63) / 64, rt == 2 ? 0.28 : rt == 4 ? 0.45 : 0.80, 0);
     } else {
         consider(Mx4Plan::TILE, 8, 256, (long long)((N + 255) / 256) * ((rows + 255) / 256), 3.1, 0);
         consider(Mx4Plan::TILE, 4, 128, (long long)((N + 127) / 128) * ((rows + 127) / 128), 1.2, 2.0);
@@ -665,15 +667,12 @@ static hipError_t multiply(const Mx4Args& a, const Mx4Plan& p, hipStream_t st) {
         const dim3 grid((a.N + p.cols - 1) / p.cols, 1, p.splits);
         // RT, NT, WN, WK, WJ, ST
 #define SUN_STREAM(...) hipLaunchKernelGGL((mx4_stream_kernel<T, P, __VA_ARGS__>), grid, dim3(mx4_threads<__VA_ARGS__>()), 0, st, a)
-        if (p.rt == 2 && p.cols == 128) SUN_STREAM(2, 4, 2, 2, 2, 4);
-        else if (p.rt == 2 && p.cols == 64) SUN_STREAM(2, 4, 1, 2, 4, 4);
-        else if (p.rt == 2) SUN_STREAM(2, 2, 1, 4, 2, 3);
-        else if (p.rt == 4 && p.cols == 128) SUN_STREAM(4, 4, 2, 2, 2, 3);
-        else if (p.rt == 4 && p.cols == 64) SUN_STREAM(4, 4, 1, 2, 4, 3);
-        else if (p.rt == 4) SUN_STREAM(4, 2, 1, 4, 2, 2);
-        else if (p.cols == 128) SUN_STREAM(8, 4, 2, 1, 4, 3);
-        else if (p.cols == 64) SUN_STREAM(8, 4, 1, 2, 4, 2);
-        else SUN_STREAM(8, 2, 1, 2, 2, 2);
+        if (p.rt == 2 && p.cols == 128) SUN_STREAM(2, 2, 4, 2, 1, 4);
+        else if (p.rt == 2) SUN_STREAM(2, 2, 2, 2, 2, 4);
+        else if (p.rt == 4 && p.cols == 128) SUN_STREAM(4, 2, 4, 2, 1, 3);
+        else if (p.rt == 4) SUN_STREAM(4, 2, 2, 2, 2, 3);
+        else if (p.cols == 128) SUN_STREAM(8, 2, 4, 1, 2, 3);
+        else SUN_STREAM(8, 2, 2, 2, 2, 2);
 #undef SUN_STREAM
     } else {
         const long long groups = (long long)((a.N + p.cols - 1) / p.cols) * p.splits, rows = (a.rows + p.cols - 1) / p.cols;
