@@ -512,24 +512,23 @@ def _refuse(message: str):
 
 
 def _dtype(t: torch.Tensor, name: str) -> int:
-    if t.dtype not in _DTYPES:
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
         _refuse(f"{name} must be float32 or bfloat16, is {t.dtype}")
-    return _DTYPES[t.dtype]
+    return dt
 
 
 def _want(name: str, t: torch.Tensor, device: int, dtype, shape, rows: bool = False) -> int:
     """The address of a tensor of this type and shape on GPU `device`: contiguous, or with rows any stride between rows."""
-    if t.dtype is not dtype or t.shape != shape:
-        _refuse(f"{name} must be {dtype} {shape}, is {t.dtype} {tuple(t.shape)}")
-    if t.get_device() != device:
-        _refuse(f"{name} is on {t.device}, not on GPU {device}")
-    if not (t.is_contiguous() or (rows and t.stride(1) == 1)):
-        _refuse(f"{name} must be contiguous" + (" within a row" if rows else ""))
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and (t.is_contiguous() or (rows and t.stride(1) == 1)):
+        return t.data_ptr()
+    _refuse(f"{name} must be {dtype} {tuple(shape)} on GPU {device}, " + ("contiguous within a row" if rows else "contiguous")
+            + f"; is {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
 def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else cols
 
 
 def _workspace(t: torch.Tensor, device: int):
@@ -551,17 +550,16 @@ def _table(page_tables: torch.Tensor):
     return page_tables.shape
 
 
-def _with_flags(fn, flags: int):
-    return lambda *args: fn(*args, flags)
+_raw_stream = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream(), an object, takes longer than a launch
+_current_gpu = torch._C._cuda_getDevice
 
 
-def _call(device: int, stream, fn, *args):
-    """fn(*args, stream) with GPU `device` current."""
-    if device == torch._C._cuda_getDevice():
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
-    else:
+def _call(device: int, stream, fn, args, behind=()):
+    """fn(*args, stream, *behind) with GPU `device` current."""
+    if device != _current_gpu():
         with torch.cuda.device(device):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream))
+            return _call(device, stream, fn, args, behind)
+    rc = fn(*args, _raw_stream(device) if stream is None else _stream(stream), *behind)
     if rc:
         _check(rc)
 
@@ -605,16 +603,19 @@ def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page
                    stream=None, flags: int = 0):
     """k, v [rows, Hkv*d] (and q [rows, Hq*d], or None with q_out None), rows at any stride; positions, requests int32 [rows];
     page_tables int32 [n_requests, max_pages]; gains [d] of the same type as q, k and v."""
-    dev, dt, t, i32 = _gpu(pool.mem), _dtype(k, "k"), k.dtype, torch.int32
+    dev, t, i32, kd = _gpu(pool.mem), k.dtype, torch.int32, pool.kv_dim
     rows, (n_requests, max_pages) = k.shape[0], _table(page_tables)
-    _call(dev, stream, _with_flags(lib().sun_kv8_append, flags), pool.handle, layer, rows, dt,
-          None if q is None else _want("q", q, dev, t, (rows, pool.q_dim), True), 0 if q is None else _row_stride(q),
-          _want("k", k, dev, t, (rows, pool.kv_dim), True), _row_stride(k), _want("v", v, dev, t, (rows, pool.kv_dim), True), _row_stride(v),
-          _want("positions", positions, dev, i32, (rows,)), _want("requests", requests, dev, i32, (rows,)),
-          _want("page_tables", page_tables, dev, i32, (n_requests, max_pages)), n_requests, max_pages,
-          None if q_norm is None else _want("q_norm", q_norm, dev, t, (pool.head_dim,)),
-          None if k_norm is None else _want("k_norm", k_norm, dev, t, (pool.head_dim,)),
-          None if q_out is None else _want("q_out", q_out, dev, t, (rows, pool.q_dim)))
+    if q is None:
+        pq = lq = None
+    else:
+        pq, lq = _want("q", q, dev, t, (rows, pool.q_dim), True), _row_stride(q)
+    _call(dev, stream, lib().sun_kv8_append, (
+        pool.handle, layer, rows, _dtype(k, "k"), pq, lq or 0, _want("k", k, dev, t, (rows, kd), True), _row_stride(k),
+        _want("v", v, dev, t, (rows, kd), True), _row_stride(v), _want("positions", positions, dev, i32, (rows,)),
+        _want("requests", requests, dev, i32, (rows,)), _want("page_tables", page_tables, dev, i32, (n_requests, max_pages)), n_requests, max_pages,
+        None if q_norm is None else _want("q_norm", q_norm, dev, t, (pool.head_dim,)),
+        None if k_norm is None else _want("k_norm", k_norm, dev, t, (pool.head_dim,)),
+        None if q_out is None else _want("q_out", q_out, dev, t, (rows, pool.q_dim))), (flags,))
 
 
 def sun_kv8_attention_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int) -> int:
@@ -624,11 +625,12 @@ def sun_kv8_attention_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int)
 def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, workspace, window: int = 0, stream=None,
                       flags: int = 0):
     """q, out [batch, Hq*d]; page_tables int32 [batch, max_pages]; n_tokens int32 [batch]."""
-    dev, dt, (batch, max_pages) = _gpu(pool.mem), _dtype(q, "q"), _table(page_tables)
-    _call(dev, stream, _with_flags(lib().sun_kv8_attention, flags), pool.handle, layer, batch, dt,
-          _want("q", q, dev, q.dtype, (batch, pool.q_dim)), _want("page_tables", page_tables, dev, torch.int32, (batch, max_pages)), max_pages,
-          _want("n_tokens", n_tokens, dev, torch.int32, (batch,)), window, _want("out", out, dev, q.dtype, (batch, pool.q_dim)),
-          *_workspace(workspace, dev))
+    dev, t, i32 = _gpu(pool.mem), q.dtype, torch.int32
+    batch, max_pages = _table(page_tables)
+    shape = (batch, pool.q_dim)
+    _call(dev, stream, lib().sun_kv8_attention, (
+        pool.handle, layer, batch, _dtype(q, "q"), _want("q", q, dev, t, shape), _want("page_tables", page_tables, dev, i32, (batch, max_pages)),
+        max_pages, _want("n_tokens", n_tokens, dev, i32, (batch,)), window, _want("out", out, dev, t, shape), *_workspace(workspace, dev)), (flags,))
 
 
 def sun_mx4_quantize(w: torch.Tensor, stream=None):
@@ -636,9 +638,8 @@ def sun_mx4_quantize(w: torch.Tensor, stream=None):
     if w.dim() != 2 or w.shape[1] % 32:
         _refuse("w must be [rows, cols], cols a multiple of 32")
     (rows, cols), dev = w.shape, _gpu(w)
-    dt, src = _dtype(w, "w"), _want("w", w, dev, w.dtype, w.shape)
     codes, scales = w.new_empty((rows, cols // 2), dtype=torch.uint8), w.new_empty((rows, cols // 32), dtype=torch.uint8)
-    _call(dev, stream, lib().sun_mx4_quantize, src, dt, rows, cols, codes.data_ptr(), scales.data_ptr())
+    _call(dev, stream, lib().sun_mx4_quantize, (_want("w", w, dev, w.dtype, w.shape), _dtype(w, "w"), rows, cols, codes.data_ptr(), scales.data_ptr()))
     return codes, scales
 
 
@@ -654,7 +655,7 @@ def sun_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.d
     dev = _gpu(codes)
     pc, ps, n, k = _mx4(codes, scales, dev)
     out = codes.new_empty((n, k), dtype=dtype)
-    _call(dev, stream, lib().sun_mx4_dequantize, pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr())
+    _call(dev, stream, lib().sun_mx4_dequantize, (pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr()))
     return out
 
 
@@ -666,9 +667,10 @@ def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):
     """out [rows, N] = x [rows, K] W^T; x and out float32 or bfloat16 each, rows at any stride."""
     dev = _gpu(codes)
     pc, ps, n, k = _mx4(codes, scales, dev)
-    rows = x.shape[0]
-    _call(dev, stream, lib().sun_mx4_linear, pc, ps, n, k, rows, _want("x", x, dev, x.dtype, (rows, k), True), _dtype(x, "x"), _row_stride(x),
-          _want("out", out, dev, out.dtype, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev))
+    rows, tx, to = x.shape[0], x.dtype, out.dtype
+    _call(dev, stream, lib().sun_mx4_linear, (
+        pc, ps, n, k, rows, _want("x", x, dev, tx, (rows, k), True), _dtype(x, "x"), _row_stride(x),
+        _want("out", out, dev, to, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev)))
 
 
 def sun_hbm_read_probe(src, block_bytes: int, perm, workgroups: int, sink, streaming_loads: bool = False, stream=None):
