@@ -98,23 +98,41 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
     const int rows = a.r.rows;
     if ((int)blockIdx.x < a.row_blocks * a.parts) {
         const int row0 = ((int)blockIdx.x / a.parts) * RG, part = (int)blockIdx.x % a.parts;
-        if (tid < RG * (D / 2)) {
-            const int r = tid / (D / 2), j = tid % (D / 2);
-            const int pos = row0 + r < rows ? a.r.positions[row0 + r] : -1;
-            if (pos >= 0) turn[r][j] = rope_pair(a.theta[j], pos);
-        }
-        __syncthreads();
         const int nq = a.r.q ? a.Hq : 0, heads = nq + a.Hkv, total = heads * min(RG, rows - row0);
         const int sub = lane % LPH, j0 = 4 * sub, group = tid / LPH;
         constexpr int GROUPS = 256 / LPH;
-        for (int base = part * GROUPS; base < total; base += a.parts * GROUPS) {   // the same for all lanes, which read one another
-            const int at = base + group, r = min(at, total - 1) / heads, head = min(at, total - 1) % heads, row = row0 + r;
-            const int pos = a.r.positions[row];
-            const bool live = at < total && pos >= 0, is_q = head < nq;
-            const T* src = is_q ? (const T*)a.r.q + row * a.r.ld_q + head * D : (const T*)a.r.k + row * a.r.ld_k + (head - nq) * D;
-            float x[4], y[4];
+        // Vector `at` of the workgroup's rows; behind the last that one again, which is not stored
+        struct Vec { int r, head, pos; bool live, is_q; };
+        auto vec = [&](int at) {
+            const int i = min(at, total - 1), r = i / heads, head = i % heads, pos = a.r.positions[row0 + r];
+            return Vec{r, head, pos, at < total && pos >= 0, head < nq};
+        };
+        float x[4], y[4];
+        auto load = [&](const Vec& v) {
+            const int64_t row = row0 + v.r;
+            const T* src = v.is_q ? (const T*)a.r.q + row * a.r.ld_q + v.head * D : (const T*)a.r.k + row * a.r.ld_k + (v.head - nq) * D;
             load4(src + j0, x);
             load4(src + D / 2 + j0, y);
+        };
+        Vec v = vec(part * GROUPS + group);
+        load(v);   // on its way while the angles are computed
+        if (tid < RG * (D / 2)) {
+            const int r = tid / (D / 2), j = tid % (D / 2);
+            const int pos = row0 + r < rows ? a.r.positions[row0 + r] : -1;
+            if (pos >= 0) {
+                double sine, cosine;
+                sincos((double)pos * a.theta[j], &sine, &cosine);
+                turn[r][j] = float2{(float)cosine, (float)sine};
+            }
+        }
+        __syncthreads();
+        for (int base = part * GROUPS; base < total; base += a.parts * GROUPS) {   // the same for all lanes, which read one another
+            if (base != part * GROUPS) {
+                v = vec(base + group);
+                load(v);
+            }
+            const int r = v.r, head = v.head, row = row0 + r, pos = v.pos;
+            const bool live = v.live, is_q = v.is_q;
             const T* gain = (const T*)(is_q ? a.r.q_norm : a.r.k_norm);
             float gx[4], gy[4];
             if (gain) {
@@ -188,8 +206,11 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
         return;
     }
     // ---- v: lane (row lane / 4, quarter lane % 4) of 16 rows
-    const int blk = (int)blockIdx.x - a.row_blocks * a.parts, per = (a.Hkv + 3) / 4;
-    const int row0 = (blk / per) * 16, head = (blk % per) * 4 + wave;
+    // Few rows: the four waves of a workgroup have one head, and each stores a quarter of what all four have; a head each otherwise.
+    constexpr bool SHARED = RG == 1;
+    const int blk = (int)blockIdx.x - a.row_blocks * a.parts, per = SHARED ? a.Hkv : (a.Hkv + 3) / 4;
+    const int row0 = (blk / per) * 16, head = SHARED ? blk % per : (blk % per) * 4 + wave;
+    const int share = SHARED ? wave : 0, shares = SHARED ? 4 : 1;
     if (head >= a.Hkv) return;   // a wave is by itself from here on
     constexpr int E = 16 / (int)sizeof(T), NL = D / (4 * E);   // values of a load, loads of a lane
     const int r = lane >> 2, quarter = lane & 3, row = min(row0 + r, rows - 1);
@@ -216,30 +237,30 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
     const int byte = entry_scale(top);
     const float inv = entry_inverse(byte);
     uint8_t* vbase = a.codes + a.v_off + head * a.v_head;
-    if (page >= 0 && quarter == 0) a.scales[a.vs_off + page * a.s_page + head * a.s_head + pos % kPageTokens] = (uint8_t)byte;
-    // Sixteen rows that are consecutive positions of one request and have their pages leave in groups of four tokens; others byte by byte.
-    const int pos0 = __builtin_amdgcn_readfirstlane(pos), req = row0 + r < rows ? a.r.requests[row] : -1;
-    const int req0 = __builtin_amdgcn_readfirstlane(req), count = min(16, rows - row0);
-    const bool run = __all(r >= count || (page >= 0 && req == req0 && pos == pos0 + r));
+    if (page >= 0 && quarter == 0 && share == 0) a.scales[a.vs_off + page * a.s_page + head * a.s_head + pos % kPageTokens] = (uint8_t)byte;
     uint32_t* mine = &vcode[wave][r][0];
 #pragma unroll
     for (int i = 0; i < NL; ++i)
 #pragma unroll
-        for (int h = 0; h < E; h += 4) {
-            const uint32_t w = entry_codes(x[i][h], x[i][h + 1], x[i][h + 2], x[i][h + 3], inv);
-            const int dim = i * 4 * E + quarter * E + h;
-            mine[dim / 4] = w;
-            if (!run && page >= 0) {
-                uint8_t* dst = vbase + page * a.v_page + dim * kPageTokens + pos % kPageTokens;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) dst[b * kPageTokens] = (uint8_t)(w >> (8 * b));
-            }
-        }
-    if (!run) return;
+        for (int h = 0; h < E; h += 4)
+            mine[(i * 4 * E + quarter * E + h) / 4] = entry_codes(x[i][h], x[i][h + 1], x[i][h + 2], x[i][h + 3], inv);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a wave's LDS operations are in order, and other waves use other places
     const uint8_t* got = reinterpret_cast<const uint8_t*>(&vcode[wave][0][0]);
     constexpr int LDR = (D / 4 + 1) * 4;
-    for (int quad = pos0 >> 2; quad <= (pos0 + count - 1) >> 2; ++quad) {
+    // Sixteen rows that are consecutive positions of one request and have their pages leave in groups of four tokens, others byte by byte:
+    // lanes side by side on dims, 16 bytes apart.
+    const int pos0 = __builtin_amdgcn_readfirstlane(pos), req = row0 + r < rows ? a.r.requests[row] : -1;
+    const int req0 = __builtin_amdgcn_readfirstlane(req), count = min(16, rows - row0);
+    if (!__all(r >= count || (page >= 0 && req == req0 && pos == pos0 + r))) {
+        for (int i = share; i < count; i += shares) {
+            const int pg = __shfl(page, i * 4), slot = __shfl(pos, i * 4) & (kPageTokens - 1);
+            if (pg < 0) continue;
+            uint8_t* dst = vbase + pg * a.v_page + slot;
+            for (int dim = lane; dim < D; dim += 64) dst[dim * kPageTokens] = got[i * LDR + dim];
+        }
+        return;
+    }
+    for (int quad = (pos0 >> 2) + share; quad <= (pos0 + count - 1) >> 2; quad += shares) {
         const int t0 = quad * 4 - pos0;   // row of the quad's first token
         const int pg = __shfl(page, min(max(t0, 0), count - 1) * 4);
         uint8_t* dst = vbase + pg * a.v_page + (quad & 3) * 4;
@@ -261,14 +282,17 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
 template <class T, int D>
 static hipError_t append(const Kv8AppendArgs& a0, hipStream_t st) {
     Kv8AppendArgs a = a0;
-    const int rows = a.r.rows, v_blocks = (rows + 15) / 16 * ((a.Hkv + 3) / 4);
+    const int rows = a.r.rows;
     if (rows >= 1024) {
+        const int v_blocks = (rows + 15) / 16 * ((a.Hkv + 3) / 4);
         a.row_blocks = (rows + 3) / 4;
         a.parts = 1;
         hipLaunchKernelGGL((kv8_append_kernel<T, D, 4>), dim3(a.row_blocks * a.parts + v_blocks), dim3(256), 0, st, a);
-    } else {
+    } else {   // a row's heads are shared by as many workgroups as keep one pass each, while there are few rows
+        const int passes = ((a.r.q ? a.Hq : 0) + a.Hkv + 256 / (D / 8) - 1) / (256 / (D / 8));
+        const int v_blocks = (rows + 15) / 16 * a.Hkv;
         a.row_blocks = rows;
-        a.parts = 1;
+        a.parts = rows <= 256 ? passes : 1;
         hipLaunchKernelGGL((kv8_append_kernel<T, D, 1>), dim3(a.row_blocks * a.parts + v_blocks), dim3(256), 0, st, a);
     }
     return hipGetLastError();
