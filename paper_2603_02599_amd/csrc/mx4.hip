@@ -19,84 +19,118 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-}
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
-    *reinterpret_cast<u32x4_s*>(p) = u32x4_s{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
-}
-
 // A lane takes eight columns, four lanes a block: reads and writes are contiguous over the wave.  The matrix is contiguous, so
-// rows do not matter.  The converter rounds to the nearest even code and stops at 6.
-template <class T>
+// rows do not matter.  A workgroup has R runs of 256 octets under way.  The converter rounds to the nearest even code and stops at 6.
+template <class T, int R>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* w, int64_t octets, uint32_t* codes, uint8_t* scales) {
-    const int64_t stride = (int64_t)gridDim.x * 256;
-    for (int64_t u0 = (int64_t)blockIdx.x * 256; u0 < octets; u0 += stride) {
-        const int64_t u = u0 + threadIdx.x;
-        float x[8];
-        load8(w + min(u, octets - 1) * 8, x);
-        float top = 0.f;
-        bool bad = false;
+    const int64_t stride = (int64_t)gridDim.x * 256 * R;
+    for (int64_t u0 = (int64_t)blockIdx.x * 256 * R; u0 < octets; u0 += stride) {
+        float x[R][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            top = fmaxf(top, fabsf(x[i]));
-            bad |= !(fabsf(x[i]) < INFINITY);
-        }
-        if (bad) top = INFINITY;
-        top = fmaxf(top, lane_xor<1>(top));
-        top = fmaxf(top, lane_xor<2>(top));
-        int byte = max((int)(__float_as_uint(top) >> 23) - 2, 0);   // floor(log2) - 2, + 127; the subnormals' is 0 either way
-        const float scale = byte ? __uint_as_float((uint32_t)byte << 23) : 0x1p-127f;
-        uint32_t c = 0;
-        if (top < INFINITY) {
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
-            c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
-        } else {
-            byte = 255;
-        }
-        if (u < octets) {
-            codes[u] = c;
-            if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+        for (int r = 0; r < R; ++r) load8(w + min(u0 + r * 256 + threadIdx.x, octets - 1) * 8, x[r]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t u = u0 + r * 256 + threadIdx.x;
+            float top = 0.f;
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                top = fmaxf(top, fabsf(x[r][i]));
+                bad |= !(fabsf(x[r][i]) < INFINITY);
+            }
+            if (bad) top = INFINITY;
+            top = fmaxf(top, lane_xor<1>(top));
+            top = fmaxf(top, lane_xor<2>(top));
+            int byte = max((int)(__float_as_uint(top) >> 23) - 2, 0);   // floor(log2) - 2, + 127; the subnormals' is 0 either way
+            const float scale = byte ? __uint_as_float((uint32_t)byte << 23) : 0x1p-127f;
+            uint32_t c = 0;
+            if (top < INFINITY) {
+                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][0], x[r][1], scale, 0);
+                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][2], x[r][3], scale, 1);
+                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][4], x[r][5], scale, 2);
+                c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[r][6], x[r][7], scale, 3);
+            } else {
+                byte = 255;
+            }
+            if (u < octets) {
+                codes[u] = c;
+                if ((u & 3) == 0) scales[u >> 2] = (uint8_t)byte;
+            }
         }
     }
 }
+
+// A lane takes sixteen bytes of the output, so that a wave's store is a KiB without gaps, which is what stores past the caches need.
+template <class T, int R, bool STREAM>
+__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int64_t units, T* out) {
+    constexpr int E = 16 / (int)sizeof(T);   // values of a unit
+    typedef std::conditional_t<E == 8, uint32_t, uint16_t> Codes;
+    const int64_t stride = (int64_t)gridDim.x * 256 * R;
+    for (int64_t u0 = (int64_t)blockIdx.x * 256 * R + threadIdx.x; u0 < units; u0 += stride) {
+        uint32_t code[R];
+        int byte[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t u = min(u0 + r * 256, units - 1);
+            code[r] = reinterpret_cast<const Codes*>(codes)[u];
+            byte[r] = scales[u / (kMxBlock / E)];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (u0 + r * 256 >= units) break;
+            const float scale = byte[r] == 255 ? NAN : byte[r] ? __uint_as_float((uint32_t)byte[r] << 23) : 0x1p-127f;
+            float x[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const uint32_t k = (code[r] >> (4 * i)) & 15u, mag = k & 7u;
+                // codes 2 to 7 are (1 + m / 2) 2^(e - 1); 1 is a half
+                float v = mag >= 2 ? __uint_as_float((126u + (mag >> 1)) << 23 | (mag & 1u) << 22) : mag ? 0.5f : 0.f;
+                if (k & 8u) v = -v;
+                x[i] = v * scale;
+            }
+            u32x4_s w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (E == 8) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                else w[i] = __float_as_uint(x[i]);
+            }
+            u32x4_s* to = reinterpret_cast<u32x4_s*>(out) + u0 + r * 256;
+            if constexpr (STREAM) __builtin_nontemporal_store(w, to);
+            else *to = w;
+        }
+    }
+}
+
+// One run to a workgroup while there are few, which then start at once: 2048 x 2048 3.8 / 5.1 us, with four runs 4.4 / 5.7; four where the
+// matrix is large: the values of 28672 x 4096 in bf16 72 -> 58 us.
+constexpr int64_t kMxFewUnits = 1 << 20;
+static unsigned unit_grid(int64_t units, int runs) { return (unsigned)std::min<int64_t>((units + 256 * runs - 1) / (256 * runs), 1 << 16); }
+// Values that the memory-side cache cannot hold beside what they are made from leave past it: those of 28672 x 4096 in bf16 (62 MB to 235)
+// 58 -> 51 us, and the matrix that is read next is still there.  Smaller ones stay in it for whoever reads them.
+constexpr int64_t kMxStreamBytes = (int64_t)256 << 20;
 
 template <class T>
-__global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint32_t* codes, const uint8_t* scales, int64_t octets, T* out) {
-    const int64_t stride = (int64_t)gridDim.x * 256;
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < octets; u += stride) {
-        const uint32_t c = codes[u];
-        const int byte = scales[u >> 2];
-        const float scale = byte == 255 ? NAN : byte ? __uint_as_float((uint32_t)byte << 23) : 0x1p-127f;
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t k = (c >> (4 * i)) & 15u, mag = k & 7u;
-            // codes 2 to 7 are (1 + m / 2) 2^(e - 1); 1 is a half
-            float v = mag >= 2 ? __uint_as_float((126u + (mag >> 1)) << 23 | (mag & 1u) << 22) : mag ? 0.5f : 0.f;
-            if (k & 8u) v = -v;
-            x[i] = v * scale;
-        }
-        store8(out + u * 8, x);
-    }
+static hipError_t quantize(const T* w, int64_t octets, void* codes, void* scales, hipStream_t st) {
+    if (octets <= kMxFewUnits) hipLaunchKernelGGL((mx4_quantize_kernel<T, 1>), dim3(unit_grid(octets, 1)), dim3(256), 0, st, w, octets, (uint32_t*)codes, (uint8_t*)scales);
+    else hipLaunchKernelGGL((mx4_quantize_kernel<T, 4>), dim3(unit_grid(octets, 4)), dim3(256), 0, st, w, octets, (uint32_t*)codes, (uint8_t*)scales);
+    return hipGetLastError();
 }
-
-static unsigned octet_grid(int64_t octets) { return (unsigned)std::min<int64_t>((octets + 255) / 256, 256 * 32); }
+template <class T>
+static hipError_t dequantize(const void* codes, const void* scales, int64_t values, T* out, hipStream_t st) {
+    const int64_t units = values / (16 / (int)sizeof(T));
+    const uint8_t *c = (const uint8_t*)codes, *s = (const uint8_t*)scales;
+    if (units <= kMxFewUnits) hipLaunchKernelGGL((mx4_dequantize_kernel<T, 1, false>), dim3(unit_grid(units, 1)), dim3(256), 0, st, c, s, units, out);
+    else if (values * (int64_t)sizeof(T) + values / 2 <= kMxStreamBytes)
+        hipLaunchKernelGGL((mx4_dequantize_kernel<T, 4, false>), dim3(unit_grid(units, 4)), dim3(256), 0, st, c, s, units, out);
+    else hipLaunchKernelGGL((mx4_dequantize_kernel<T, 4, true>), dim3(unit_grid(units, 4)), dim3(256), 0, st, c, s, units, out);
+    return hipGetLastError();
+}
 
 hipError_t launch_mx4_quantize(const void* w, bool f32, int64_t rows, int64_t cols, void* codes, void* scales, hipStream_t st) {
-    const int64_t octets = rows * (cols / 8);
-    if (f32) hipLaunchKernelGGL(mx4_quantize_kernel<float>, dim3(octet_grid(octets)), dim3(256), 0, st, (const float*)w, octets, (uint32_t*)codes, (uint8_t*)scales);
-    else hipLaunchKernelGGL(mx4_quantize_kernel<uint16_t>, dim3(octet_grid(octets)), dim3(256), 0, st, (const uint16_t*)w, octets, (uint32_t*)codes, (uint8_t*)scales);
-    return hipGetLastError();
+    return f32 ? quantize((const float*)w, rows * (cols / 8), codes, scales, st) : quantize((const uint16_t*)w, rows * (cols / 8), codes, scales, st);
 }
 hipError_t launch_mx4_dequantize(const void* codes, const void* scales, bool f32, int64_t rows, int64_t cols, void* out, hipStream_t st) {
-    const int64_t octets = rows * (cols / 8);
-    if (f32) hipLaunchKernelGGL(mx4_dequantize_kernel<float>, dim3(octet_grid(octets)), dim3(256), 0, st, (const uint32_t*)codes, (const uint8_t*)scales, octets, (float*)out);
-    else hipLaunchKernelGGL(mx4_dequantize_kernel<uint16_t>, dim3(octet_grid(octets)), dim3(256), 0, st, (const uint32_t*)codes, (const uint8_t*)scales, octets, (uint16_t*)out);
-    return hipGetLastError();
+    return f32 ? dequantize(codes, scales, rows * cols, (float*)out, st) : dequantize(codes, scales, rows * cols, (uint16_t*)out, st);
 }
 
 // ---------------------------------------------------------------- product
@@ -702,7 +736,7 @@ hipError_t launch_mx4_linear(const Mx4Linear& m, void* workspace, hipStream_t st
         a.ld_x = m.K;
         a.plane = (int64_t)m.rows * m.K;
         a.part = (float*)((char*)workspace + align256((size_t)3 * m.rows * m.K * 2));
-        hipLaunchKernelGGL(mx4_planes_kernel, dim3(octet_grid((int64_t)m.rows * (m.K / 8))), dim3(256), 0, st, (const float*)m.x, m.ld_x, m.rows, m.K,
+        hipLaunchKernelGGL(mx4_planes_kernel, dim3(unit_grid((int64_t)m.rows * (m.K / 8), 1)), dim3(256), 0, st, (const float*)m.x, m.ld_x, m.rows, m.K,
                            (uint16_t*)workspace, a.plane);
         if (hipError_t e = hipGetLastError()) return e;
         return m.out_f32 ? multiply<float, 3>(a, p, st) : multiply<uint16_t, 3>(a, p, st);
