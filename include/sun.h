@@ -521,7 +521,7 @@ void sun_kv8_pool_destroy(sun_kv8_pool* pool);
  *   dtype      of q, k, v, the gains and q_out: SUN_F32 or SUN_BF16
  *   q          dev [rows, Hq*d], row stride ld_q elements, or NULL with q_out NULL: keys and values alone
  *   k, v       dev [rows, Hkv*d], row strides ld_k, ld_v: not rotated, biases added
- *   positions  dev int32 [rows]: position of the row in its request; < 0: a padding row, which reads and writes nothing
+ *   positions  dev int32 [rows]: position of the row in its request; < 0: a padding row, whose values are not used and which writes nothing
  *   requests   dev int32 [rows]: row of page_tables, in [0, n_requests)
  *   page_tables dev int32 [n_requests, max_pages]
  *   q_norm, k_norm  dev [d]: gains of the head norm (RMSNorm over head_dim, eps = rms_eps, before the rotation); required
@@ -534,8 +534,8 @@ void sun_kv8_pool_destroy(sun_kv8_pool* pool);
  * read by work of another stream meanwhile.
  * With SUN_VALIDATE positions, requests and tables are copied to the host (synchronises) and checked.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, rows < 1, n_requests < 1, max_pages outside [1, 2^26], dtype, a pointer that is not
- * 16-byte aligned, a row stride that is shorter than a row or no multiple of 16 bytes, q and q_out not given together); under
- * SUN_VALIDATE also SUN_ERR_SEQ_LEN (position beyond the table, two rows at one place) and SUN_ERR_PAGE_RANGE (request
+ * 16-byte aligned, a row stride that is shorter than a row or no multiple of 16 bytes, q and q_out not given together,
+ * more rows than one launch takes, which is 2^23 or more for up to 8 KV heads); under SUN_VALIDATE also SUN_ERR_SEQ_LEN (position beyond the table, two rows at one place) and SUN_ERR_PAGE_RANGE (request
  * or page).
  */
 int sun_kv8_append(sun_kv8_pool* pool, int layer, int rows, int dtype, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
@@ -543,7 +543,8 @@ int sun_kv8_append(sun_kv8_pool* pool, int layer, int rows, int dtype, const voi
                    const int32_t* page_tables, int n_requests, int max_pages, const void* q_norm, const void* k_norm,
                    void* q_out, void* stream, unsigned flags);
 
-/* Bytes of device workspace sun_kv8_attention needs for up to `batch` requests with max_pages table columns, any window. */
+/* Bytes of device workspace sun_kv8_attention needs for up to `batch` requests with max_pages table columns, any window; 0 for
+ * sizes that it refuses. */
 size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages);
 
 /*
@@ -559,7 +560,8 @@ size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, in
  * Cached numbers enter exactly; weights of the softmax carry 16 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
  * Under SUN_VALIDATE counts and tables are copied to the host (synchronises) and checked.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, batch outside [1, 1024], max_pages outside [1, 2^26], window < 0, dtype, q or out not
- * 16-byte aligned), SUN_ERR_WORKSPACE (too small or not 256-byte aligned); under SUN_VALIDATE also SUN_ERR_SEQ_LEN and SUN_ERR_PAGE_RANGE.
+ * 16-byte aligned, more requests and tokens than one launch takes: 1024 of 2^20 tokens are taken for up to 8 KV heads), SUN_ERR_WORKSPACE
+ * (too small or not 256-byte aligned); under SUN_VALIDATE also SUN_ERR_SEQ_LEN and SUN_ERR_PAGE_RANGE.
  */
 int sun_kv8_attention(const sun_kv8_pool* pool, int layer, int batch, int dtype, const void* q, const int32_t* page_tables,
                       int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace, size_t workspace_bytes,
@@ -583,7 +585,7 @@ int sun_kv8_attention(const sun_kv8_pool* pool, int layer, int batch, int dtype,
 int sun_mx4_quantize(const void* w, int dtype, int rows, int cols, void* codes, void* scales, void* stream);
 int sun_mx4_dequantize(const void* codes, const void* scales, int rows, int cols, int dtype, void* out, void* stream);
 
-/* Bytes of device workspace sun_mx4_linear needs for a matrix [N, K] and up to `rows` rows, any types. */
+/* Bytes of device workspace sun_mx4_linear needs for a matrix [N, K] and up to `rows` rows, any types; 0 for sizes that it refuses. */
 size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows);
 
 /*
@@ -592,7 +594,8 @@ size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows);
  * Weights and activations enter the matrix cores exactly (32-bit activations as three bf16 planes), sums are in 32 bits; values
  * below the normal numbers of bf16 (2^-126) may count as zero.  A row's result depends on N, K, the row count and the types, not on
  * the other rows' values.  out must not overlap x or the matrix.
- * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (N, rows < 1, K < 32 or no multiple of 32, a type, codes or x not 16-byte aligned, ld_x < K or no
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (N, rows < 1, K < 32 or no multiple of 32, N > 2^28, K or rows > 2^30, more than 2^22 tiles of
+ * 128 x 128 outputs, a type, codes or x not 16-byte aligned, ld_x < K or no
  * multiple of 16 bytes, ld_out < N, out not aligned to its type), SUN_ERR_WORKSPACE (too small or not 256-byte aligned).
  */
 int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x,

@@ -554,6 +554,13 @@ _raw_stream = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream()
 _current_gpu = torch._C._cuda_getDevice
 
 
+def _int32(**values):
+    """Counts that the library takes in 32 bits, which a conversion would cut without a word."""
+    for name, v in values.items():
+        if not -1 << 31 <= v < 1 << 31:
+            _refuse(f"{name} = {v} is beyond 32 bits")
+
+
 def _call(device: int, stream, fn, args, behind=()):
     """fn(*args, stream, *behind) with GPU `device` current."""
     if device != _current_gpu():
@@ -605,6 +612,7 @@ def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page
     page_tables int32 [n_requests, max_pages]; gains [d] of the same type as q, k and v."""
     dev, t, i32, kd = _gpu(pool.mem), k.dtype, torch.int32, pool.kv_dim
     rows, (n_requests, max_pages) = k.shape[0], _table(page_tables)
+    _int32(layer=layer, rows=rows, n_requests=n_requests)
     if q is None:
         pq = lq = None
     else:
@@ -628,6 +636,7 @@ def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, 
     dev, t, i32 = _gpu(pool.mem), q.dtype, torch.int32
     batch, max_pages = _table(page_tables)
     shape = (batch, pool.q_dim)
+    _int32(layer=layer, max_pages=max_pages, window=window)
     _call(dev, stream, lib().sun_kv8_attention, (
         pool.handle, layer, batch, _dtype(q, "q"), _want("q", q, dev, t, shape), _want("page_tables", page_tables, dev, i32, (batch, max_pages)),
         max_pages, _want("n_tokens", n_tokens, dev, i32, (batch,)), window, _want("out", out, dev, t, shape), *_workspace(workspace, dev)), (flags,))
@@ -638,6 +647,7 @@ def sun_mx4_quantize(w: torch.Tensor, stream=None):
     if w.dim() != 2 or w.shape[1] % 32:
         _refuse("w must be [rows, cols], cols a multiple of 32")
     (rows, cols), dev = w.shape, _gpu(w)
+    _int32(rows=rows, cols=cols)
     codes, scales = w.new_empty((rows, cols // 2), dtype=torch.uint8), w.new_empty((rows, cols // 32), dtype=torch.uint8)
     _call(dev, stream, lib().sun_mx4_quantize, (_want("w", w, dev, w.dtype, w.shape), _dtype(w, "w"), rows, cols, codes.data_ptr(), scales.data_ptr()))
     return codes, scales
@@ -647,6 +657,7 @@ def _mx4(codes: torch.Tensor, scales: torch.Tensor, device: int):
     if codes.dim() != 2:
         _refuse("codes must be [rows, cols/2]")
     n, half = codes.shape
+    _int32(rows=n, cols=2 * half)
     return (_want("codes", codes, device, torch.uint8, (n, half)), _want("scales", scales, device, torch.uint8, (n, half // 16)), n, 2 * half)
 
 
@@ -668,6 +679,7 @@ def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):
     dev = _gpu(codes)
     pc, ps, n, k = _mx4(codes, scales, dev)
     rows, tx, to = x.shape[0], x.dtype, out.dtype
+    _int32(rows=rows)
     _call(dev, stream, lib().sun_mx4_linear, (
         pc, ps, n, k, rows, _want("x", x, dev, tx, (rows, k), True), _dtype(x, "x"), _row_stride(x),
         _want("out", out, dev, to, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev)))

@@ -1459,7 +1459,8 @@ static sun_kv8_layout make_kv8_layout(const sun_model_cfg& c, int64_t n_pages) {
     return L;
 }
 
-constexpr int kKv8MaxPages = 1 << 26;  // table columns: positions fit 31 bits
+constexpr int kKv8MaxPages = 1 << 26;     // table columns: positions fit 31 bits
+constexpr int64_t kMaxGroups = 1 << 22;   // workgroups of a launch of these operators: none has more than 512 threads, and a launch holds fewer than 2^32
 
 size_t sun_kv8_pool_bytes(const sun_model_cfg* cfg, int64_t n_pages, int page_tokens) {
     if (!cfg || n_pages < 0 || page_tokens != kPageTokens) return 0;
@@ -1543,6 +1544,7 @@ int sun_kv8_append(sun_kv8_pool* pool_, int layer, int rows, int dtype, const vo
         return fail(SUN_ERR_SHAPE, "row strides must be at least a row and multiples of 16 bytes");
     if (q && q == q_out && ld_q != qd) return fail(SUN_ERR_SHAPE, "q_out may be q only where q is contiguous");
     const Kv8Rows r{q, k, v, ld_q, ld_k, ld_v, positions, requests, page_tables, rows, n_requests, max_pages, q_norm, k_norm, q_out};
+    if (kv8_append_groups(c, r) > kMaxGroups) return fail(SUN_ERR_SHAPE, "%d rows are more than one launch takes", rows);
     hipStream_t st = (hipStream_t)stream;
     if (flags & SUN_VALIDATE)
         if (int rc = guarded([&] { return validate_kv8_rows(pool, r, st); })) return rc;
@@ -1550,9 +1552,17 @@ int sun_kv8_append(sun_kv8_pool* pool_, int layer, int rows, int dtype, const vo
     return SUN_OK;
 }
 
+constexpr int kKv8MaxBatch = 1024;
+static bool kv8_attention_fits(const sun_model_cfg& c, int batch, int chunks) {
+    return (int64_t)batch * std::max<int64_t>(c.n_q_heads, (int64_t)c.n_kv_heads * chunks) <= kMaxGroups;
+}
+
 size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages) {
-    if (!cfg || batch < 1 || max_pages < 1 || max_pages > kKv8MaxPages || check_cfg(cfg) != SUN_OK) return 0;
-    return align_up(std::max<size_t>(kv8_partial_floats(*cfg, batch, kv8_max_chunks(*cfg, batch, max_pages, 0)) * 4, 1));
+    if (!cfg || batch < 1 || batch > kKv8MaxBatch || max_pages < 1 || max_pages > kKv8MaxPages || check_cfg(cfg) != SUN_OK) return 0;
+    if (!kv8_attention_fits(*cfg, batch, kv8_max_chunks(*cfg, batch, max_pages, 0))) return 0;
+    size_t most = 1;   // fewer requests have more chunks each
+    for (int b = 1; b <= batch; ++b) most = std::max(most, kv8_partial_floats(*cfg, b, kv8_max_chunks(*cfg, b, max_pages, 0)) * 4);
+    return align_up(most);
 }
 
 static int validate_kv8_requests(const Kv8Pool& pool, int batch, const int32_t* page_tables, int max_pages, const int32_t* n_tokens,
@@ -1581,11 +1591,13 @@ int sun_kv8_attention(const sun_kv8_pool* pool_, int layer, int batch, int dtype
     const sun_model_cfg& c = pool.cfg;
     if (!is_dtype(dtype)) return fail(SUN_ERR_SHAPE, "dtype must be SUN_F32 or SUN_BF16");
     if (layer < 0 || layer >= c.n_layers) return fail(SUN_ERR_SHAPE, "layer out of range");
-    if (batch < 1 || batch > 1024 || max_pages < 1 || max_pages > kKv8MaxPages || window < 0)
-        return fail(SUN_ERR_SHAPE, "batch must be in [1,1024], max_pages in [1, %d], window >= 0", kKv8MaxPages);
+    if (batch < 1 || batch > kKv8MaxBatch || max_pages < 1 || max_pages > kKv8MaxPages || window < 0)
+        return fail(SUN_ERR_SHAPE, "batch must be in [1, %d], max_pages in [1, %d], window >= 0", kKv8MaxBatch, kKv8MaxPages);
     if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(SUN_ERR_SHAPE, "q and out must be 16-byte aligned");
     if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    const size_t need = kv8_partial_floats(c, batch, kv8_max_chunks(c, batch, max_pages, window)) * 4;
+    const int chunks = kv8_max_chunks(c, batch, max_pages, window);
+    if (!kv8_attention_fits(c, batch, chunks)) return fail(SUN_ERR_SHAPE, "%d requests of %d pages are more than one launch takes", batch, max_pages);
+    const size_t need = kv8_partial_floats(c, batch, chunks) * 4;
     if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
     hipStream_t st = (hipStream_t)stream;
     if (flags & SUN_VALIDATE)
@@ -1615,8 +1627,13 @@ int sun_mx4_dequantize(const void* codes, const void* scales, int rows, int cols
     return SUN_OK;
 }
 
+// Up to 128 rows a workgroup has at least 16 columns, 64 of 2^14 columns and more; above, tiles of 128 x 128 or more
+static bool mx4_linear_fits(int64_t N, int64_t K, int64_t rows) {
+    return N <= 64 * kMaxGroups && K <= 1 << 30 && rows <= 1 << 30 && ((N + 127) / 128) * ((rows + 127) / 128) <= kMaxGroups;
+}
+
 size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows) {
-    if (N < 1 || rows < 1 || K < 32 || K % 32) return 0;
+    if (N < 1 || rows < 1 || K < 32 || K % 32 || !mx4_linear_fits(N, K, rows)) return 0;
     return align_up(std::max<size_t>(mx4_linear_workspace_up_to(N, K, rows), 1));
 }
 
@@ -1627,6 +1644,7 @@ int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows
     if (!is_dtype(out_dtype) || rows < 1) return fail(SUN_ERR_SHAPE, "out_dtype must be SUN_F32 or SUN_BF16, rows >= 1");
     if (ld_x < K || ld_x % (16 / dtype_bytes(x_dtype)) || ld_out < N || (uintptr_t)out % dtype_bytes(out_dtype))
         return fail(SUN_ERR_SHAPE, "ld_x must be >= K and a multiple of 16 bytes, ld_out >= N, out aligned to its type");
+    if (!mx4_linear_fits(N, K, rows)) return fail(SUN_ERR_SHAPE, "%d x %d by %d rows is more than one launch takes", N, K, rows);
     if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     const size_t need = mx4_linear_workspace(N, K, rows, x_dtype == SUN_F32);
     if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);

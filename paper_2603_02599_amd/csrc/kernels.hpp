@@ -106,6 +106,7 @@ struct Kv8Rows {   // rows of an append, see sun_kv8_append
     const void *q_norm, *k_norm;
     void* q_out;
 };
+int64_t kv8_append_groups(const sun_model_cfg& c, const Kv8Rows& r);   // workgroups that it takes
 hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, bool f32, hipStream_t st);
 // Chunks of a request at most, whatever its length, and the scratch that they take when there are several.
 int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window);

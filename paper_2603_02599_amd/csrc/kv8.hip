@@ -22,7 +22,7 @@ struct Kv8AppendArgs {
     uint8_t *codes, *scales;   // the layer's
     int64_t k_page, k_head, v_off, v_page, v_head, s_page, s_head, vs_off;
     Kv8Rows r;
-    int n_pages, Hq, Hkv, heads_a_block, row_blocks, parts;
+    int n_pages, Hq, Hkv, row_blocks, parts;
     float eps;
     double theta[kKv8Half];
 };
@@ -37,6 +37,8 @@ __device__ __forceinline__ void load4(const T* p, float (&x)[4]) {
         x[0] = bf16_lo(v.x), x[1] = bf16_hi(v.x), x[2] = bf16_lo(v.y), x[3] = bf16_hi(v.y);
     }
 }
+constexpr int kKv8ManyRows = 1024;   // rows of an append from which a workgroup takes four
+
 template <int O>
 __device__ __forceinline__ double lane_xor_f64(double v) {
     const uint2 w = __builtin_bit_cast(uint2, v);
@@ -279,22 +281,27 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
     }
 }
 
+struct Kv8AppendGrid {
+    bool many;                             // rows by fours
+    int64_t row_blocks, parts, v_blocks;   // workgroups of q and k are row_blocks * parts
+};
+// A row's heads are shared by as many workgroups as keep one pass each, while there are few rows: 64 / 256 rows of the 8B shape 5.8 / 6.6 us with one
+// a row, 5.1 / 6.5 shared, but 600 rows 12.6 and 16.8.
+static Kv8AppendGrid append_grid(const sun_model_cfg& c, const Kv8Rows& r) {
+    const int64_t rows = r.rows, windows = (rows + 15) / 16, lanes = c.head_dim / 8;
+    if (rows >= kKv8ManyRows) return Kv8AppendGrid{true, (rows + 3) / 4, 1, windows * ((c.n_kv_heads + 3) / 4)};
+    const int64_t passes = (((r.q ? c.n_q_heads : 0) + (int64_t)c.n_kv_heads) * lanes + 255) / 256;
+    return Kv8AppendGrid{false, rows, rows <= 256 ? passes : 1, windows * c.n_kv_heads};
+}
+int64_t kv8_append_groups(const sun_model_cfg& c, const Kv8Rows& r) {
+    const Kv8AppendGrid g = append_grid(c, r);
+    return g.row_blocks * g.parts + g.v_blocks;
+}
+
 template <class T, int D>
-static hipError_t append(const Kv8AppendArgs& a0, hipStream_t st) {
-    Kv8AppendArgs a = a0;
-    const int rows = a.r.rows;
-    if (rows >= 1024) {
-        const int v_blocks = (rows + 15) / 16 * ((a.Hkv + 3) / 4);
-        a.row_blocks = (rows + 3) / 4;
-        a.parts = 1;
-        hipLaunchKernelGGL((kv8_append_kernel<T, D, 4>), dim3(a.row_blocks * a.parts + v_blocks), dim3(256), 0, st, a);
-    } else {   // a row's heads are shared by as many workgroups as keep one pass each, while there are few rows
-        const int passes = ((a.r.q ? a.Hq : 0) + a.Hkv + 256 / (D / 8) - 1) / (256 / (D / 8));
-        const int v_blocks = (rows + 15) / 16 * a.Hkv;
-        a.row_blocks = rows;
-        a.parts = rows <= 256 ? passes : 1;
-        hipLaunchKernelGGL((kv8_append_kernel<T, D, 1>), dim3(a.row_blocks * a.parts + v_blocks), dim3(256), 0, st, a);
-    }
+static hipError_t append(const Kv8AppendArgs& a, bool many, int64_t groups, hipStream_t st) {
+    if (many) hipLaunchKernelGGL((kv8_append_kernel<T, D, 4>), dim3((unsigned)groups), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kv8_append_kernel<T, D, 1>), dim3((unsigned)groups), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
@@ -311,8 +318,11 @@ hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, b
     a.n_pages = (int)L.n_pages, a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads;
     a.eps = c.rms_eps;
     for (int j = 0; j < c.head_dim / 2; ++j) a.theta[j] = pool.theta[j];
-    if (f32) return c.head_dim == 128 ? append<float, 128>(a, st) : append<float, 64>(a, st);
-    return c.head_dim == 128 ? append<uint16_t, 128>(a, st) : append<uint16_t, 64>(a, st);
+    const Kv8AppendGrid g = append_grid(c, r);
+    a.row_blocks = (int)g.row_blocks, a.parts = (int)g.parts;
+    const int64_t groups = kv8_append_groups(c, r);
+    if (f32) return c.head_dim == 128 ? append<float, 128>(a, g.many, groups, st) : append<float, 64>(a, g.many, groups, st);
+    return c.head_dim == 128 ? append<uint16_t, 128>(a, g.many, groups, st) : append<uint16_t, 64>(a, g.many, groups, st);
 }
 
 // ---------------------------------------------------------------- attention of one new token

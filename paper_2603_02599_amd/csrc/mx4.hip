@@ -343,7 +343,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
 // at a time; lanes on rows of their own take it four times as long).  In LDS the four pieces of row r are exchanged by r / 4, so that
 // sixteen rows' pieces j, which is what an operand reads, lie on different banks.
 template <class T, int P, int RT, int NT, int WN, int WK, int WJ, int ST>
-__global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a) {
+__global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args a) {
+    static_assert(WN * WK * WJ == 8, "");
     constexpr int XF = RT * 4, CF = NT * WN;                    // operand fragments (1 KiB) of a chunk: activations, codes
     constexpr int C0 = XF * 1024, S0 = C0 + CF * 1024, CHUNK = S0 + CF * 256, STAGE = WK * CHUNK;
     constexpr int WC = WN * WJ, XW = XF / WC, CW = CF / WC;     // waves of a chunk, and what one requests of it
@@ -495,9 +496,6 @@ __global__ __launch_bounds__(64 * WN * WK * WJ) void mx4_stream_kernel(Mx4Args a
         }
     }
 }
-
-template <int RT, int NT, int WN, int WK, int WJ, int ST>
-constexpr int mx4_threads() { return 64 * WN * WK * WJ; }
 
 // Many rows, where the matrix cores are what is short: 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations,
 // codes and powers go through LDS as above, the next step's on their way while one is computed on.  Two places for the activations; codes and powers,
@@ -700,14 +698,13 @@ static hipError_t multiply(const Mx4Args& a, const Mx4Plan& p, hipStream_t st) {
     if (p.kind == Mx4Plan::STREAM) {
         const dim3 grid((a.N + p.cols - 1) / p.cols, 1, p.splits);
         // RT, NT, WN, WK, WJ, ST
-#define SUN_STREAM(...) hipLaunchKernelGGL((mx4_stream_kernel<T, P, __VA_ARGS__>), grid, dim3(mx4_threads<__VA_ARGS__>()), 0, st, a)
-        if (p.rt == 2 && p.cols == 128) SUN_STREAM(2, 2, 4, 2, 1, 4);
-        else if (p.rt == 2) SUN_STREAM(2, 2, 2, 2, 2, 4);
-        else if (p.rt == 4 && p.cols == 128) SUN_STREAM(4, 2, 4, 2, 1, 3);
-        else if (p.rt == 4) SUN_STREAM(4, 2, 2, 2, 2, 3);
-        else if (p.cols == 128) SUN_STREAM(8, 2, 4, 1, 2, 3);
-        else SUN_STREAM(8, 2, 2, 2, 2, 2);
-#undef SUN_STREAM
+        const dim3 block(512);
+        if (p.rt == 2 && p.cols == 128) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 2, 2, 4, 2, 1, 4>), grid, block, 0, st, a);
+        else if (p.rt == 2) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 2, 2, 2, 2, 2, 4>), grid, block, 0, st, a);
+        else if (p.rt == 4 && p.cols == 128) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 4, 2, 4, 2, 1, 3>), grid, block, 0, st, a);
+        else if (p.rt == 4) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 4, 2, 2, 2, 2, 3>), grid, block, 0, st, a);
+        else if (p.cols == 128) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 2, 4, 1, 2, 3>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 2, 2, 2, 2, 2>), grid, block, 0, st, a);
     } else {
         const long long groups = (long long)((a.N + p.cols - 1) / p.cols) * p.splits, rows = (a.rows + p.cols - 1) / p.cols;
         const dim3 grid((unsigned)(8 * (groups / 8 * rows + (groups % 8 * rows + 7) / 8)));

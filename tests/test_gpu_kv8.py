@@ -485,3 +485,98 @@ def test_block_on_another_stream():
         b.step()
     torch.cuda.synchronize()
     assert torch.equal(a.out, b.out) and torch.equal(a.cache.mem, b.cache.mem)
+
+
+def test_blocks_on_two_streams_at_once():
+    """Two blocks with workspaces of their own, their steps under way together, give what they give alone."""
+    lens = [[40, 700, 3], [2000, 5]]
+    alone, together = ([Block(n, "bf16", seed=i) for i, n in enumerate(lens)] for _ in range(2))
+    for b in alone:
+        for _ in range(8):
+            b.step()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in lens]
+    for _ in range(8):
+        for b, s in zip(together, streams):
+            with torch.cuda.stream(s):
+                b.step()
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        assert torch.equal(a.out, b.out) and torch.equal(a.cache.mem, b.cache.mem)
+
+
+def test_two_graphs_share_a_workspace():
+    """Graphs replayed one behind the other on a stream may use the same workspace."""
+    lens = [[3000, 90], [40, 700, 3]]
+    eager, graphed = ([Block(n, "bf16", seed=i) for i, n in enumerate(lens)] for _ in range(2))
+    ws = max((b.ws for b in graphed), key=lambda t: t.numel())
+    graphs = []
+    for b in graphed:
+        b.ws = ws
+        start = (b.lens.clone(), b.cache.mem.clone())
+        b.step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.step()
+        graphs.append(g)
+        b.lens.copy_(start[0])
+        b.cache.mem.copy_(start[1])
+    for step in range(4):
+        for b in eager:
+            b.step()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager, graphed):
+            assert torch.equal(a.out, b.out) and torch.equal(a.cache.mem, b.cache.mem), step
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pages_beyond_32_bit_offsets(dtype):
+    """Pages at the end of a pool of more than 2^32 bytes a layer: the same bytes and results as in a small pool."""
+    shape = make_shape(16, 8, 128)
+    small = Cache(shape, [40, 900], poison=False)
+    small.fill(1, [37, 893])
+    cols = small.table.shape[1]
+    n_pages = (9 << 30) // 2 // sun.sun_kv8_pool_bytes(small.cfg, 1) * 2 + 7
+    mem = torch.zeros(sun.sun_kv8_pool_bytes(small.cfg, n_pages), dtype=torch.uint8, device=DEV)
+    pool = sun.sun_kv8_pool_create(small.cfg, mem)
+    lay, first = pool.layout(), n_pages - small.n_pages
+    assert lay.k_layer > 1 << 32 and lay.n_pages == n_pages
+
+    def blocks(m, l, page, pages):   # codes and scales of the second layer's pages
+        c, s = l.k_off + l.k_layer + page * l.k_page, l.ks_off + l.s_layer + page * l.s_page
+        return m[c:c + pages * l.k_page], m[s:s + pages * l.s_page]
+    for a, b in zip(blocks(mem, lay, first, small.n_pages), blocks(small.mem, small.lay, 0, small.n_pages)):
+        a.copy_(b)
+    table = torch.where(small.dev_table >= 0, small.dev_table + first, small.dev_table)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    pos, req = i32([37, 38, 39, 893, 894, 895, 896, 897, 898, 899]), i32([0] * 3 + [1] * 7)
+    q, k, v = (torch.randn(10, h * 128, generator=g, device=DEV).to(DT[dtype]) for h in (16, 8, 8))
+    outs = []
+    for p, t in ((small.pool, small.dev_table), (pool, table)):
+        q_out, out = torch.zeros_like(q), torch.zeros(2, 16 * 128, device=DEV, dtype=DT[dtype])
+        sun.sun_kv8_append(p, 1, q, k, v, pos, req, t, q_out)
+        ws = torch.zeros(sun.sun_kv8_attention_workspace_bytes(small.cfg, 2, cols), dtype=torch.uint8, device=DEV)
+        sun.sun_kv8_attention(p, 1, q_out[[2, 9]], t, i32([40, 900]), out, ws)
+        outs.append((q_out, out))
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and outs[0][1].abs().min() > 0
+    for a, b in zip(blocks(mem, lay, first, small.n_pages), blocks(small.mem, small.lay, 0, small.n_pages)):
+        assert torch.equal(a, b)
+
+
+def test_workspace_of_a_larger_batch_serves_a_smaller():
+    """Five requests are cut finer than eight: the workspace made for eight holds their parts."""
+    lens = [16 * 300] * 5
+    cache = Cache(make_shape(8, 8, 64), lens, extra_cols=0)
+    cache.fill(0, lens)
+    q = torch.randn(5, 8 * 64, device=DEV)
+    results = []
+    for batch in (5, 8):
+        out = torch.zeros_like(q)
+        ws = torch.zeros(sun.sun_kv8_attention_workspace_bytes(cache.cfg, batch, cache.table.shape[1]), dtype=torch.uint8, device=DEV)
+        sun.sun_kv8_attention(cache.pool, 0, q, cache.dev_table, i32(lens), out, ws)
+        results.append(out)
+    assert torch.equal(*results)

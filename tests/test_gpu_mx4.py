@@ -147,3 +147,57 @@ def test_linear_again_and_other_rows(rows):
     y = x.clone()
     y[1:] = torch.randn_like(y[1:].float()).to(y.dtype)
     assert torch.equal(multiply(codes, scales, y, "f32")[0], a[0])
+
+
+@pytest.mark.parametrize("x_dtype, out_dtype", [("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("n, k, rows", [(8200, 160, 3), (16400, 96, 16), (300, 4096, 20), (300, 4096, 60), (300, 4096, 100), (17000, 160, 20), (17000, 288, 60),
+                                        (17000, 416, 100), (15000, 160, 2000), (2000, 8192, 500), (4000, 2080, 1100)])
+def test_linear_every_way_of_dealing(n, k, rows, x_dtype, out_dtype):
+    """Wide and narrow workgroups, whole and split along k, large and small tiles with and without a last few column tiles."""
+    check_linear(*make_linear(n, k, rows, x_dtype), out_dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_many_with_a_ragged_end(dtype):
+    g = torch.Generator(device=DEV).manual_seed(3)
+    check_quantize(torch.randn(1031, 8224, generator=g, device=DEV).to(DT[dtype]))
+
+
+@pytest.mark.parametrize("dtype, n, k", [("f32", 1873, 32800), ("bf16", 3301, 32800)])
+def test_values_past_the_caches(dtype, n, k):
+    """Values that leave past the caches, against a table of the codes' values."""
+    g = torch.Generator(device=DEV).manual_seed(4)
+    codes = torch.randint(0, 256, (n, k // 2), generator=g, device=DEV, dtype=torch.uint8)
+    scales = torch.randint(100, 140, (n, k // 32), generator=g, device=DEV, dtype=torch.uint8)
+    got = sun.sun_mx4_dequantize(codes, scales, DT[dtype])
+    table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], device=DEV)
+    table = torch.cat([table, -table])
+    for at in range(0, n, 500):
+        c, s = codes[at:at + 500].int(), scales[at:at + 500].float()
+        want = torch.stack([table[c & 15], table[c >> 4]], -1).view(-1, k // 32, 32) * torch.exp2(s - 127)[:, :, None]
+        assert torch.equal(got[at:at + 500].float(), want.view(-1, k))
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 values to convert, and activations and outputs of more than 2^31 elements: the last rows are like those of a small call."""
+    n, k = 131080, 32800
+    w = torch.empty(n, k, device=DEV, dtype=torch.bfloat16)
+    w[:-9] = 1.0
+    w[-9:] = torch.randn(9, k, device=DEV)
+    codes, scales = sun.sun_mx4_quantize(w)
+    few_codes, few_scales = sun.sun_mx4_quantize(w[-9:].clone())
+    assert torch.equal(codes[-9:], few_codes) and torch.equal(scales[-9:], few_scales)
+    del w
+    values = sun.sun_mx4_dequantize(codes, scales)
+    assert torch.equal(values[-9:], sun.sun_mx4_dequantize(few_codes, few_scales)) and (values[:-9:5000] == 1).all()
+    del values, codes, scales
+    rows, n, k = 70000, 32768, 32
+    codes, scales, _ = make_linear(n, k, 1, "bf16")
+    x = torch.zeros(rows, n, device=DEV, dtype=torch.bfloat16)[:, :k]
+    x[-300:] = torch.randn(300, k, device=DEV).to(x.dtype)
+    out = torch.empty(rows, n, device=DEV, dtype=torch.bfloat16)
+    sun.sun_mx4_linear(codes, scales, x, out, torch.empty(sun.sun_mx4_linear_workspace_bytes(n, k, rows), device=DEV, dtype=torch.uint8))
+    xs, wv = host(x[-300:]), R.mx4_values(codes.cpu().numpy(), scales.cpu().numpy())
+    ref = xs @ wv.T
+    assert (np.abs(host(out[-300:]) - ref) <= R.linear_bound(xs, wv, ref, "bf16")).all()
+    assert (out[:-300:700] == 0).all()
