@@ -1552,7 +1552,6 @@ int sun_kv8_append(sun_kv8_pool* pool_, int layer, int rows, int dtype, const vo
     return SUN_OK;
 }
 
-constexpr int kKv8MaxBatch = 1024;
 static bool kv8_attention_fits(const sun_model_cfg& c, int batch, int chunks) {
     return (int64_t)batch * std::max<int64_t>(c.n_q_heads, (int64_t)c.n_kv_heads * chunks) <= kMaxGroups;
 }

@@ -108,6 +108,7 @@ struct Kv8Rows {   // rows of an append, see sun_kv8_append
 };
 int64_t kv8_append_groups(const sun_model_cfg& c, const Kv8Rows& r);   // workgroups that it takes
 hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, bool f32, hipStream_t st);
+constexpr int kKv8MaxBatch = 1024;   // requests of an attention
 // Chunks of a request at most, whatever its length, and the scratch that they take when there are several.
 int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window);
 size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks);

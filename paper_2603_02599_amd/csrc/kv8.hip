@@ -401,14 +401,20 @@ __device__ __forceinline__ void store_as(T* p, float v) {
     else *p = f32_to_bf16_bits(v);
 }
 
+template <int D>
+struct Kv8Parts {   // of the waves
+    float o[kKv8Waves][kMaxGroup][D];
+    float2 ml[kKv8Waves][kMaxGroup];
+};
+
+// Chunk ci of request b, KV head `head`.
 template <class T, int D>
-__global__ __launch_bounds__(64 * kKv8Waves, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
+__device__ __forceinline__ void kv8_attend(const Kv8AttnArgs& a, int b, int head, int ci, Kv8Parts<D>& parts) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NH = D / 64, NB = D / 16;   // loads of a key's quarter, dim blocks of the output
-    __shared__ float part_o[kKv8Waves][kMaxGroup][D];
-    __shared__ float2 part_ml[kKv8Waves][kMaxGroup];
+    auto& part_o = parts.o;
+    auto& part_ml = parts.ml;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
-    const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, b = rest % a.batch, ci = rest / a.batch;
     const Kv8Span s = kv8_span(a, b);
     const int G = a.Hq / a.Hkv;
     if (ci >= s.chunks) {
@@ -660,6 +666,62 @@ __global__ __launch_bounds__(64 * kKv8Waves, 2) void kv8_attn_kernel(Kv8AttnArgs
     }
 }
 
+// A workgroup for every chunk that the table has room for: the ones behind a request's last end at once.
+template <class T, int D>
+__global__ __launch_bounds__(64 * kKv8Waves, 2) void kv8_attn_kernel(Kv8AttnArgs a) {
+    __shared__ Kv8Parts<D> parts;
+    const int rest = blockIdx.x / a.Hkv;
+    kv8_attend<T, D>(a, rest % a.batch, blockIdx.x % a.Hkv, rest / a.batch, parts);
+}
+
+// The chunks that there are, dealt to a fixed number of workgroups, each of which counts them first (one of a request without a token, whose
+// output is zeros).  Neighbours in the order of work are kKv8Apart-ths of the list apart: neighbouring chunks of one request at a time are
+// slower (64 requests of 8192 tokens: 238 us so, 182 apart).
+constexpr int kKv8Apart = 16;
+template <class T, int D>
+__global__ __launch_bounds__(64 * kKv8Waves, 2) void kv8_attn_dealt_kernel(Kv8AttnArgs a) {
+    __shared__ Kv8Parts<D> parts;
+    __shared__ int ends[kKv8MaxBatch], sums[kKv8Waves];   // chunks of the requests up to each
+    constexpr int EACH = kKv8MaxBatch / (64 * kKv8Waves);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int count[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int b = (int)threadIdx.x * EACH + i;
+        count[i] = b < a.batch ? max(kv8_span(a, b).chunks, 1) : 0;
+        sum += count[i];
+    }
+    int before = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int v = __shfl_up(before, o);
+        if (lane >= o) before += v;
+    }
+    if (lane == 63) sums[wave] = before;
+    __syncthreads();
+    before -= sum;
+#pragma unroll
+    for (int w = 0; w < kKv8Waves - 1; ++w) before += w < wave ? sums[w] : 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) ends[threadIdx.x * EACH + i] = before += count[i];
+    __syncthreads();
+    const int chunks = ends[a.batch - 1], stretch = (chunks + kKv8Apart - 1) / kKv8Apart, items = stretch * kKv8Apart * a.Hkv;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int place = item / a.Hkv, chunk = place % stretch * kKv8Apart + place / stretch;
+        if (chunk >= chunks) continue;
+        int lo = 0, hi = a.batch - 1;   // the first request whose chunks end behind this one
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (ends[mid] > chunk) hi = mid;
+            else lo = mid + 1;
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        const int first = __builtin_amdgcn_readfirstlane(lo ? ends[lo - 1] : 0);
+        kv8_attend<T, D>(a, lo, item % a.Hkv, chunk - first, parts);
+        __syncthreads();   // `parts` is written again
+    }
+}
+
 // out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c over a request's chunks, a workgroup a head: chunk c is wave c % 4's.  The first
 // partials are requested before their weights are known.
 template <class T, int D>
@@ -731,9 +793,18 @@ size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks) {
     return chunks < 2 ? 0 : (size_t)batch * chunks * c.n_q_heads * (c.head_dim + 2);
 }
 
+// How chunks come to workgroups.  A workgroup behind a request's last chunk costs 1.25 ns, counting the chunks 1 us and more for each of the 512
+// workgroups that are on the chip at a time.  64 requests of 500 tokens, table of 512 / 1024 / 8192 pages (4096 / 8192 / 32768 workgroups): 22 / 28 / 56 us
+// with a workgroup for each, 28 in all three dealt; 64 of 4096 tokens, 8192 workgroups: 109 and 99; 256 of 1000, 32768: 136 and 99.  Where one chunk a
+// request is all there can be, none is behind the last: 1024 of 100 tokens 83 us, dealt 106.
+constexpr int64_t kKv8Room = 4096;
+constexpr int kKv8Dealt = 2048;   // 1024: 256 requests of up to 4000 tokens 170 -> 178 us, 256 of 300 52.7 -> 49.1
+
 template <class T, int D>
 static hipError_t attend(const Kv8AttnArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((kv8_attn_kernel<T, D>), dim3((unsigned)((long long)a.batch * a.Hkv * a.chunks)), dim3(64 * kKv8Waves), 0, st, a);
+    const int64_t room = (int64_t)a.batch * a.Hkv * a.chunks;
+    if (a.chunks == 1 || room <= kKv8Room) hipLaunchKernelGGL((kv8_attn_kernel<T, D>), dim3((unsigned)room), dim3(64 * kKv8Waves), 0, st, a);
+    else hipLaunchKernelGGL((kv8_attn_dealt_kernel<T, D>), dim3(kKv8Dealt), dim3(64 * kKv8Waves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.chunks > 1)
         hipLaunchKernelGGL((kv8_join_kernel<T, D>), dim3((unsigned)(a.batch * a.Hq)), dim3(256), 0, st, a);

@@ -567,6 +567,28 @@ def test_pages_beyond_32_bit_offsets(dtype):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq, hkv, d, batch", [(8, 8, 64, 11), (16, 8, 128, 300), (4, 2, 128, 1024)])
+def test_attention_with_room_for_far_more(hq, hkv, d, batch, dtype):
+    """A table that is far wider than the caches are long: the same bits, whichever way the chunks are dealt."""
+    lens = [(0, 1, 700, 16, 2500, 0, 257)[i % 7] for i in range(batch)]
+    cache = Cache(make_shape(hq, hkv, d), lens, extra_cols=0)
+    cache.fill(1, lens)
+    q = torch.randn(batch, hq * d, device=DEV).to(DT[dtype])
+    results = []
+    for cols in (cache.table.shape[1], 16000):
+        table = torch.full((batch, cols), -1, device=DEV, dtype=torch.int32)
+        table[:, :cache.table.shape[1]] = cache.dev_table
+        ws = torch.zeros(sun.sun_kv8_attention_workspace_bytes(cache.cfg, batch, cols), dtype=torch.uint8, device=DEV)
+        for window in (0, 600):
+            out = torch.full_like(q, 9.0)
+            sun.sun_kv8_attention(cache.pool, 1, q, table, i32(lens), out, ws, window=window)
+            results.append(out)
+    assert torch.equal(results[0], results[2]) and torch.equal(results[1], results[3])
+    assert not torch.equal(results[0], results[1]) and (results[0][[i for i, n in enumerate(lens) if n == 0]] == 0).all()
+    check_attention(cache, 1, lens, dtype)
+
+
 def test_workspace_of_a_larger_batch_serves_a_smaller():
     """Five requests are cut finer than eight: the workspace made for eight holds their parts."""
     lens = [16 * 300] * 5
