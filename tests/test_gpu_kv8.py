@@ -143,15 +143,15 @@ def test_append_one_row_per_request(hq, hkv, d, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hq, hkv, d", [(4, 2, 64), (10, 2, 128)])
-@pytest.mark.parametrize("counts, firsts", [((16,), (0,)), ((16,), (5,)), ((1,), (16,)), ((33, 50), (0, 7)), ((15, 17, 3, 64), (1, 16, 31, 0)), ((700, 340), (3, 1000))])
+@pytest.mark.parametrize("counts, firsts", [((16,), (0,)), ((16,), (5,)), ((1,), (16,)), ((33, 50), (0, 7)), ((15, 17, 3, 64), (1, 16, 31, 0)), ((700, 340), (3, 1000)), ((2050, 63, 1, 2001), (3, 1000, 15, 7))])
 def test_append_prompts(counts, firsts, hq, hkv, d, dtype):
-    """Runs of positions that start and end anywhere in a page, of several requests in one call (past 1024 rows: four rows a workgroup)."""
+    """Runs of positions that start and end anywhere in a page, of several requests in one call (4096 rows and more: four a workgroup)."""
     cache = Cache(make_shape(hq, hkv, d), [f + c for f, c in zip(firsts, counts)])
     run_append(cache, 0, [(f + t, r) for r, (f, c) in enumerate(zip(firsts, counts)) for t in range(c)], dtype, flags=sun.SUN_VALIDATE)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [37, 1061])
+@pytest.mark.parametrize("rows", [37, 1061, 4133])
 def test_append_padding_and_any_order(rows, dtype):
     """Rows in any order with padding between them; a row of the last block stays within the arrays."""
     rng = np.random.default_rng(rows)
