@@ -630,8 +630,10 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
 
 // How a product is dealt to workgroups.  Times in microseconds, measured on the 8B and 14B shapes' matrices with one plane of activations: a chunk
 // of 128 k takes a streaming workgroup of 128 (64) columns 0.40 (0.28) with 32 rows, 0.60 (0.45) with 64, 0.90 (0.80) with 128; narrower ones were
-// never faster.  A step of 128 k of a 256 x 256 tile takes 3.1, of one or two 128 x 128 tiles on a compute unit 1.2 and 2.0.  A joining
-// launch takes 4 and its parts' bytes at 4 TB/s.
+// never faster.  A step of 128 k takes a tile of 256 columns and 32 * rt rows 0.5 + 0.325 * rt (3.1 with 256 rows), one or two of 128 x 128 on a
+// compute unit 1.2 and 2.0.  A joining launch takes 4 and its parts' bytes at 4 TB/s.  Tiles of 160, 192 and 224 rows against 256 and 128 alone:
+// 5120 x 13824 at 150 rows in 32 bits 95 -> 75 us, 14336 x 4096 at 1500 171 -> 149, 20000 x 5120 at 400 in 32 bits 267 -> 233; the
+// worst that the estimate does is 28672 x 4096 at 192 rows, 57.5 -> 61.6.
 constexpr int kMx4SplitRows = 1 << 17;   // more rows are never split along k
 struct Mx4Plan {
     enum { FEW, STREAM, TILE } kind;
@@ -660,7 +662,7 @@ static Mx4Plan mx4_plan(int N, int K, int rows, int planes) {
         consider(Mx4Plan::STREAM, rt, 128, (N + 127) / 128, rt == 2 ? 0.40 : rt == 4 ? 0.60 : 0.90, 0);
         consider(Mx4Plan::STREAM, rt, 64, (N + 63) / 64, rt == 2 ? 0.28 : rt == 4 ? 0.45 : 0.80, 0);
     } else {
-        consider(Mx4Plan::TILE, 8, 256, (long long)((N + 255) / 256) * ((rows + 255) / 256), 3.1, 0);
+        for (int rt : {8, 7, 6, 5}) consider(Mx4Plan::TILE, rt, 256, (long long)((N + 255) / 256) * ((rows + 32 * rt - 1) / (32 * rt)), 0.5 + 0.325 * rt, 0);
         consider(Mx4Plan::TILE, 4, 128, (long long)((N + 127) / 128) * ((rows + 127) / 128), 1.2, 2.0);
     }
     return best;
@@ -676,7 +678,7 @@ size_t mx4_linear_workspace(int N, int K, int rows, bool x_f32) {
 size_t mx4_linear_workspace_up_to(int N, int K, int rows) {
     size_t parts = 0;
     int from = 17;
-    for (int64_t to = 32; from <= std::min(rows, kMx4SplitRows); from = (int)to + 1, to += to < 128 ? to : 128)
+    for (int64_t to = 32; from <= std::min(rows, kMx4SplitRows); from = (int)to + 1, to += to < 128 ? to : 32)
         for (int planes : {1, 3}) {
             const int s = mx4_plan(N, K, from, planes).splits;
             if (s > 1) parts = std::max(parts, (size_t)s * (size_t)std::min<int64_t>(to, rows) * N * 4);
@@ -706,9 +708,12 @@ static hipError_t multiply(const Mx4Args& a, const Mx4Plan& p, hipStream_t st) {
         else if (p.cols == 128) hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 2, 4, 1, 2, 3>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((mx4_stream_kernel<T, P, 8, 2, 2, 2, 2, 2>), grid, block, 0, st, a);
     } else {
-        const long long groups = (long long)((a.N + p.cols - 1) / p.cols) * p.splits, rows = (a.rows + p.cols - 1) / p.cols;
+        const long long groups = (long long)((a.N + p.cols - 1) / p.cols) * p.splits, rows = (a.rows + 32 * p.rt - 1) / (32 * p.rt);
         const dim3 grid((unsigned)(8 * (groups / 8 * rows + (groups % 8 * rows + 7) / 8)));
         if (p.rt == 8) hipLaunchKernelGGL((mx4_tile_kernel<T, P, 8, 4, 2, 4>), grid, dim3(512), 0, st, a);
+        else if (p.rt == 7) hipLaunchKernelGGL((mx4_tile_kernel<T, P, 7, 4, 2, 4>), grid, dim3(512), 0, st, a);
+        else if (p.rt == 6) hipLaunchKernelGGL((mx4_tile_kernel<T, P, 6, 4, 2, 4>), grid, dim3(512), 0, st, a);
+        else if (p.rt == 5) hipLaunchKernelGGL((mx4_tile_kernel<T, P, 5, 4, 2, 4>), grid, dim3(512), 0, st, a);
         else hipLaunchKernelGGL((mx4_tile_kernel<T, P, 4, 4, 2, 2>), grid, dim3(256), 0, st, a);
     }
     if (hipError_t e = hipGetLastError()) return e;

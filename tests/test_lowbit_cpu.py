@@ -253,6 +253,16 @@ def test_linear_workspace_holds_fewer_rows_too(lib, N, K):
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
 
 
+@pytest.mark.parametrize("N, K", [(17, 5120), (1000, 4096), (5120, 13824), (28672, 4096), (300, 2080)])
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls get as far as the launch, which must find no GPU")
+def test_linear_workspace_is_enough(lib, N, K):
+    """No call with the bytes that were asked for finds them too few: it fails for want of a GPU instead."""
+    for rows in list(range(1, 700)) + list(range(700, 6000, 61)):
+        need = lib.sun_mx4_linear_workspace_bytes(N, K, rows)
+        for x_dtype in (0, 1):
+            assert lib.sun_mx4_linear(FAKE, FAKE, N, K, rows, FAKE, x_dtype, K, FAKE, 1, N, FAKE, need, None) not in (0, 2, 4), rows
+
+
 def test_binding_refuses_what_does_not_fit():
     """Types, shapes and devices are looked at before the library is called; tensors here are on the CPU, which is refused last."""
     x = torch.zeros(4, 64)
