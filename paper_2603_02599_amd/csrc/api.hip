@@ -1626,7 +1626,7 @@ int sun_mx4_dequantize(const void* codes, const void* scales, int rows, int cols
     return SUN_OK;
 }
 
-// Up to 128 rows a workgroup has at least 16 columns, 64 of 2^14 columns and more; above, tiles of 128 x 128 or more
+// Up to 128 rows a workgroup has at least 16 columns, 64 of 2^13 columns and more; above, tiles of 128 x 128 or more
 static bool mx4_linear_fits(int64_t N, int64_t K, int64_t rows) {
     return N <= 64 * kMaxGroups && K <= 1 << 30 && rows <= 1 << 30 && ((N + 127) / 128) * ((rows + 127) / 128) <= kMaxGroups;
 }

@@ -91,8 +91,11 @@ __device__ __forceinline__ int row_page(const Kv8AppendArgs& a, int row, int pos
 }
 
 // Workgroups [0, row_blocks * parts): q and k of RG rows, head_dim / 8 lanes a head with four pairs each.  The rest: v of 16 rows, a wave
-// a head.  Queries are computed in 32 bits; keys, which are rounded to few bits behind it, in 64 up to one rounding to 32, so that no
-// code depends on the order of operations.
+// a head, through LDS, where the dims of a row come to lie side by side as the pool has them.  Queries are computed in 32 bits; keys, which are
+// rounded to few bits behind it, in 64 up to one rounding to 32, so that no code depends on the order of operations.
+// Memory bounds many rows: 4096 of the 14B shape in 32 bits (q, k, v in, q and codes out: 209 MB) take 48 us, 4.4 TB/s read + written, a large copy's
+// 4.95.  Few rows are bound by the chain position -> table -> store and the sine of the angle in 64 bits, which run beside the first loads: 64 rows of the 8B
+// shape in bf16 (1.4 MB) take 5.1 us.
 template <class T, int D, int RG>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a) {
     constexpr int LPH = D / 8;   // lanes per head
@@ -339,13 +342,18 @@ hipError_t launch_kv8_append(const Kv8Pool& pool, int layer, const Kv8Rows& r, b
 // query as three truncations of 8 bits, which are exact.  Codes become bf16 exactly.  Powers of two are applied to scores and weights.
 // The running maximum and sum are in 32 bits; the sum is over the weights before they are split.
 // A step's keys are requested when the step before has its scores, its values when that has its output, page numbers a step ahead of both.
+// Reading the cache bounds it.  24 requests of the 14B shape of 2048 to 32768 tokens in bf16 (951 MB): 167 us and 4.7 for joining, 5.5 TB/s; 256 of the 8B shape with a window of
+// 1500 in 32 bits (656 MB): 119 us, 5.5 TB/s.  One request of 8191 tokens has two steps' latency and a second launch: 8.1 and 3.2 us for 17 MB.
+// Against a wave a chunk, four that share one have a quarter of the partial results; keys by whole token rows and past the caches took 24 long requests from
+// 176 to 170 us, values past the caches from 204 to 196.
 
 constexpr int kKv8Step = 64;
 constexpr int kKv8Waves = 4;
 constexpr int kKv8MinChunk = kKv8Step * kKv8Waves, kKv8MaxChunk = 2048;
 
-// Tokens of a chunk: a power of two that gives about 512 of them over the batch if all requests were like this one.  It depends on the
-// request's own length, the batch size and the heads, so a request's result does not depend on its batch-mates.
+// Tokens of a chunk: a power of two that gives about 512 of them (two a compute unit) over the batch if all requests were like this one.  It depends on the
+// request's own length, the batch size and the heads, so a request's result does not depend on its batch-mates.  At least a step of each wave.  At most
+// 2048: with 512 / 1024 / 2048 the 256 requests with the window took 163 / 148 / 128 us, with 1024 / 2048 the 24 long ones 204 / 190.
 constexpr int kKv8Chunks = 512;
 __host__ __device__ inline int kv8_chunk(int span, int batch, int Hkv) {
     const long long target = (long long)span * Hkv * batch / kKv8Chunks;

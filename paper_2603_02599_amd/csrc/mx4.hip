@@ -21,6 +21,7 @@ __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
 }
 // A lane takes eight columns, four lanes a block: reads and writes are contiguous over the wave.  The matrix is contiguous, so
 // rows do not matter.  A workgroup has R runs of 256 octets under way.  The converter rounds to the nearest even code and stops at 6.
+// Memory bounds it: 28672 x 4096 in bf16 (297 MB in and out) 48 us, 6.2 TB/s.
 template <class T, int R>
 __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* w, int64_t octets, uint32_t* codes, uint8_t* scales) {
     const int64_t stride = (int64_t)gridDim.x * 256 * R;
@@ -60,7 +61,8 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* w, int64_t o
     }
 }
 
-// A lane takes sixteen bytes of the output, so that a wave's store is a KiB without gaps, which is what stores past the caches need.
+// A lane takes sixteen bytes of the output, so that a wave's store is a KiB without gaps, which is what stores past the caches need.  Memory bounds it:
+// 28672 x 4096 in bf16 44 to 48 us, 6.2 to 6.7 TB/s.
 template <class T, int R, bool STREAM>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* codes, const uint8_t* scales, int64_t units, T* out) {
     constexpr int E = 16 / (int)sizeof(T);   // values of a unit
@@ -185,7 +187,7 @@ __device__ __forceinline__ void mx4_planes(const float (&v)[8], bf16x8 (&planes)
     for (int p = 0; p < 3; ++p) planes[p] = __builtin_bit_cast(bf16x8, w[p]);
 }
 
-// a lane takes eight
+// The planes of 32-bit activations for more than sixteen rows, once for all workgroups.  A lane takes eight.  150 x 13824: 6 us.
 __global__ __launch_bounds__(256) void mx4_planes_kernel(const float* x, int64_t ld_x, int rows, int K, uint16_t* planes, int64_t plane) {
     const int64_t octets = (int64_t)rows * (K / 8), stride = (int64_t)gridDim.x * 256;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < octets; u += stride) {
@@ -244,7 +246,9 @@ __device__ __forceinline__ void store_quad(const Mx4Args& a, T* out, int64_t ld,
         if (n + i < a.N) store_as(p + i, v[i]);
 }
 
-// Up to sixteen rows: 16 * NT columns a workgroup, the chunks of 128 k dealt to its eight waves, whose sums meet in LDS.  A wave has U chunks under
+// Up to sixteen rows: reading the weights is what costs, and latency where they are few: 6144 x 4096 at one row (13.4 MB) takes 5.5 us, of which about four are a launch
+// and one request's way; 28672 x 4096 at one row 13.1 us (4.8 TB/s), at 16 18.1, in 32 bits 22.8 and 39.5, where cutting x into planes in every workgroup shows.
+// 16 * NT columns a workgroup, the chunks of 128 k dealt to its eight waves, whose sums meet in LDS.  A wave has U chunks under
 // way at a time: their codes and powers go into LDS (see the next kernel for the order), its activations straight into the operand's registers: a
 // row that is not there is not asked for.  32-bit activations are cut into their planes here.
 constexpr int kFewWaves = 8;
@@ -336,8 +340,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
     }
 }
 
-// Some dozen rows, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Codes, powers and activations of
-// ST - 1 steps of 128 k are under way into LDS while one is computed on.  A step is a chunk of k of one plane of the activations.
+// Some dozen rows, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Of its eight waves WN share the columns, NT tiles
+// each, WK have chunks of k of their own and WJ share the eighths of a block of 32; the sums of WK and WJ meet in LDS at the end.  Codes, powers and activations
+// of ST - 1 steps are under way into LDS while one is computed on.  A step is a chunk of 128 k for each of WK, of one plane of the activations.
+// 28672 x 4096 in bf16 at 32 / 64 / 128 rows: 17.7 / 23 to 25 / 33.7 us, the weights' 62 MB at 3.5 / 2.6 / 1.8 TB/s.  What bounds it is the compute unit: converting the
+// codes (a conversion of two values takes a wave 4.4 cycles), requests (a KiB of activations or codes takes the address unit 20) and products take turns on each
+// chunk, and 224 workgroups leave 32 of 256 units idle.  Rings apart for codes and activations with waves for each, a rotated start along k and deeper rings
+// were no faster.
 //
 // A request reads 64 bytes of each of sixteen rows, four lanes side by side on a row (the address unit takes four neighbouring lanes on one line
 // at a time; lanes on rows of their own take it four times as long).  In LDS the four pieces of row r are exchanged by r / 4, so that
@@ -497,7 +506,9 @@ __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args a) {
     }
 }
 
-// Many rows, where the matrix cores are what is short: 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations,
+// Many rows, where the matrix cores are what is short: 28672 x 4096 at 2048 rows in bf16 takes 394 to 423 us from card to card, 1.14 to 1.22 PFLOP/s, the dense
+// bf16 product of the library 400; 5120 x 13824 at 150 rows in 32 bits (three planes) 65 us and 15 for planes and joining.
+// 16 * RT * WR rows and 16 * NT * WN columns a workgroup, a wave RT x NT tiles.  Activations,
 // codes and powers go through LDS as above, the next step's on their way while one is computed on.  Two places for the activations; codes and powers,
 // which a wave takes into registers when it enters the step, have one.
 template <class T, int P, int RT, int NT, int WR, int WN>
@@ -630,7 +641,7 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
 
 // How a product is dealt to workgroups.  Times in microseconds, measured on the 8B and 14B shapes' matrices with one plane of activations: a chunk
 // of 128 k takes a streaming workgroup of 128 (64) columns 0.40 (0.28) with 32 rows, 0.60 (0.45) with 64, 0.90 (0.80) with 128; narrower ones were
-// never faster.  A step of 128 k takes a tile of 256 columns and 32 * rt rows 0.5 + 0.325 * rt (3.1 with 256 rows), one or two of 128 x 128 on a
+// never faster.  A step of 128 k takes a tile of 256 columns and 32 * rt rows 0.9 + 0.275 * rt (3.1 with 256 rows), one or two of 128 x 128 on a
 // compute unit 1.2 and 2.0.  A joining launch takes 4 and its parts' bytes at 4 TB/s.  Tiles of 160, 192 and 224 rows against 256 and 128 alone:
 // 5120 x 13824 at 150 rows in 32 bits 95 -> 75 us, 14336 x 4096 at 1500 171 -> 149, 20000 x 5120 at 400 in 32 bits 267 -> 233; the
 // worst that the estimate does is 28672 x 4096 at 192 rows, 57.5 -> 61.6.
@@ -643,7 +654,14 @@ struct Mx4Plan {
 };
 static Mx4Plan mx4_plan(int N, int K, int rows, int planes) {
     const int chunks = (K + 127) / 128;
-    if (rows <= 16) return Mx4Plan{Mx4Plan::FEW, 1, N >= 64 * 256 ? 64 : N >= 32 * 256 ? 32 : 16, 1};
+    // Columns of a workgroup: the fewest that leave every compute unit one workgroup at most, 64 beyond.  32-bit activations of more than eight rows, whose cutting
+    // each workgroup does again, take twice as many.  K 4096, with 16 / 32 / 64 columns: N 4096 at one row 4.3 / 5.1 / 6.8 us, N 6144 6.3 / 5.5 / 7.1, N 16384
+    // 10.7 / 8.5 / 8.6 and at 16 rows 19 / 13.7 / 12.1; 16 rows in 32 bits, N 2048 14.9 / 12.3 / 14.4, N 6144 40 / 18.9 / 15.9.
+    if (rows <= 16) {
+        int cols = N <= 16 * 256 ? 16 : N <= 32 * 256 ? 32 : 64;
+        if (planes > 1 && rows > 8) cols = std::min(2 * cols, 64);
+        return Mx4Plan{Mx4Plan::FEW, 1, cols, 1};
+    }
     Mx4Plan best{};
     double least = 1e30;
     auto consider = [&](auto kind, int rt, int cols, long long tiles, double step, double step2) {
@@ -662,7 +680,7 @@ static Mx4Plan mx4_plan(int N, int K, int rows, int planes) {
         consider(Mx4Plan::STREAM, rt, 128, (N + 127) / 128, rt == 2 ? 0.40 : rt == 4 ? 0.60 : 0.90, 0);
         consider(Mx4Plan::STREAM, rt, 64, (N + 63) / 64, rt == 2 ? 0.28 : rt == 4 ? 0.45 : 0.80, 0);
     } else {
-        for (int rt : {8, 7, 6, 5}) consider(Mx4Plan::TILE, rt, 256, (long long)((N + 255) / 256) * ((rows + 32 * rt - 1) / (32 * rt)), 0.5 + 0.325 * rt, 0);
+        for (int rt : {8, 7, 6, 5}) consider(Mx4Plan::TILE, rt, 256, (long long)((N + 255) / 256) * ((rows + 32 * rt - 1) / (32 * rt)), 0.9 + 0.275 * rt, 0);
         consider(Mx4Plan::TILE, 4, 128, (long long)((N + 127) / 128) * ((rows + 127) / 128), 1.2, 2.0);
     }
     return best;

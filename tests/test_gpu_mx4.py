@@ -150,7 +150,7 @@ def test_linear_again_and_other_rows(rows):
 
 
 @pytest.mark.parametrize("x_dtype, out_dtype", [("f32", "bf16"), ("bf16", "f32")])
-@pytest.mark.parametrize("n, k, rows", [(8200, 160, 3), (16400, 96, 16), (300, 4096, 20), (300, 4096, 60), (300, 4096, 100), (17000, 160, 20), (17000, 288, 60),
+@pytest.mark.parametrize("n, k, rows", [(4500, 160, 7), (8200, 160, 3), (16400, 96, 16), (2000, 4096, 9), (300, 4096, 20), (300, 4096, 60), (300, 4096, 100), (17000, 160, 20), (17000, 288, 60),
                                         (17000, 416, 100), (15000, 160, 2000), (2000, 8192, 500), (4000, 2080, 1100), (6000, 96, 1287), (14700, 160, 642),
                                         (16500, 96, 586), (16900, 160, 687), (5400, 3008, 178), (5500, 3200, 140)])
 def test_linear_every_way_of_dealing(n, k, rows, x_dtype, out_dtype):
