@@ -642,14 +642,23 @@ def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, 
         max_pages, _want("n_tokens", n_tokens, dev, i32, (batch,)), window, _want("out", out, dev, t, shape), *_workspace(workspace, dev)), (flags,))
 
 
+def _current(device: int, stream):
+    """`stream` as GPU `device`'s current one: what is allocated inside belongs to it.  Memory of the pool of another stream may still be
+    read by work that is queued there when it is handed out, and may be handed out again before `stream` is done with it."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+
+
 def sun_mx4_quantize(w: torch.Tensor, stream=None):
-    """Returns (codes uint8 [rows, cols/2], scales uint8 [rows, cols/32])."""
+    """Returns (codes uint8 [rows, cols/2], scales uint8 [rows, cols/32]), which belong to the stream that fills them."""
     if w.dim() != 2 or w.shape[1] % 32:
         _refuse("w must be [rows, cols], cols a multiple of 32")
     (rows, cols), dev = w.shape, _gpu(w)
+    if stream is not None:
+        with _current(dev, stream):
+            return sun_mx4_quantize(w)
     _int32(rows=rows, cols=cols)
     codes, scales = w.new_empty((rows, cols // 2), dtype=torch.uint8), w.new_empty((rows, cols // 32), dtype=torch.uint8)
-    _call(dev, stream, lib().sun_mx4_quantize, (_want("w", w, dev, w.dtype, w.shape), _dtype(w, "w"), rows, cols, codes.data_ptr(), scales.data_ptr()))
+    _call(dev, None, lib().sun_mx4_quantize, (_want("w", w, dev, w.dtype, w.shape), _dtype(w, "w"), rows, cols, codes.data_ptr(), scales.data_ptr()))
     return codes, scales
 
 
@@ -662,11 +671,14 @@ def _mx4(codes: torch.Tensor, scales: torch.Tensor, device: int):
 
 
 def sun_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
-    """The values [rows, cols], float32 or bfloat16."""
+    """The values [rows, cols], float32 or bfloat16, which belong to the stream that fills them."""
     dev = _gpu(codes)
+    if stream is not None:
+        with _current(dev, stream):
+            return sun_mx4_dequantize(codes, scales, dtype)
     pc, ps, n, k = _mx4(codes, scales, dev)
     out = codes.new_empty((n, k), dtype=dtype)
-    _call(dev, stream, lib().sun_mx4_dequantize, (pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr()))
+    _call(dev, None, lib().sun_mx4_dequantize, (pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr()))
     return out
 
 

@@ -202,3 +202,34 @@ def test_offsets_beyond_32_bits():
     ref = xs @ wv.T
     assert (np.abs(host(out[-300:]) - ref) <= R.linear_bound(xs, wv, ref, "bf16")).all()
     assert (out[:-300:700] == 0).all()
+
+
+def pool_of(t):
+    """The stream whose pool of the allocator the tensor's memory comes from."""
+    at = t.data_ptr()
+    return next(s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"])
+
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_outputs_belong_to_the_stream_that_fills_them(dtype, raw):
+    """A block of the current stream's pool may still be read by work that is queued there, and would be handed out again while `stream` writes it."""
+    x = torch.randn(300, 416, device=DEV).to(DT[dtype])
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    assert side.cuda_stream != here.cuda_stream
+    side.wait_stream(here)
+    stream = side.cuda_stream if raw else side
+    codes, scales = sun.sun_mx4_quantize(x, stream=stream)
+    values = sun.sun_mx4_dequantize(codes, scales, DT[dtype], stream=stream)
+    assert torch.cuda.current_stream() == here
+    here.wait_stream(side)
+    assert [pool_of(t) for t in (codes, scales, values)] == [side.cuda_stream] * 3 and pool_of(x) == here.cuda_stream
+    want_c, want_s = R.mx4_quantize(host(x))
+    assert np.array_equal(codes.cpu().numpy(), want_c) and np.array_equal(scales.cpu().numpy(), want_s)
+    assert np.array_equal(host(values), R.mx4_values(want_c, want_s))
+    on = torch.zeros(5, 300, device=DEV)
+    workspace = torch.zeros(sun.sun_mx4_linear_workspace_bytes(300, 416, 5), device=DEV, dtype=torch.uint8)
+    side.wait_stream(here)
+    sun.sun_mx4_linear(codes, scales, x[:5], on, workspace, stream=stream)
+    here.wait_stream(side)
+    assert torch.equal(on, multiply(codes, scales, x[:5], "f32"))
