@@ -201,6 +201,12 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _current(device, stream):
+    """`stream` as GPU `device`'s current one: what is allocated inside belongs to it.  Memory of the pool of another stream may still be
+    read by work that is queued there when it is handed out, and may be handed out again before `stream` is done with it."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+
+
 def make_cfg(shape, act_dtype: str) -> ModelCfg:
     """shape: object with n_layers, hidden, n_q_heads, n_kv_heads, head_dim, ffn, vocab, rms_eps, rope_base and
     optionally qk_norm (bool), qkv_bias (bool) and rope_scaling = (factor, low_freq_factor, high_freq_factor, original_max_position)."""
@@ -282,7 +288,10 @@ def sun_weights_pack_bytes(cfg: ModelCfg) -> int:
 
 
 def sun_weights_create(cfg: ModelCfg, w: Dict[str, object], stream=None, keep_sources: bool = True) -> Weights:
-    """w: dict from workloads.make_weights (torch CUDA tensors).  Allocates the pack buffer with torch."""
+    """w: dict from workloads.make_weights (torch CUDA tensors).  Allocates the pack buffer with torch, from the pool of the stream that packs."""
+    if stream is not None:
+        with _current(w["embed"].device, stream):
+            return sun_weights_create(cfg, w, keep_sources=keep_sources)
     ptrs = WeightPtrs()
     keep: List[object] = []
     ptrs.embed = w["embed"].data_ptr()
@@ -295,7 +304,7 @@ def sun_weights_create(cfg: ModelCfg, w: Dict[str, object], stream=None, keep_so
     nbytes = sun_weights_pack_bytes(cfg)
     pack = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=w["embed"].device) if cfg.act_dtype == SUN_BF16 else None
     out = C.c_void_p()
-    _check(lib().sun_weights_create(C.byref(cfg), C.byref(ptrs), _p(pack), nbytes, _stream(stream), C.byref(out)))
+    _check(lib().sun_weights_create(C.byref(cfg), C.byref(ptrs), _p(pack), nbytes, _stream(None), C.byref(out)))
     keep.append(pack)
     if keep_sources or cfg.act_dtype == SUN_F32:
         keep.append(w)
@@ -311,7 +320,10 @@ def sun_qweights_pack_bytes(cfg: ModelCfg, group: int = 128) -> int:
 def sun_qweights_create(cfg: ModelCfg, w: Dict[str, object], quant: Dict[str, list], group: int = 128,
                         stream=None) -> Weights:
     """quant[key][layer] = (q uint8 [out, in/2], s fp16 [out, in/128], z fp16 [out, in/128]) CUDA tensors;
-    w supplies embed, g1, g2, gf, wlm."""
+    w supplies embed, g1, g2, gf, wlm.  The pack buffer is from the pool of the stream that packs."""
+    if stream is not None:
+        with _current(w["embed"].device, stream):
+            return sun_qweights_create(cfg, w, quant, group)
     ptrs = QWeightPtrs()
     keep: List[object] = [w["embed"], w["g1"], w["g2"], w["gf"], w["wlm"], quant]
     ptrs.embed = w["embed"].data_ptr()
@@ -329,21 +341,24 @@ def sun_qweights_create(cfg: ModelCfg, w: Dict[str, object], quant: Dict[str, li
     nbytes = sun_qweights_pack_bytes(cfg, group)
     pack = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=w["embed"].device) if cfg.act_dtype == SUN_BF16 else None
     out = C.c_void_p()
-    _check(lib().sun_qweights_create(C.byref(cfg), C.byref(ptrs), group, _p(pack), nbytes, _stream(stream), C.byref(out)))
+    _check(lib().sun_qweights_create(C.byref(cfg), C.byref(ptrs), group, _p(pack), nbytes, _stream(None), C.byref(out)))
     keep.append(pack)
     return Weights(out.value, keep, True)
 
 
 def sun_quantize_w4(w: torch.Tensor, group: int = 128, mode: str = "asym", stream=None):
     """Returns (q uint8 [rows, cols/2], s fp16 [rows, cols/group], z fp16 [rows, cols/group]); mode "sym_noz" is
-    the symmetric grid without stored zero points (z is None: 8 everywhere)."""
+    the symmetric grid without stored zero points (z is None: 8 everywhere).  They belong to the stream that fills them."""
+    if stream is not None:
+        with _current(w.device, stream):
+            return sun_quantize_w4(w, group, mode)
     rows, cols = w.shape
     dt = {torch.float32: SUN_F32, torch.bfloat16: SUN_BF16}[w.dtype]
     q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
     s = torch.empty((rows, cols // group), dtype=torch.float16, device=w.device)
     z = torch.empty_like(s) if mode != "sym_noz" else None
     _check(lib().sun_quantize_w4(_p(w), dt, rows, cols, group, {"asym": 0, "sym": 1, "sym_noz": 1}[mode], _p(q), _p(s),
-                                 _p(z), _stream(stream)))
+                                 _p(z), _stream(None)))
     return q, s, z
 
 
@@ -640,12 +655,6 @@ def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, 
     _call(dev, stream, lib().sun_kv8_attention, (
         pool.handle, layer, batch, _dtype(q, "q"), _want("q", q, dev, t, shape), _want("page_tables", page_tables, dev, i32, (batch, max_pages)),
         max_pages, _want("n_tokens", n_tokens, dev, i32, (batch,)), window, _want("out", out, dev, t, shape), *_workspace(workspace, dev)), (flags,))
-
-
-def _current(device: int, stream):
-    """`stream` as GPU `device`'s current one: what is allocated inside belongs to it.  Memory of the pool of another stream may still be
-    read by work that is queued there when it is handed out, and may be handed out again before `stream` is done with it."""
-    return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
 
 
 def sun_mx4_quantize(w: torch.Tensor, stream=None):

@@ -517,3 +517,32 @@ def test_linear_op_bf16_above_64_rows_ragged_columns(H, batch):
         got = out.double().cpu().numpy()
         tol = 1e-2 * np.abs(want) + 2e-3 if mat == 2 else 2e-4 + 1e-5 * np.abs(want)   # mat 2 output is bf16
         assert np.all(np.abs(got - want) <= tol), f"mat {mat}: max diff {np.abs(got - want).max():.3e}"
+
+
+# ------------------------------------------------------------------ memory of calls that are given a stream
+def _pool_of(t):
+    """The stream whose pool of the allocator the tensor's memory comes from."""
+    at = t.data_ptr()
+    return next(s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"])
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_quantised_and_packed_weights_belong_to_the_stream_that_fills_them(H, raw):
+    """What these calls allocate comes from the given stream's pool: a block of the current stream's may still be read by work that is queued there."""
+    w = wl.make_weights(wl.SMALL128, "bf16", "cuda:0", 3)
+    cfg = sun.make_cfg(wl.SMALL128, "bf16")
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+    plain = {k: [sun.sun_quantize_w4(m) for m in w[k]] for k in sun.QUANT_KEYS}
+    packed = [sun.sun_weights_create(cfg, w), sun.sun_qweights_create(cfg, w, plain)]
+    side.wait_stream(here)
+    q, s, z = sun.sun_quantize_w4(w["wq"][0], stream=stream)
+    q2, s2, z2 = sun.sun_quantize_w4(w["wq"][0], mode="sym_noz", stream=stream)
+    aside = [sun.sun_weights_create(cfg, w, stream=stream), sun.sun_qweights_create(cfg, w, plain, stream=stream)]
+    assert torch.cuda.current_stream() == here
+    here.wait_stream(side)
+    assert z2 is None
+    packs = [[t for t in h.keep if isinstance(t, torch.Tensor) and t.dtype == torch.uint8 and t.dim() == 1] for h in packed + aside]
+    assert [len(p) for p in packs] == [1] * 4
+    assert {_pool_of(t) for t in (q, s, z, q2, s2, packs[2][0], packs[3][0])} == {side.cuda_stream}
+    assert all(torch.equal(a, b) for a, b in zip((q, s, z), plain["wq"][0]))
