@@ -565,8 +565,9 @@ def _table(page_tables: torch.Tensor):
     return page_tables.shape
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream(), an object, takes longer than a launch
-_current_gpu = torch._C._cuda_getDevice
+# torch.cuda.current_stream(), an object, takes longer than a launch.  A torch build without GPUs has neither name, nor tensors that get as far.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _int32(**values):

@@ -4,6 +4,7 @@ import ctypes as C
 import math
 import os
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -273,3 +274,21 @@ def test_binding_refuses_what_does_not_fit():
         with pytest.raises(sun.SunError) as e:
             bad()
         assert e.value.status == 2
+
+
+def test_binding_loads_without_a_gpu_build_of_torch():
+    """The names that only a GPU build of torch has are not needed to load the module, to ask for sizes or to be refused."""
+    code = """
+import torch
+for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+from paper_2603_02599_amd import binding as sun
+assert sun.sun_mx4_linear_workspace_bytes(100, 64, 40) > 0
+try:
+    sun.sun_mx4_quantize(torch.zeros(4, 64))
+except sun.SunError as e:
+    print(e.status)
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert done.returncode == 0 and done.stdout.strip() == "2", done.stderr
