@@ -555,7 +555,8 @@ size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, in
  *   n_tokens   dev int32 [batch]: positions 0 .. n_tokens[i] - 1 are cached; counts are cut to [0, max_pages*16]
  *   window     > 0: only the last `window` of them are attended to, and table entries of pages in front of them are not read as
  *              pages (they may be -1); 0: all
- *   out        dev [batch, Hq*d]; a request without a token gets zeros
+ *   out        dev [batch, Hq*d]; a request without a token gets zeros, a head whose query is not finite
+ *              not-a-numbers where there is one
  * Tokens of a page outside the pool are left out.  A request's result does not depend on the others of the batch.
  * Cached numbers enter exactly; weights of the softmax carry 16 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
  * Under SUN_VALIDATE counts and tables are copied to the host (synchronises) and checked.

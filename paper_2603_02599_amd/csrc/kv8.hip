@@ -4,6 +4,7 @@
 // which the largest finite |y| is at most 448 * 2^e, code = e4m3(y * 2^-e) and the scale byte is e + 127.  Scaling by a power of
 // two is exact, so a value has one rounding (2^-4 of itself at most, above the format's subnormals), and the power can be applied behind a
 // product: to a key's score, and to a value's weight.
+#include <float.h>
 #include <math.h>
 
 #include "kernels.hpp"
@@ -411,6 +412,9 @@ __device__ __forceinline__ void store_as(T* p, float v) {
     else *p = f32_to_bf16_bits(v);
 }
 
+// What is stored of a weighted sum v, the weights' sum and the largest score: zeros where there is no token
+__device__ __forceinline__ float kv8_quotient(float v, float sum, float top) { return sum == 0.f && top == -INFINITY ? 0.f : v / sum; }
+
 template <int D>
 struct Kv8Parts {   // of the waves
     float o[kKv8Waves][kMaxGroup][D];
@@ -634,6 +638,16 @@ __device__ __forceinline__ void kv8_attend(const Kv8AttnArgs& a, int b, int head
             step(tok, std::true_type{}, here);
         }
         step(tok, std::false_type{}, next);
+        // A head whose every score is minus infinity has weights 0 / 0, not-a-numbers, where one without a token has zeros: its maximum is finite from
+        // here on, and its sum 0.  The tokens are looked for again, so that no step has to count them.
+        if (__any(m == -INFINITY)) {
+            bool any = false;
+            for (tok = begin; tok < end; tok += STRIDE) {
+                const int at = tok + kPageTokens * g;
+                any |= max(at, s.lo) < min(at + kPageTokens, end) && usable(table[min(tok / kPageTokens + g, a.max_pages - 1)]);
+            }
+            if (__any(any) && m == -INFINITY) m = -FLT_MAX;
+        }
     }
     // sums of the four pages' lanes, planes of the output, and both to LDS by the lanes of heads 4 g + i
     {
@@ -668,7 +682,7 @@ __device__ __forceinline__ void kv8_attend(const Kv8AttnArgs& a, int b, int head
             v += f * part_o[w][hd][dim];
         }
         if (s.chunks == 1) {
-            store_as((T*)a.out + ((int64_t)b * a.Hq + head * G) * D + e, sum == 0.f ? 0.f : v / sum);
+            store_as((T*)a.out + ((int64_t)b * a.Hq + head * G) * D + e, kv8_quotient(v, sum, top));
         } else {
             a.partial[at0 * D + e] = v;
             if (dim == 0) reinterpret_cast<float2*>(a.partial + (int64_t)a.batch * a.chunks * a.Hq * D)[at0 + hd] = float2{top, sum};
@@ -760,7 +774,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnArgs a) {
     float top = -INFINITY;
     for (int c = lane; c < s.chunks; c += 64) top = fmaxf(top, ml[at0 + (int64_t)c * a.Hq].x);
     top = wave_max(top);
-    if (top == -INFINITY) top = 0.f;
+    const float ref = top == -INFINITY ? 0.f : top;
     float sum = 0.f, o[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) o[j] = 0.f;
@@ -769,7 +783,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (c0 + u * W >= s.chunks) break;
-            const float w = __builtin_amdgcn_exp2f(p[u].x - top);
+            const float w = __builtin_amdgcn_exp2f(p[u].x - ref);
             sum += w * p[u].y;
 #pragma unroll
             for (int j = 0; j < E; ++j) o[j] += w * v[u][j];
@@ -783,7 +797,7 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8AttnArgs a) {
     if (dim >= D) return;
     const float l = ((sums[0] + sums[1]) + sums[2]) + sums[3];
     const float r = ((part[0][dim] + part[1][dim]) + part[2][dim]) + part[3][dim];
-    store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + dim, l == 0.f ? 0.f : r / l);
+    store_as((T*)a.out + ((int64_t)b * a.Hq + h) * D + dim, kv8_quotient(r, l, top));
 }
 
 int kv8_max_chunks(const sun_model_cfg& c, int batch, int max_pages, int window) {

@@ -602,3 +602,51 @@ def test_workspace_of_a_larger_batch_serves_a_smaller():
         sun.sun_kv8_attention(cache.pool, 0, q, cache.dev_table, i32(lens), out, ws)
         results.append(out)
     assert torch.equal(*results)
+
+
+# ------------------------------------------------------------------ queries that are not numbers
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols, window", [(0, 0), (0, 300), (8000, 0), (8000, 300)])
+@pytest.mark.parametrize("hq, hkv, d", [(8, 2, 64), (8, 2, 128)])
+def test_attention_queries_that_are_not_numbers(hq, hkv, d, cols, window, dtype):
+    """A query with an infinity or a not-a-number has no softmax: not-a-numbers in its head, whether its scores are infinities of one sign, of both or
+    not-a-numbers themselves.  Zeros stay where no token is, and every other head keeps its bits."""
+    lens = [1, 700, 3, 2500, 0, 90, 16, 257]
+    cache = Cache(make_shape(hq, hkv, d, n_layers=1), lens)
+    cache.fill(0, lens)
+    m = cache.mem.cpu().numpy().copy()
+    k = R.pool_views(m, cache.lay, 1, hkv, d)[0][0]
+    for r, n in enumerate(lens):
+        for t in range(n):
+            k[cache.table[r, t // 16], :, t % 16, 5] = 0x38   # every key's dim 5 is 1 times its power: an infinite query there gives scores of one sign
+    cache.mem.copy_(torch.from_numpy(m))
+    cache.table[6, 0] = -1                                    # a request whose page is gone
+    table = torch.full((len(lens), max(cols, cache.table.shape[1])), -1, device=DEV, dtype=torch.int32)
+    table[:, :cache.table.shape[1]] = i32(cache.table)
+    ws = torch.zeros(sun.sun_kv8_attention_workspace_bytes(cache.cfg, len(lens), table.shape[1]), dtype=torch.uint8, device=DEV)
+    q = (torch.randn(len(lens), hq, d, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV) * 1.5).to(DT[dtype])
+
+    def attend(q):
+        out = torch.full_like(q, 33.0)
+        sun.sun_kv8_attention(cache.pool, 0, q.view(len(lens), -1), table, i32(lens), out.view(len(lens), -1), ws, window=window)
+        return out
+
+    clean = attend(q)
+    assert torch.isfinite(clean).all() and (clean[4] == 0).all() and (clean[6] == 0).all()
+    bad = q.clone()
+    inf, nan = float("inf"), float("nan")
+    places = [(0, 0, 5, -inf), (0, 1, 5, inf), (0, 5, 9, nan), (1, 2, 5, -inf), (1, 4, 5, inf), (1, 7, 40, -inf), (2, 3, 5, -inf), (3, 6, 5, -inf), (3, 1, 63, nan),
+              (4, 0, 5, -inf), (4, 1, 5, nan), (5, 7, 5, -inf), (5, 0, 11, inf), (6, 2, 5, -inf), (7, 5, 5, -inf), (7, 4, 5, inf)]
+    want = torch.zeros(len(lens), hq, d, dtype=torch.bool, device=DEV)
+    for r, h, j, value in places:
+        bad[r, h, j] = value
+        want[r, h] = r not in (4, 6)
+    got = attend(bad)
+    assert torch.equal(torch.isnan(got), want)
+    assert torch.equal(got[~want], clean[~want])
+    views = cache.views()
+    for r, n in enumerate(lens):   # the plain form says the same
+        with np.errstate(invalid="ignore"):
+            ref = R.attention(host(bad[r]), views, 0, cache.table[r], n, window, hkv, cache.n_pages)[0]
+        assert np.array_equal(np.isnan(ref), want[r].cpu().numpy())

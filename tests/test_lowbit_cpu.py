@@ -276,7 +276,7 @@ def test_binding_refuses_what_does_not_fit():
         assert e.value.status == 2
 
 
-def test_binding_loads_without_a_gpu_build_of_torch():
+def test_binding_loads_without_a_gpu_build_of_torch(lib):
     """The names that only a GPU build of torch has are not needed to load the module, to ask for sizes or to be refused."""
     code = """
 import torch
