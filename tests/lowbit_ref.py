@@ -138,3 +138,49 @@ def mx4_values(codes, scales):
 def linear_bound(x, w, ref, dtype):
     """K products summed in 32 bits in any order, activations carried exactly, and the output's own rounding."""
     return (x.shape[1] + 8) * 2.0 ** -24 * (np.abs(x) @ np.abs(w).T) + np.abs(ref) * HALF[dtype] * 1.01 + 1e-37
+
+
+# ------------------------------------------------------------------ what only the low bits of 32-bit attention decide
+
+def close_queries(batch, heads, seed=8):
+    """Pairs of 24-bit numbers in [2^20, 2^21) that differ in their last 8 bits alone; the 8 bits before those begin with a one, so that a cut behind
+    the upper 8 and the next 8 bits leaves nothing of the difference."""
+    rng = np.random.default_rng(seed)
+    upper = (rng.integers(128, 256, (batch, heads)) << 8 | rng.integers(128, 256, (batch, heads))) << 8
+    a, b = (rng.integers(0, 256, (batch, heads)) for _ in range(2))
+    b = np.where(a == b, 255 - a, b)
+    return tuple(((upper | x) / 8.0).astype(np.float32) for x in (a, b))
+
+
+def cut(x, planes):
+    """x as its first `planes` truncations to 8 significant bits add up to it."""
+    left, total = np.asarray(x, np.float32), 0.0
+    for _ in range(planes):
+        top = (left.view(np.uint32) & np.uint32(0xffff0000)).view(np.float32)
+        total, left = total + top.astype(np.float64), left - top
+    return total
+
+
+def close_queries_out(q_a, q_b, d):
+    """Two tokens with scores (q_a - q_b) / sqrt d and 0 and values 1 and 0: the first one's weight, and how far 32 bits may be from it.  The products' partial
+    sums are multiples of 2^-3 below 2^21 in any order, so q_a - q_b is exact.  The factor log2(e) / sqrt(d) is good to 2^-23, the product with the maximum and the
+    fused one to 2^-24 each: s * 2^-22 of a weight; two exponentials to 2^-23, the weights' planes and sums to 2^-24 each, the quotient 2^-24: 2^-21 is more."""
+    s = (np.asarray(q_a, np.float64) - np.asarray(q_b, np.float64)) / math.sqrt(d)
+    out = 1 / (1 + np.exp(-s))
+    return out, out * (np.abs(s) * 2.0 ** -22 + 2.0 ** -21)
+
+
+def close_gaps(batch, heads, d, seed=9):
+    """Queries whose scores against a key of one -1 are gaps of e^-0.5 to e^-0.01 between two weights."""
+    return (np.random.default_rng(seed).uniform(0.01, 0.5, (batch, heads)) * math.sqrt(d)).astype(np.float32)
+
+
+def close_gaps_out(q, d):
+    """Two tokens with scores 0 and -g = -q / sqrt d, values 1 and -1: (1 - w) / (1 + w), w = e^-g in [0.6, 1), and how far 32 bits may be from it.  The first
+    weight is 1.  The second is off by g * 2^-22 (see above), 2^-23 of its exponential and 2^-24 for its planes, the numerator by another 2^-24 and
+    the denominator by 2^-24 of itself; the quotient rounds once more."""
+    g = np.asarray(q, np.float64) / math.sqrt(d)
+    w = np.exp(-g)
+    out = (1 - w) / (1 + w)
+    weight = w * (g * 2.0 ** -22 + 2.0 ** -23 + 2.0 ** -24)
+    return out, ((1 + out) * weight + 2.0 ** -24) / (1 + w) + out * 2.0 ** -23

@@ -650,3 +650,57 @@ def test_attention_queries_that_are_not_numbers(hq, hkv, d, cols, window, dtype)
         with np.errstate(invalid="ignore"):
             ref = R.attention(host(bad[r]), views, 0, cache.table[r], n, window, hkv, cache.n_pages)[0]
         assert np.array_equal(np.isnan(ref), want[r].cpu().numpy())
+
+
+# ------------------------------------------------------------------ what only the low bits decide
+
+def two_tokens(dims, values, d, hq, batch):
+    """Requests of two tokens whose keys are zero but for `dims` (request -> [(token, dim, code)], power 0) and whose values are `values` in every dim."""
+    cache = Cache(make_shape(hq, 1, d, n_layers=1), [2] * batch)
+    m = cache.mem.cpu().numpy().copy()
+    k, v, ks, vs = (x[0] for x in R.pool_views(m, cache.lay, 1, 1, d))
+    for r in range(batch):
+        page = cache.table[r, 0]
+        k[page, 0, :2] = 0
+        ks[page, 0, :2] = vs[page, 0, :2] = 127
+        for t in range(2):
+            v[page, 0, :, t] = values[t]
+        for t, j, code in dims[r]:
+            k[page, 0, t, j] = code
+    cache.mem.copy_(torch.from_numpy(m))
+    return cache
+
+
+def attend_two(cache, q):
+    batch, hq, d = q.shape
+    out = torch.full((batch, hq * d), 33.0, device=DEV)
+    ws = torch.zeros(sun.sun_kv8_attention_workspace_bytes(cache.cfg, batch, cache.table.shape[1]), dtype=torch.uint8, device=DEV)
+    sun.sun_kv8_attention(cache.pool, 0, torch.from_numpy(q.reshape(batch, -1)).to(DEV), cache.dev_table, i32([2] * batch), out, ws)
+    return host(out).reshape(batch, hq, d)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_32_bit_queries_carry_24_bits(d):
+    """Scores that are what the last 8 of a query's 24 bits leave."""
+    q_a, q_b = R.close_queries(12, 8)
+    places = [(0, d - 1), (5, 6), (33, 2), (d // 2, 1), (31, 32), (17, 16)] * 2
+    q = np.zeros((12, 8, d), np.float32)
+    for r, (a, b) in enumerate(places):
+        q[r, :, a], q[r, :, b] = q_a[r], q_b[r]
+    cache = two_tokens([[(0, a, 0x38), (0, b, 0xb8)] for a, b in places], (0x38, 0), d, 8, 12)   # token 0: 1 at a, -1 at b, value 1; token 1: zeros
+    got = attend_two(cache, q)
+    ref, bound = R.close_queries_out(q_a, q_b, d)
+    assert (np.abs(got - ref[..., None]) <= bound[..., None]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_32_bit_weights_carry_24_bits(d):
+    """Values that cancel but for what the weights' last bits leave."""
+    gaps = R.close_gaps(12, 8, d)
+    q = np.zeros((12, 8, d), np.float32)
+    for r in range(12):
+        q[r, :, 3 * r] = gaps[r]
+    cache = two_tokens([[(1, 3 * r, 0xb8)] for r in range(12)], (0x38, 0xb8), d, 8, 12)   # scores 0 and -gap / sqrt d, values 1 and -1
+    got = attend_two(cache, q)
+    ref, bound = R.close_gaps_out(gaps, d)
+    assert (np.abs(got - ref[..., None]) <= bound[..., None]).all()

@@ -292,3 +292,27 @@ except sun.SunError as e:
 """
     done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert done.returncode == 0 and done.stdout.strip() == "2", done.stderr
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_bounds_of_the_low_planes_reject_two_planes(d):
+    """What 32-bit attention is measured by where only its low bits decide: three planes pass, two do not."""
+    q_a, q_b = R.close_queries(12, 8)
+    ref, bound = R.close_queries_out(q_a, q_b, d)
+    assert (R.cut(q_a, 3) == q_a).all() and (R.cut(q_b, 3) == q_b).all()
+    for planes, passes in ((3, True), (2, False)):
+        s = ((R.cut(q_a, planes) - R.cut(q_b, planes)) / math.sqrt(d)).astype(np.float32)
+        w = np.exp(-np.abs(s))
+        out = np.where(s > 0, 1 / (1 + w), w / (1 + w))
+        assert ((np.abs(out - ref) <= bound) == passes).all()
+    q = R.close_gaps(12, 8, d)
+    ref, bound = R.close_gaps_out(q, d)
+    w = np.exp(-(q / np.float32(math.sqrt(d)))).astype(np.float32)
+    bf16 = lambda x: torch.from_numpy(x).bfloat16().float().numpy()  # noqa: E731
+    hi = bf16(w)
+    lo = bf16(w - hi)
+    for kept, passes in ((hi.astype(np.float64) + lo + bf16(w - hi - lo), True), (hi.astype(np.float64) + lo, False)):
+        out = (1 - kept) / (1 + w.astype(np.float64))
+        assert (np.abs(out - ref) <= bound).all() == passes
+    two = np.abs((1 - hi.astype(np.float64) - lo) / (1 + w.astype(np.float64)) - ref) / bound
+    assert (two > 2).sum() > 20
