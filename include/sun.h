@@ -543,9 +543,11 @@ int sun_kv8_append(sun_kv8_pool* pool, int layer, int rows, int dtype, const voi
                    const int32_t* page_tables, int n_requests, int max_pages, const void* q_norm, const void* k_norm,
                    void* q_out, void* stream, unsigned flags);
 
-/* Bytes of device workspace sun_kv8_attention needs for up to `batch` requests with max_pages table columns, any window; 0 for
- * sizes that it refuses. */
+/* Bytes of device workspace sun_kv8_attention needs for up to `batch` requests with max_pages table columns and any window, or a
+ * window in [1, window] (window 0: any); 0 for sizes that it refuses.  A window bounds the parts that a request is split into, so it may
+ * take far less, and is taken where the tables alone are more than one launch takes. */
 size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages);
+size_t sun_kv8_attention_window_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages, int window);
 
 /*
  * Attention of one new token per request over one layer of an 8-bit pool, split over each cache's length and joined:

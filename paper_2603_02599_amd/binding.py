@@ -37,7 +37,7 @@ EXPORTS = [
     "sun_paged_attention", "sun_paged_attention_static", "sun_paged_attention_static_bytes",
     "sun_paged_attention_static_limit", "sun_linear",
     "sun_kv8_pool_bytes", "sun_kv8_pool_create", "sun_kv8_pool_layout", "sun_kv8_pool_destroy", "sun_kv8_append",
-    "sun_kv8_attention", "sun_kv8_attention_workspace_bytes",
+    "sun_kv8_attention", "sun_kv8_attention_workspace_bytes", "sun_kv8_attention_window_workspace_bytes",
     "sun_mx4_quantize", "sun_mx4_dequantize", "sun_mx4_linear", "sun_mx4_linear_workspace_bytes",
     "sun_hbm_read_probe", "sun_profile_read", "sun_profile_reset", "sun_last_error", "sun_version",
 ]
@@ -115,7 +115,7 @@ def lib() -> C.CDLL:
         for f in ("sun_kv_pool_bytes", "sun_weights_pack_bytes", "sun_qweights_pack_bytes", "sun_workspace_bytes",
                   "sun_prefill_workspace_bytes", "sun_serve_workspace_bytes", "sun_paged_attention_static_bytes",
                   "sun_paged_attention_static_limit", "sun_kv8_pool_bytes", "sun_kv8_attention_workspace_bytes",
-                  "sun_mx4_linear_workspace_bytes"):
+                  "sun_kv8_attention_window_workspace_bytes", "sun_mx4_linear_workspace_bytes"):
             getattr(L, f).restype = C.c_size_t
         L.sun_kv_pool_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int64, C.c_int]
         L.sun_kv_pool_create.argtypes = [C.POINTER(ModelCfg), C.c_void_p, C.c_size_t, C.c_int, C.c_int,
@@ -167,6 +167,7 @@ def lib() -> C.CDLL:
                                      C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p,
                                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint]
         L.sun_kv8_attention_workspace_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int, C.c_int]
+        L.sun_kv8_attention_window_workspace_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int, C.c_int, C.c_int]
         L.sun_kv8_attention.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
                                         C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint]
         L.sun_mx4_quantize.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
@@ -644,6 +645,11 @@ def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page
 
 def sun_kv8_attention_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int) -> int:
     return int(lib().sun_kv8_attention_workspace_bytes(C.byref(cfg), batch, max_pages))
+
+
+def sun_kv8_attention_window_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int, window: int) -> int:
+    """For calls with a window in [1, window] alone (0: any)."""
+    return int(lib().sun_kv8_attention_window_workspace_bytes(C.byref(cfg), batch, max_pages, window))
 
 
 def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, workspace, window: int = 0, stream=None,

@@ -1556,12 +1556,16 @@ static bool kv8_attention_fits(const sun_model_cfg& c, int batch, int chunks) {
     return (int64_t)batch * std::max<int64_t>(c.n_q_heads, (int64_t)c.n_kv_heads * chunks) <= kMaxGroups;
 }
 
-size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages) {
-    if (!cfg || batch < 1 || batch > kKv8MaxBatch || max_pages < 1 || max_pages > kKv8MaxPages || check_cfg(cfg) != SUN_OK) return 0;
-    if (!kv8_attention_fits(*cfg, batch, kv8_max_chunks(*cfg, batch, max_pages, 0))) return 0;
+size_t sun_kv8_attention_window_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages, int window) {
+    if (!cfg || batch < 1 || batch > kKv8MaxBatch || max_pages < 1 || max_pages > kKv8MaxPages || window < 0 || check_cfg(cfg) != SUN_OK) return 0;
+    if (!kv8_attention_fits(*cfg, batch, kv8_max_chunks(*cfg, batch, max_pages, window))) return 0;
     size_t most = 1;   // fewer requests have more chunks each
-    for (int b = 1; b <= batch; ++b) most = std::max(most, kv8_partial_floats(*cfg, b, kv8_max_chunks(*cfg, b, max_pages, 0)) * 4);
+    for (int b = 1; b <= batch; ++b) most = std::max(most, kv8_partial_floats(*cfg, b, kv8_max_chunks(*cfg, b, max_pages, window)) * 4);
     return align_up(most);
+}
+
+size_t sun_kv8_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int max_pages) {
+    return sun_kv8_attention_window_workspace_bytes(cfg, batch, max_pages, 0);
 }
 
 static int validate_kv8_requests(const Kv8Pool& pool, int batch, const int32_t* page_tables, int max_pages, const int32_t* n_tokens,

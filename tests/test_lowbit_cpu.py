@@ -316,3 +316,44 @@ def test_bounds_of_the_low_planes_reject_two_planes(d):
         assert (np.abs(out - ref) <= bound).all() == passes
     two = np.abs((1 - hi.astype(np.float64) - lo) / (1 + w.astype(np.float64)) - ref) / bound
     assert (two > 2).sum() > 20
+
+
+@pytest.mark.parametrize("hkv, hq", [(1, 8), (2, 4), (8, 40)])
+def test_attention_window_workspace_is_enough(lib, hkv, hq):
+    """Every windowed call that is accepted has a size: it holds the chunks of any length in the window, for fewer requests and shorter windows too."""
+    cfg = sun.make_cfg(wl.Shape("s", 1, 256, hq, hkv, 128, 128, 32), "f32")
+    whole = lambda b, p: lib.sun_kv8_attention_workspace_bytes(C.byref(cfg), b, p)  # noqa: E731
+    size = lambda b, p, w: lib.sun_kv8_attention_window_workspace_bytes(C.byref(cfg), b, p, w)  # noqa: E731
+    for pages in (1, 40, 2049, 1 << 26):
+        need = 0
+        rooms = {w: [] for w in (1, 241, 242, 700, 1500, 40000)}
+        for batch in range(1, 1025):
+            assert size(batch, pages, 0) == whole(batch, pages) and (whole(batch, pages) == 0 or size(batch, pages, 700) <= whole(batch, pages))
+            for window, rooms_of in rooms.items():
+                most = min(pages * 16, window + 15)   # the pages in front of a window are whole
+                ends = [most] + [e for ch in (256, 512, 1024, 2048) for e in ((2 * ch * 512 - 1) // (hkv * batch),) if 0 < e <= most]
+                chunks = max(-(-e // chunk(e, batch, hkv)) for e in ends)
+                rooms_of.append((size(batch, pages, window), batch * chunks * hq * 130 * 4 if chunks > 1 else 0))
+        for window, rooms_of in rooms.items():
+            got, needs = zip(*rooms_of)
+            assert all(g >= n and g > 0 for g, n in zip(got, np.maximum.accumulate(needs))), (pages, window)
+            assert list(got) == sorted(got) and got[-1] <= max(needs) + 256
+        assert all(a[0] <= b[0] for w, v in ((1, 241), (241, 242), (242, 700), (700, 1500), (1500, 40000)) for a, b in zip(rooms[w], rooms[v]))
+    assert size(2, 40, -1) == size(0, 40, 5) == size(1025, 40, 5) == size(2, 0, 5) == size(2, (1 << 26) + 1, 5) == 0
+    assert lib.sun_kv8_attention_window_workspace_bytes(None, 1, 1, 1) == 0
+    assert sun.sun_kv8_attention_window_workspace_bytes(cfg, 256, 8192, 1500) == size(256, 8192, 1500)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls get as far as the launch, which must find no GPU")
+def test_windowed_calls_have_the_size_that_they_ask_for(lib):
+    """Batches and tables that no call without a window may have: with the bytes that were asked for a windowed one fails for want of a GPU only."""
+    cfg, rc, pool = make_pool(lib)
+    assert rc == 0
+    hkv = wl.TINY.n_kv_heads
+    for batch, pages in ((1024, 1 << 26), (1024, (1 << 29) // hkv // 128 + 128), (256, 8192), (1, 1 << 26)):
+        for window in (1, 4096, 100000):
+            need = lib.sun_kv8_attention_window_workspace_bytes(C.byref(cfg), batch, pages, window)
+            assert need > 0
+            for w in (1, window // 2 + 1, window):
+                assert lib.sun_kv8_attention(pool, 0, batch, 0, FAKE, FAKE, pages, FAKE, w, FAKE, FAKE, need, None, 0) not in (0, 2, 4), (batch, pages, window, w)
+    lib.sun_kv8_pool_destroy(pool)
