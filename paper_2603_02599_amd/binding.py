@@ -574,8 +574,12 @@ _current_gpu = getattr(torch._C, "_cuda_getDevice", None)
 def _int32(**values):
     """Counts that the library takes in 32 bits, which a conversion would cut without a word."""
     for name, v in values.items():
-        if not -1 << 31 <= v < 1 << 31:
+        if not _fits(v):
             _refuse(f"{name} = {v} is beyond 32 bits")
+
+
+def _fits(*values) -> bool:
+    return all(-1 << 31 <= v < 1 << 31 for v in values)
 
 
 def _call(device: int, stream, fn, args, behind=()):
@@ -589,7 +593,7 @@ def _call(device: int, stream, fn, args, behind=()):
 
 
 def sun_kv8_pool_bytes(cfg: ModelCfg, n_pages: int, page_tokens: int = 16) -> int:
-    return int(lib().sun_kv8_pool_bytes(C.byref(cfg), n_pages, page_tokens))
+    return int(lib().sun_kv8_pool_bytes(C.byref(cfg), n_pages, page_tokens)) if _fits(page_tokens) else 0
 
 
 class Kv8Pool:
@@ -644,12 +648,12 @@ def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page
 
 
 def sun_kv8_attention_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int) -> int:
-    return int(lib().sun_kv8_attention_workspace_bytes(C.byref(cfg), batch, max_pages))
+    return int(lib().sun_kv8_attention_workspace_bytes(C.byref(cfg), batch, max_pages)) if _fits(batch, max_pages) else 0
 
 
 def sun_kv8_attention_window_workspace_bytes(cfg: ModelCfg, batch: int, max_pages: int, window: int) -> int:
     """For calls with a window in [1, window] alone (0: any)."""
-    return int(lib().sun_kv8_attention_window_workspace_bytes(C.byref(cfg), batch, max_pages, window))
+    return int(lib().sun_kv8_attention_window_workspace_bytes(C.byref(cfg), batch, max_pages, window)) if _fits(batch, max_pages, window) else 0
 
 
 def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, workspace, window: int = 0, stream=None,
@@ -699,7 +703,7 @@ def sun_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.d
 
 
 def sun_mx4_linear_workspace_bytes(N: int, K: int, rows: int) -> int:
-    return int(lib().sun_mx4_linear_workspace_bytes(N, K, rows))
+    return int(lib().sun_mx4_linear_workspace_bytes(N, K, rows)) if _fits(N, K, rows) else 0
 
 
 def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):

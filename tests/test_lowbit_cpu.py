@@ -357,3 +357,15 @@ def test_windowed_calls_have_the_size_that_they_ask_for(lib):
             for w in (1, window // 2 + 1, window):
                 assert lib.sun_kv8_attention(pool, 0, batch, 0, FAKE, FAKE, pages, FAKE, w, FAKE, FAKE, need, None, 0) not in (0, 2, 4), (batch, pages, window, w)
     lib.sun_kv8_pool_destroy(pool)
+
+
+def test_binding_has_no_size_for_counts_beyond_32_bits(lib):
+    """Counts that the library takes in 32 bits are not cut to some smaller call's."""
+    cfg, far = sun.make_cfg(wl.TINY, "f32"), 1 << 32
+    assert sun.sun_mx4_linear_workspace_bytes(100, 64, 40) > 0 and sun.sun_kv8_attention_workspace_bytes(cfg, 2, 100) > 0
+    for n, k, rows in ((far + 100, 64, 40), (100, far + 64, 40), (100, 64, far + 40)):
+        assert sun.sun_mx4_linear_workspace_bytes(n, k, rows) == 0
+    for batch, pages in ((far + 2, 100), (2, far + 100)):
+        assert sun.sun_kv8_attention_workspace_bytes(cfg, batch, pages) == sun.sun_kv8_attention_window_workspace_bytes(cfg, batch, pages, 5) == 0
+    assert sun.sun_kv8_attention_window_workspace_bytes(cfg, 2, 100, far + 5) == 0
+    assert sun.sun_kv8_pool_bytes(cfg, 4, far + 16) == 0 < sun.sun_kv8_pool_bytes(cfg, 4, 16)
