@@ -704,3 +704,12 @@ def test_attention_32_bit_weights_carry_24_bits(d):
     got = attend_two(cache, q)
     ref, bound = R.close_gaps_out(gaps, d)
     assert (np.abs(got - ref[..., None]) <= bound[..., None]).all()
+
+
+def test_keys_that_are_no_matrix_are_refused():
+    cache = Cache(make_shape(4, 2, 64), [40])
+    k, at = torch.zeros(1, 128, device=DEV), i32([0])
+    for bad in (k[0, 0], k[0], k[None]):
+        with pytest.raises(sun.SunError) as e:
+            sun.sun_kv8_append(cache.pool, 0, None, bad, bad, at, at, cache.dev_table, None)
+        assert e.value.status == 2

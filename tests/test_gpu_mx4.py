@@ -233,3 +233,12 @@ def test_outputs_belong_to_the_stream_that_fills_them(dtype, raw):
     sun.sun_mx4_linear(codes, scales, x[:5], on, workspace, stream=stream)
     here.wait_stream(side)
     assert torch.equal(on, multiply(codes, scales, x[:5], "f32"))
+
+
+def test_activations_that_are_no_matrix_are_refused():
+    codes, scales, x = make_linear(16, 64, 1, "f32")
+    ws, out = torch.zeros(sun.sun_mx4_linear_workspace_bytes(16, 64, 1), device=DEV, dtype=torch.uint8), torch.zeros(1, 16, device=DEV)
+    for bad in (x[0, 0], x[0], x[None], x[:, :, None]):
+        with pytest.raises(sun.SunError) as e:
+            sun.sun_mx4_linear(codes, scales, bad, out, ws)
+        assert e.value.status == 2
