@@ -340,7 +340,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
     }
 }
 
-// Some dozen rows, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Of its eight waves WN share the columns, NT tiles
+// Some dozen rows, all in one workgroup, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Of its eight waves WN share the columns, NT tiles
 // each, WK have chunks of k of their own and WJ share the eighths of a block of 32; the sums of WK and WJ meet in LDS at the end.  Codes, powers and activations
 // of ST - 1 steps are under way into LDS while one is computed on.  A step is a chunk of 128 k for each of WK, of one plane of the activations.
 // 28672 x 4096 in bf16 at 32 / 64 / 128 rows: 17.7 / 23 to 25 / 33.7 us, the weights' 62 MB at 3.5 / 2.6 / 1.8 TB/s.  What bounds it is the compute unit: converting the
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args a) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ST * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c16 = lane & 15, g = lane >> 4;
     const int wn = wave % WN, wj = wave / WN % WJ, wk = wave / WC, wq = wave % WC;
-    const int nb = blockIdx.x * (16 * CF), n0 = nb + wn * 16 * NT, row0 = blockIdx.y * (16 * RT);
+    const int nb = blockIdx.x * (16 * CF), n0 = nb + wn * 16 * NT;
     const int blocks = a.K / kMxBlock, chunks = (blocks + 3) / 4;
     const int per = (chunks + gridDim.z - 1) / gridDim.z, c0 = blockIdx.z * per, c1 = min(chunks, c0 + per), steps = (c1 - c0 + WK - 1) / WK * P;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args a) {
 #pragma unroll
     for (int i = 0; i < XW; ++i) {
         const int f = wq * XW + i;   // row tile f / 4, block f % 4 of the chunk
-        x[i] = a.x + (int64_t)min(row0 + 16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
+        x[i] = a.x + (int64_t)min(16 * (f >> 2) + row16, a.rows - 1) * a.ld_x + (f & 3) * 32 + piece * 8;
     }
     int chunk = c0 + wk, plane = 0, fill = 0;   // what is requested next, and its place in the ring
     // Request i of OPS.  Behind the last chunk zeros are requested, so that every step has the same number of requests under way.
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args a) {
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = row0 + 16 * r + c16;
+        const int row = 16 * r + c16;
         if (row >= a.rows) continue;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
