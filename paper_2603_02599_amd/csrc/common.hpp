@@ -51,6 +51,12 @@ constexpr int kMaxPrefillTile = 2048;  // rows of a prefill block (bf16 projecti
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint16_t f32_to_bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+// to a float or the bits of a bf16 value
+template <class T>
+__device__ __forceinline__ void store_as(T* p, float v) {
+    if constexpr (sizeof(T) == 4) *p = v;
+    else *p = f32_to_bf16_bits(v);
+}
 __device__ __forceinline__ float bf16_bits_to_f32(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

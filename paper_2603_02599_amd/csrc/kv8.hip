@@ -406,12 +406,6 @@ __device__ __forceinline__ float below(float x) {
     return fabsf(x) < INFINITY ? r : 0.f;
 }
 
-template <class T>
-__device__ __forceinline__ void store_as(T* p, float v) {
-    if constexpr (sizeof(T) == 4) *p = v;
-    else *p = f32_to_bf16_bits(v);
-}
-
 // What is stored of a weighted sum v, the weights' sum and the largest score: zeros where there is no token
 __device__ __forceinline__ float kv8_quotient(float v, float sum, float top) { return sum == 0.f && top == -INFINITY ? 0.f : v / sum; }
 

@@ -212,12 +212,6 @@ __device__ __forceinline__ bf16x8 mx4_values(uint32_t w, float scale) {
 // the converter reads the power's exponent field: all ones is not-a-number
 __device__ __forceinline__ float mx4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-template <class T>
-__device__ __forceinline__ void store_as(T* p, float v) {
-    if constexpr (sizeof(T) == 4) *p = v;
-    else *p = f32_to_bf16_bits(v);
-}
-
 __device__ u32x4_s g_mx4_zeros = {0, 0, 0, 0};   // what lanes behind the last column are given
 
 // Requests from memory straight into LDS, the address a lane's own: 16 bytes a lane (lane i's land at lds_byte + 16 i), or a byte, which
