@@ -812,10 +812,12 @@ size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks) {
 }
 
 // How chunks come to workgroups.  A workgroup behind a request's last chunk costs 1.25 ns, counting the chunks 1 us and more for each of the 512
-// workgroups that are on the chip at a time.  64 requests of 500 tokens, table of 512 / 1024 / 8192 pages (4096 / 8192 / 32768 workgroups): 22 / 28 / 56 us
-// with a workgroup for each, 28 in all three dealt; 64 of 4096 tokens, 8192 workgroups: 109 and 99; 256 of 1000, 32768: 136 and 99.  Where one chunk a
-// request is all there can be, none is behind the last: 1024 of 100 tokens 83 us, dealt 106.
-constexpr int64_t kKv8Room = 4096;
+// workgroups that are on the chip at a time.  64 requests of 500 tokens, table of 512 / 1024 / 1536 / 2048 / 8192 pages (2048 / 4096 / 6144 / 8192 / 32768
+// workgroups): 24.5 / 26.2 / 28.3 / 30.6 / 58 us with a workgroup for each, 30.3 in all five dealt; 64 of 4096 tokens, 6144 / 8192 / 16384: 97.8 / 100.2 / 111
+// and 101; 256 of 1000, 16384: 112 and 106; 24 of 2048 to 32768 tokens, 6144: 162 and 158.5.  One to 256 requests on 2 and 8 KV heads, lengths from a
+// sixteenth of the table's to all of it: up to 8192 none of 64 is more than 1.5 % faster dealt and 50 are 2 to 30 % slower, at 12288 three of seven are
+// faster.  Where one chunk a request is all there can be, none is behind the last: 1024 of 100 tokens 86 us, dealt 106.
+constexpr int64_t kKv8Room = 8192;
 constexpr int kKv8Dealt = 2048;   // 1024: 256 requests of up to 4000 tokens 170 -> 178 us, 256 of 300 52.7 -> 49.1
 
 template <class T, int D>

@@ -607,7 +607,7 @@ def test_workspace_of_a_larger_batch_serves_a_smaller():
 # ------------------------------------------------------------------ queries that are not numbers
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("cols, window", [(0, 0), (0, 300), (8000, 0), (8000, 300)])
+@pytest.mark.parametrize("cols, window", [(0, 0), (0, 300), (8000, 0), (8000, 300), (150000, 0)])
 @pytest.mark.parametrize("hq, hkv, d", [(8, 2, 64), (8, 2, 128)])
 def test_attention_queries_that_are_not_numbers(hq, hkv, d, cols, window, dtype):
     """A query with an infinity or a not-a-number has no softmax: not-a-numbers in its head, whether its scores are infinities of one sign, of both or
