@@ -542,12 +542,6 @@ def _want(name: str, t: torch.Tensor, device: int, dtype, shape, rows: bool = Fa
             + f"; is {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
-def _rows(t: torch.Tensor, name: str) -> int:
-    if t.dim() != 2:
-        _refuse(f"{name} must be [rows, columns], is {tuple(t.shape)}")
-    return t.shape[0]
-
-
 def _row_stride(t: torch.Tensor) -> int:
     rows, cols = t.shape
     return t.stride(0) if rows > 1 else cols
@@ -580,7 +574,7 @@ _current_gpu = getattr(torch._C, "_cuda_getDevice", None)
 def _int32(**values):
     """Counts that the library takes in 32 bits, which a conversion would cut without a word."""
     for name, v in values.items():
-        if not _fits(v):
+        if not -1 << 31 <= v < 1 << 31:
             _refuse(f"{name} = {v} is beyond 32 bits")
 
 
@@ -638,7 +632,9 @@ def sun_kv8_append(pool: Kv8Pool, layer: int, q, k, v, positions, requests, page
     """k, v [rows, Hkv*d] (and q [rows, Hq*d], or None with q_out None), rows at any stride; positions, requests int32 [rows];
     page_tables int32 [n_requests, max_pages]; gains [d] of the same type as q, k and v."""
     dev, t, i32, kd = _gpu(pool.mem), k.dtype, torch.int32, pool.kv_dim
-    rows, (n_requests, max_pages) = _rows(k, "k"), _table(page_tables)
+    if k.dim() != 2:
+        _refuse("k must be [rows, Hkv*d]")
+    rows, (n_requests, max_pages) = k.shape[0], _table(page_tables)
     _int32(layer=layer, rows=rows, n_requests=n_requests)
     if q is None:
         pq = lq = None
@@ -716,7 +712,9 @@ def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):
     """out [rows, N] = x [rows, K] W^T; x and out float32 or bfloat16 each, rows at any stride."""
     dev = _gpu(codes)
     pc, ps, n, k = _mx4(codes, scales, dev)
-    rows, tx, to = _rows(x, "x"), x.dtype, out.dtype
+    if x.dim() != 2:
+        _refuse("x must be [rows, K]")
+    rows, tx, to = x.shape[0], x.dtype, out.dtype
     _int32(rows=rows)
     _call(dev, stream, lib().sun_mx4_linear, (
         pc, ps, n, k, rows, _want("x", x, dev, tx, (rows, k), True), _dtype(x, "x"), _row_stride(x),
