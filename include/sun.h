@@ -526,9 +526,10 @@ void sun_kv8_pool_destroy(sun_kv8_pool* pool);
  *   page_tables dev int32 [n_requests, max_pages]
  *   q_norm, k_norm  dev [d]: gains of the head norm (RMSNorm over head_dim, eps = rms_eps, before the rotation); required
  *              if cfg.qk_norm (q_norm only with q), NULL if not
- *   q_out      dev [rows, Hq*d], contiguous: q, normed and rotated; may be q itself where ld_q = Hq*d
+ *   q_out      dev [rows, Hq*d], contiguous: q, normed and rotated; may be q itself where ld_q = Hq*d, and must not overlap the
+ *              other inputs, or q in any other way
  * Angles are computed in 64 bits from cfg.rope_* and their cosines and sines rounded to 32; a key is computed in 64 bits and
- * rounded to 32 once before it is rounded to the cache's 8.  A row whose position has no page (beyond the table, or an entry outside
+ * rounded to 32 once before it is rounded to the cache's 8, a query in 32.  A row whose position has no page (beyond the table, or an entry outside
  * the pool, or a request outside [0, n_requests)) leaves the pool as it is; its q_out is written.  Only the entries of the
  * given positions are written.  No two rows may name the same position of the same page, and a position must not be
  * read by work of another stream meanwhile.
@@ -582,7 +583,8 @@ int sun_kv8_attention(const sun_kv8_pool* pool, int layer, int batch, int dtype,
  * sun_mx4_quantize: w dev dense, dtype SUN_F32 or SUN_BF16 -> codes, scales.  s = max(floor(log2 max|w|) - 2, -127) + 127 over
  * the block, code = w * 2^(127 - s) rounded to the nearest (ties to the even code), at most 6; a block with a value that is
  * not finite gets scale byte 255 and codes 0, one of zeros scale byte 0.
- * sun_mx4_dequantize: the values, exact in either type.
+ * sun_mx4_dequantize: the values, exact in either type; those of 2^128 and more (4 and 6 at scale byte 253, 2 to 6 at 254, which
+ * sun_mx4_quantize does not write) are infinite.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (rows < 1, cols < 32 or no multiple of 32, dtype, alignment).
  */
 int sun_mx4_quantize(const void* w, int dtype, int rows, int cols, void* codes, void* scales, void* stream);
@@ -595,7 +597,8 @@ size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows);
  * out[b, n] = sum_k W[n, k] x[b, k] with W [N, K] in the format above, from one row to a prefill block.  Enqueued on `stream`.
  *   x    dev [rows, K], type x_dtype, row stride ld_x elements; out dev [rows, N], type out_dtype, row stride ld_out
  * Weights and activations enter the matrix cores exactly (32-bit activations as three bf16 planes), sums are in 32 bits; values
- * below the normal numbers of bf16 (2^-126) may count as zero.  A row's result depends on N, K, the row count and the types, not on
+ * below the normal numbers of bf16 (2^-126) may count as zero, and weights of 2^128 and more are infinite, in a product with 32-bit activations
+ * not-a-numbers.  A row's result depends on N, K, the row count and the types, not on
  * the other rows' values.  out must not overlap x or the matrix.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (N, rows < 1, K < 32 or no multiple of 32, N > 2^28, K or rows > 2^30, more than 2^22 tiles of
  * 128 x 128 outputs, a type, codes or x not 16-byte aligned, ld_x < K or no

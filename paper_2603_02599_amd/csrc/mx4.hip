@@ -241,7 +241,8 @@ __device__ __forceinline__ void store_quad(const Mx4Args& a, T* out, int64_t ld,
 }
 
 // Up to sixteen rows: reading the weights is what costs, and latency where they are few: 6144 x 4096 at one row (13.4 MB) takes 5.5 us, of which about four are a launch
-// and one request's way; 28672 x 4096 at one row 13.1 us (4.8 TB/s), at 16 18.1, in 32 bits 22.8 and 39.5, where cutting x into planes in every workgroup shows.
+// and one request's way; 28672 x 4096 at one row 13.1 us (4.8 TB/s) while the memory-side cache holds the matrix and 17.3 where it is read from memory, at 16 18.1 and 23.1.
+// In 32 bits 26.3 and 40.8: every workgroup cuts all sixteen places into planes.  Rows of x are read a lane a row, which the address unit takes line by line.
 // 16 * NT columns a workgroup, the chunks of 128 k dealt to its eight waves, whose sums meet in LDS.  A wave has U chunks under
 // way at a time: their codes and powers go into LDS (see the next kernel for the order), its activations straight into the operand's registers: a
 // row that is not there is not asked for.  32-bit activations are cut into their planes here.
@@ -337,9 +338,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
 // Some dozen rows, all in one workgroup, where reading the weights is what costs: 16 * RT rows and 16 * NT * WN columns a workgroup.  Of its eight waves WN share the columns, NT tiles
 // each, WK have chunks of k of their own and WJ share the eighths of a block of 32; the sums of WK and WJ meet in LDS at the end.  Codes, powers and activations
 // of ST - 1 steps are under way into LDS while one is computed on.  A step is a chunk of 128 k for each of WK, of one plane of the activations.
-// 28672 x 4096 in bf16 at 32 / 64 / 128 rows: 17.7 / 23 to 25 / 33.7 us, the weights' 62 MB at 3.5 / 2.6 / 1.8 TB/s.  What bounds it is the compute unit: converting the
-// codes (a conversion of two values takes a wave 4.4 cycles), requests (a KiB of activations or codes takes the address unit 20) and products take turns on each
-// chunk, and 224 workgroups leave 32 of 256 units idle.  Rings apart for codes and activations with waves for each, a rotated start along k and deeper rings
+// 28672 x 4096 in bf16 at 32 / 64 / 128 rows: 17.7 / 23 to 25 / 33.7 us while the memory-side cache holds the weights' 62 MB, 21.5 / 26.4 / 38.6 from memory; in 32 bits 46 / 61 / 103.
+// No unit bounds it (at 64 rows matrix cores 21 %, vector ALU 20 % busy, a wave waits 31 % of its time): one workgroup a compute unit, whose waves meet at each step, so that converting the
+// codes (a conversion of two values takes a wave 4.4 cycles), requests (a KiB of activations or codes takes the address unit 20) and products come one after
+// another, and 224 workgroups leave 32 of 256 units idle.  Rings apart for codes and activations with waves for each, a rotated start along k and deeper rings
 // were no faster.
 //
 // A request reads 64 bytes of each of sixteen rows, four lanes side by side on a row (the address unit takes four neighbouring lanes on one line
