@@ -202,10 +202,21 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _current(device, stream):
-    """`stream` as GPU `device`'s current one: what is allocated inside belongs to it.  Memory of the pool of another stream may still be
-    read by work that is queued there when it is handed out, and may be handed out again before `stream` is done with it."""
-    return torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device))
+def _aside(device, stream, shape, dtype) -> torch.Tensor:
+    """An empty tensor of the pool of `stream`, which is about to fill it.  A block of the current stream's pool may still be read by work that is
+    queued there.  Nor is it handed out again before what the current stream, whose work may use it, has queued by then is done."""
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(here)
+    return t
+
+
+def _pack_buffer(cfg: ModelCfg, nbytes: int, device, stream) -> Optional[torch.Tensor]:
+    if cfg.act_dtype != SUN_BF16:
+        return None
+    n = max(nbytes, 256)
+    return torch.empty(n, dtype=torch.uint8, device=device) if stream is None else _aside(device, stream, n, torch.uint8)
 
 
 def make_cfg(shape, act_dtype: str) -> ModelCfg:
@@ -290,9 +301,6 @@ def sun_weights_pack_bytes(cfg: ModelCfg) -> int:
 
 def sun_weights_create(cfg: ModelCfg, w: Dict[str, object], stream=None, keep_sources: bool = True) -> Weights:
     """w: dict from workloads.make_weights (torch CUDA tensors).  Allocates the pack buffer with torch, from the pool of the stream that packs."""
-    if stream is not None:
-        with _current(w["embed"].device, stream):
-            return sun_weights_create(cfg, w, keep_sources=keep_sources)
     ptrs = WeightPtrs()
     keep: List[object] = []
     ptrs.embed = w["embed"].data_ptr()
@@ -303,9 +311,9 @@ def sun_weights_create(cfg: ModelCfg, w: Dict[str, object], stream=None, keep_so
     ptrs.gf, ptrs.wlm = w["gf"].data_ptr(), w["wlm"].data_ptr()
     _set_head_norms(ptrs, w, cfg, keep)
     nbytes = sun_weights_pack_bytes(cfg)
-    pack = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=w["embed"].device) if cfg.act_dtype == SUN_BF16 else None
+    pack = _pack_buffer(cfg, nbytes, w["embed"].device, stream)
     out = C.c_void_p()
-    _check(lib().sun_weights_create(C.byref(cfg), C.byref(ptrs), _p(pack), nbytes, _stream(None), C.byref(out)))
+    _check(lib().sun_weights_create(C.byref(cfg), C.byref(ptrs), _p(pack), nbytes, _stream(stream), C.byref(out)))
     keep.append(pack)
     if keep_sources or cfg.act_dtype == SUN_F32:
         keep.append(w)
@@ -322,9 +330,6 @@ def sun_qweights_create(cfg: ModelCfg, w: Dict[str, object], quant: Dict[str, li
                         stream=None) -> Weights:
     """quant[key][layer] = (q uint8 [out, in/2], s fp16 [out, in/128], z fp16 [out, in/128]) CUDA tensors;
     w supplies embed, g1, g2, gf, wlm.  The pack buffer is from the pool of the stream that packs."""
-    if stream is not None:
-        with _current(w["embed"].device, stream):
-            return sun_qweights_create(cfg, w, quant, group)
     ptrs = QWeightPtrs()
     keep: List[object] = [w["embed"], w["g1"], w["g2"], w["gf"], w["wlm"], quant]
     ptrs.embed = w["embed"].data_ptr()
@@ -340,9 +345,9 @@ def sun_qweights_create(cfg: ModelCfg, w: Dict[str, object], quant: Dict[str, li
     ptrs.gf, ptrs.wlm = w["gf"].data_ptr(), w["wlm"].data_ptr()
     _set_head_norms(ptrs, w, cfg, keep)
     nbytes = sun_qweights_pack_bytes(cfg, group)
-    pack = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=w["embed"].device) if cfg.act_dtype == SUN_BF16 else None
+    pack = _pack_buffer(cfg, nbytes, w["embed"].device, stream)
     out = C.c_void_p()
-    _check(lib().sun_qweights_create(C.byref(cfg), C.byref(ptrs), group, _p(pack), nbytes, _stream(None), C.byref(out)))
+    _check(lib().sun_qweights_create(C.byref(cfg), C.byref(ptrs), group, _p(pack), nbytes, _stream(stream), C.byref(out)))
     keep.append(pack)
     return Weights(out.value, keep, True)
 
@@ -350,16 +355,13 @@ def sun_qweights_create(cfg: ModelCfg, w: Dict[str, object], quant: Dict[str, li
 def sun_quantize_w4(w: torch.Tensor, group: int = 128, mode: str = "asym", stream=None):
     """Returns (q uint8 [rows, cols/2], s fp16 [rows, cols/group], z fp16 [rows, cols/group]); mode "sym_noz" is
     the symmetric grid without stored zero points (z is None: 8 everywhere).  They belong to the stream that fills them."""
-    if stream is not None:
-        with _current(w.device, stream):
-            return sun_quantize_w4(w, group, mode)
     rows, cols = w.shape
     dt = {torch.float32: SUN_F32, torch.bfloat16: SUN_BF16}[w.dtype]
-    q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=w.device)
-    s = torch.empty((rows, cols // group), dtype=torch.float16, device=w.device)
-    z = torch.empty_like(s) if mode != "sym_noz" else None
+    new = (lambda shape, t: torch.empty(shape, dtype=t, device=w.device)) if stream is None else (lambda shape, t: _aside(w.device, stream, shape, t))
+    q, s = new((rows, cols // 2), torch.uint8), new((rows, cols // group), torch.float16)
+    z = new(s.shape, torch.float16) if mode != "sym_noz" else None
     _check(lib().sun_quantize_w4(_p(w), dt, rows, cols, group, {"asym": 0, "sym": 1, "sym_noz": 1}[mode], _p(q), _p(s),
-                                 _p(z), _stream(None)))
+                                 _p(z), _stream(stream)))
     return q, s, z
 
 
@@ -675,12 +677,12 @@ def sun_mx4_quantize(w: torch.Tensor, stream=None):
     if w.dim() != 2 or w.shape[1] % 32:
         _refuse("w must be [rows, cols], cols a multiple of 32")
     (rows, cols), dev = w.shape, _gpu(w)
-    if stream is not None:
-        with _current(dev, stream):
-            return sun_mx4_quantize(w)
     _int32(rows=rows, cols=cols)
-    codes, scales = w.new_empty((rows, cols // 2), dtype=torch.uint8), w.new_empty((rows, cols // 32), dtype=torch.uint8)
-    _call(dev, None, lib().sun_mx4_quantize, (_want("w", w, dev, w.dtype, w.shape), _dtype(w, "w"), rows, cols, codes.data_ptr(), scales.data_ptr()))
+    if stream is None:
+        codes, scales = w.new_empty((rows, cols // 2), dtype=torch.uint8), w.new_empty((rows, cols // 32), dtype=torch.uint8)
+    else:
+        codes, scales = _aside(dev, stream, (rows, cols // 2), torch.uint8), _aside(dev, stream, (rows, cols // 32), torch.uint8)
+    _call(dev, stream, lib().sun_mx4_quantize, (_want("w", w, dev, w.dtype, w.shape), _dtype(w, "w"), rows, cols, codes.data_ptr(), scales.data_ptr()))
     return codes, scales
 
 
@@ -695,12 +697,9 @@ def _mx4(codes: torch.Tensor, scales: torch.Tensor, device: int):
 def sun_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.bfloat16, stream=None) -> torch.Tensor:
     """The values [rows, cols], float32 or bfloat16, which belong to the stream that fills them."""
     dev = _gpu(codes)
-    if stream is not None:
-        with _current(dev, stream):
-            return sun_mx4_dequantize(codes, scales, dtype)
     pc, ps, n, k = _mx4(codes, scales, dev)
-    out = codes.new_empty((n, k), dtype=dtype)
-    _call(dev, None, lib().sun_mx4_dequantize, (pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr()))
+    out = codes.new_empty((n, k), dtype=dtype) if stream is None else _aside(dev, stream, (n, k), dtype)
+    _call(dev, stream, lib().sun_mx4_dequantize, (pc, ps, n, k, _dtype(out, "dtype"), out.data_ptr()))
     return out
 
 

@@ -242,3 +242,23 @@ def test_activations_that_are_no_matrix_are_refused():
         with pytest.raises(sun.SunError) as e:
             sun.sun_mx4_linear(codes, scales, bad, out, ws)
         assert e.value.status == 2
+
+
+def test_outputs_dropped_while_the_current_stream_reads_them():
+    """What a call on another stream has returned may be dropped once its reader is queued: its memory is not handed out before that is done."""
+    xs = [torch.randn(300, 416, generator=torch.Generator(device=DEV).manual_seed(i), device=DEV) for i in range(2)]
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    side.wait_stream(here)
+    codes, scales = sun.sun_mx4_quantize(xs[0], stream=side)
+    here.wait_stream(side)
+    torch.cuda._sleep(50_000_000)   # the reader waits in the queue
+    copies = codes.clone(), scales.clone()
+    first = {codes.data_ptr(), scales.data_ptr()}
+    del codes, scales
+    again = sun.sun_mx4_quantize(xs[1], stream=side)
+    waiting = not here.query()
+    here.wait_stream(side)
+    torch.cuda.synchronize()
+    assert waiting and not first & {t.data_ptr() for t in again}
+    for x, got in zip(xs, (copies, again)):
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(got, R.mx4_quantize(host(x))))
