@@ -571,6 +571,34 @@ int sun_kv8_attention(const sun_kv8_pool* pool, int layer, int batch, int dtype,
                       int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace, size_t workspace_bytes,
                       void* stream, unsigned flags);
 
+/* Bytes of device workspace sun_kv8_chunk_attention needs for up to `rows` rows of up to `batch` requests with max_pages table columns;
+ * 0 for sizes that it refuses. */
+size_t sun_kv8_chunk_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int rows, int max_pages);
+
+/*
+ * Attention of a chunk of new tokens of each request over one layer of an 8-bit pool, which holds them already (sun_kv8_append): drafted tokens, a
+ * block of a prompt, whole prompts, and requests with one new token or none among them.  Enqueued on `stream`; reads the pool only.
+ *   dtype      of q and out: SUN_F32 or SUN_BF16
+ *   q          dev [rows, Hq*d], rotated (sun_kv8_append's q_out), the requests' rows side by side
+ *   row_starts dev int32 [batch + 1], not falling: rows row_starts[i] .. row_starts[i+1] - 1 are request i's, its last positions in their
+ *              order: row j of c has position n_tokens[i] - c + j.  Entries are cut to [0, rows]
+ *   n_tokens   dev int32 [batch]: cached positions, the new ones among them, cut to [0, max_pages*16]
+ *   window     a row at position p attends to positions 0 .. p, with window > 0 to the last `window` of them alone: table entries of pages
+ *              in front of what a request's first row sees are not read as pages (they may be -1)
+ *   out        dev [rows, Hq*d], not q; a row that sees no token (a position below 0, every page lost) gets zeros, a head whose query is not finite
+ *              not-a-numbers where it sees one.  Rows of no request are left as they are
+ * Tokens of a page outside the pool are left out; what a row does not see cannot change its output, not-a-numbers included.  A request's result depends on
+ * `batch`, `rows`, max_pages and its own rows, not on the other requests.
+ * Cached numbers enter exactly (a key's product with its power of two as a bf16 number); weights of the softmax carry 8 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
+ * Under SUN_VALIDATE row starts, counts and tables are copied to the host (synchronises) and checked.
+ * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, batch outside [1, 1024], rows < 1, max_pages outside [1, 2^26], window < 0, dtype, q or out not
+ * 16-byte aligned, q the same as out, more rows than one launch takes: 2^24 are taken for up to 32 query heads), SUN_ERR_WORKSPACE (too small or not 256-byte aligned);
+ * under SUN_VALIDATE also SUN_ERR_SEQ_LEN (row starts that fall or lie outside [0, rows], more rows than positions, counts) and SUN_ERR_PAGE_RANGE.
+ */
+int sun_kv8_chunk_attention(const sun_kv8_pool* pool, int layer, int batch, int rows, int dtype, const void* q, const int32_t* row_starts,
+                            const int32_t* page_tables, int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace,
+                            size_t workspace_bytes, void* stream, unsigned flags);
+
 /* ------------------------------------------------------------------ microscaled 4-bit floats */
 
 /*

@@ -38,6 +38,7 @@ EXPORTS = [
     "sun_paged_attention_static_limit", "sun_linear",
     "sun_kv8_pool_bytes", "sun_kv8_pool_create", "sun_kv8_pool_layout", "sun_kv8_pool_destroy", "sun_kv8_append",
     "sun_kv8_attention", "sun_kv8_attention_workspace_bytes", "sun_kv8_attention_window_workspace_bytes",
+    "sun_kv8_chunk_attention", "sun_kv8_chunk_attention_workspace_bytes",
     "sun_mx4_quantize", "sun_mx4_dequantize", "sun_mx4_linear", "sun_mx4_linear_workspace_bytes",
     "sun_hbm_read_probe", "sun_profile_read", "sun_profile_reset", "sun_last_error", "sun_version",
 ]
@@ -115,7 +116,7 @@ def lib() -> C.CDLL:
         for f in ("sun_kv_pool_bytes", "sun_weights_pack_bytes", "sun_qweights_pack_bytes", "sun_workspace_bytes",
                   "sun_prefill_workspace_bytes", "sun_serve_workspace_bytes", "sun_paged_attention_static_bytes",
                   "sun_paged_attention_static_limit", "sun_kv8_pool_bytes", "sun_kv8_attention_workspace_bytes",
-                  "sun_kv8_attention_window_workspace_bytes", "sun_mx4_linear_workspace_bytes"):
+                  "sun_kv8_attention_window_workspace_bytes", "sun_kv8_chunk_attention_workspace_bytes", "sun_mx4_linear_workspace_bytes"):
             getattr(L, f).restype = C.c_size_t
         L.sun_kv_pool_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int64, C.c_int]
         L.sun_kv_pool_create.argtypes = [C.POINTER(ModelCfg), C.c_void_p, C.c_size_t, C.c_int, C.c_int,
@@ -170,6 +171,9 @@ def lib() -> C.CDLL:
         L.sun_kv8_attention_window_workspace_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int, C.c_int, C.c_int]
         L.sun_kv8_attention.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
                                         C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint]
+        L.sun_kv8_chunk_attention_workspace_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int, C.c_int, C.c_int]
+        L.sun_kv8_chunk_attention.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
+                                              C.c_int, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint]
         L.sun_mx4_quantize.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]
         L.sun_mx4_dequantize.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
         L.sun_mx4_linear_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
@@ -670,6 +674,26 @@ def sun_kv8_attention(pool: Kv8Pool, layer: int, q, page_tables, n_tokens, out, 
     _call(dev, stream, lib().sun_kv8_attention, (
         pool.handle, layer, batch, _dtype(q, "q"), _want("q", q, dev, t, shape), _want("page_tables", page_tables, dev, i32, (batch, max_pages)),
         max_pages, _want("n_tokens", n_tokens, dev, i32, (batch,)), window, _want("out", out, dev, t, shape), *_workspace(workspace, dev)), (flags,))
+
+
+def sun_kv8_chunk_attention_workspace_bytes(cfg: ModelCfg, batch: int, rows: int, max_pages: int) -> int:
+    return int(lib().sun_kv8_chunk_attention_workspace_bytes(C.byref(cfg), batch, rows, max_pages)) if _fits(batch, rows, max_pages) else 0
+
+
+def sun_kv8_chunk_attention(pool: Kv8Pool, layer: int, q, row_starts, page_tables, n_tokens, out, workspace, window: int = 0, stream=None,
+                            flags: int = 0):
+    """q, out [rows, Hq*d], the requests' new rows side by side; row_starts int32 [batch + 1]; page_tables int32 [batch, max_pages];
+    n_tokens int32 [batch], the new tokens counted."""
+    dev, t, i32 = _gpu(pool.mem), q.dtype, torch.int32
+    if q.dim() != 2:
+        _refuse("q must be [rows, Hq*d]")
+    rows, (batch, max_pages) = q.shape[0], _table(page_tables)
+    shape = (rows, pool.q_dim)
+    _int32(layer=layer, rows=rows, max_pages=max_pages, window=window)
+    _call(dev, stream, lib().sun_kv8_chunk_attention, (
+        pool.handle, layer, batch, rows, _dtype(q, "q"), _want("q", q, dev, t, shape), _want("row_starts", row_starts, dev, i32, (batch + 1,)),
+        _want("page_tables", page_tables, dev, i32, (batch, max_pages)), max_pages, _want("n_tokens", n_tokens, dev, i32, (batch,)), window,
+        _want("out", out, dev, t, shape), *_workspace(workspace, dev)), (flags,))
 
 
 def sun_mx4_quantize(w: torch.Tensor, stream=None):

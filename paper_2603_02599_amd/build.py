@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsun.so")
-SOURCES = ["api.hip", "proj.hip", "attention.hip", "layers.hip", "misc.hip", "kv8.hip", "mx4.hip"]
+SOURCES = ["api.hip", "proj.hip", "attention.hip", "layers.hip", "misc.hip", "kv8.hip", "kv8_chunk.hip", "mx4.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 ALU forms are kept out of the generated code on purpose
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

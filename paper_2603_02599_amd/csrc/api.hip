@@ -1609,6 +1609,62 @@ int sun_kv8_attention(const sun_kv8_pool* pool_, int layer, int batch, int dtype
     return SUN_OK;
 }
 
+static bool kv8_chunk_fits(const sun_model_cfg& c, int batch, int rows) { return kv8_chunk_groups(c, batch, rows) <= kMaxGroups; }
+
+size_t sun_kv8_chunk_attention_workspace_bytes(const sun_model_cfg* cfg, int batch, int rows, int max_pages) {
+    if (!cfg || batch < 1 || batch > kKv8MaxBatch || rows < 1 || max_pages < 1 || max_pages > kKv8MaxPages || check_cfg(cfg) != SUN_OK) return 0;
+    if (!kv8_chunk_fits(*cfg, batch, rows)) return 0;
+    return align_up(std::max<size_t>(kv8_chunk_workspace_up_to(*cfg, batch, rows, max_pages), 1));
+}
+
+static int validate_kv8_chunks(const Kv8Pool& pool, int batch, int rows, const int32_t* row_starts, const int32_t* page_tables, int max_pages,
+                               const int32_t* n_tokens, int window, hipStream_t st) {
+    std::vector<int32_t> s((size_t)batch + 1), n((size_t)batch), tab((size_t)batch * max_pages);
+    SUN_HIP_CHECK(hipMemcpyAsync(s.data(), row_starts, s.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipMemcpyAsync(n.data(), n_tokens, n.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipMemcpyAsync(tab.data(), page_tables, tab.size() * 4, hipMemcpyDeviceToHost, st));
+    SUN_HIP_CHECK(hipStreamSynchronize(st));
+    for (int i = 0; i < batch; ++i) {
+        if (s[i] < 0 || s[i + 1] < s[i] || s[i + 1] > rows)
+            return fail(SUN_ERR_SEQ_LEN, "request %d: rows %d to %d of %d", i, s[i], s[i + 1], rows);
+        const int count = s[i + 1] - s[i];
+        if (n[i] < count || n[i] > (long long)max_pages * kPageTokens)
+            return fail(SUN_ERR_SEQ_LEN, "request %d: %d tokens, %d of them new, the table has %d pages", i, n[i], count, max_pages);
+        if (!count) continue;
+        const long long first = window > 0 ? std::max(0ll, (long long)n[i] - count - window + 1) : 0;
+        for (long long p = first / kPageTokens; p * kPageTokens < n[i]; ++p) {
+            const int32_t page = tab[(size_t)i * max_pages + p];
+            if (page < 0 || page >= pool.lay.n_pages)
+                return fail(SUN_ERR_PAGE_RANGE, "request %d: page-table entry %lld = %d outside [0, %lld)", i, p, page, (long long)pool.lay.n_pages);
+        }
+    }
+    return SUN_OK;
+}
+
+int sun_kv8_chunk_attention(const sun_kv8_pool* pool_, int layer, int batch, int rows, int dtype, const void* q, const int32_t* row_starts,
+                            const int32_t* page_tables, int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace,
+                            size_t workspace_bytes, void* stream, unsigned flags) {
+    if (!pool_ || !q || !row_starts || !page_tables || !n_tokens || !out || !workspace) return fail(SUN_ERR_NULL, "NULL argument");
+    const Kv8Pool& pool = *(const Kv8Pool*)pool_;
+    const sun_model_cfg& c = pool.cfg;
+    if (!is_dtype(dtype)) return fail(SUN_ERR_SHAPE, "dtype must be SUN_F32 or SUN_BF16");
+    if (layer < 0 || layer >= c.n_layers) return fail(SUN_ERR_SHAPE, "layer out of range");
+    if (batch < 1 || batch > kKv8MaxBatch || rows < 1 || max_pages < 1 || max_pages > kKv8MaxPages || window < 0)
+        return fail(SUN_ERR_SHAPE, "batch must be in [1, %d], rows >= 1, max_pages in [1, %d], window >= 0", kKv8MaxBatch, kKv8MaxPages);
+    if (((uintptr_t)q | (uintptr_t)out) % 16) return fail(SUN_ERR_SHAPE, "q and out must be 16-byte aligned");
+    if (q == out) return fail(SUN_ERR_SHAPE, "out must not be q");
+    if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    if (!kv8_chunk_fits(c, batch, rows)) return fail(SUN_ERR_SHAPE, "%d rows are more than one launch takes", rows);
+    const size_t need = kv8_chunk_workspace(c, batch, rows, max_pages);
+    if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
+    hipStream_t st = (hipStream_t)stream;
+    if (flags & SUN_VALIDATE)
+        if (int rc = guarded([&] { return validate_kv8_chunks(pool, batch, rows, row_starts, page_tables, max_pages, n_tokens, window, st); })) return rc;
+    SUN_HIP_CHECK(launch_kv8_chunk_attention(pool, layer, batch, rows, q, dtype == SUN_F32, row_starts, page_tables, max_pages, n_tokens, window, out,
+                                             (float*)workspace, st));
+    return SUN_OK;
+}
+
 // ---------------------------------------------------------------- microscaled 4-bit floats
 static int check_mx4(const void* codes, const void* scales, int rows, int cols, const void* dense, int dtype) {
     if (!codes || !scales || !dense) return fail(SUN_ERR_NULL, "NULL argument");

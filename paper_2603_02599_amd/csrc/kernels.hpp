@@ -115,6 +115,13 @@ size_t kv8_partial_floats(const sun_model_cfg& c, int batch, int chunks);
 hipError_t launch_kv8_attention(const Kv8Pool& pool, int layer, int batch, const void* q, bool f32, const int32_t* page_tables, int max_pages,
                                 const int32_t* n_tokens, int window, void* out, float* partial, hipStream_t st);
 
+// ---------------- a chunk of new tokens over the 8-bit cache (kv8_chunk.hip) ----------------
+int64_t kv8_chunk_groups(const sun_model_cfg& c, int batch, int rows);   // (tile, KV head) pairs at most
+size_t kv8_chunk_workspace(const sun_model_cfg& c, int batch, int rows, int max_pages);
+size_t kv8_chunk_workspace_up_to(const sun_model_cfg& c, int batch, int rows, int max_pages);
+hipError_t launch_kv8_chunk_attention(const Kv8Pool& pool, int layer, int batch, int rows, const void* q, bool f32, const int32_t* row_starts, const int32_t* page_tables,
+                                      int max_pages, const int32_t* n_tokens, int window, void* out, float* partial, hipStream_t st);
+
 // ---------------- microscaled 4-bit floats (mx4.hip) ----------------
 hipError_t launch_mx4_quantize(const void* w, bool f32, int64_t rows, int64_t cols, void* codes, void* scales, hipStream_t st);
 hipError_t launch_mx4_dequantize(const void* codes, const void* scales, bool f32, int64_t rows, int64_t cols, void* out, hipStream_t st);

@@ -8,6 +8,7 @@
 #include <math.h>
 
 #include "kernels.hpp"
+#include "lowbit.hpp"
 #include "rows.hpp"
 
 namespace sun {
@@ -389,25 +390,6 @@ __device__ __forceinline__ Kv8Span kv8_span(const Kv8AttnArgs& a, int b) {
     s.chunks = (span + s.chunk - 1) / s.chunk;
     return s;
 }
-
-__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w0, uint32_t w1) {
-    struct { bf16x2_t v[4]; } r;
-    r.v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, false);
-    r.v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.f, true);
-    r.v[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, false);
-    r.v[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.f, true);
-    return __builtin_bit_cast(bf16x8, r);
-}
-__device__ __forceinline__ float power(uint32_t word, int byte) { return __uint_as_float(((word >> (8 * byte)) & 255u) << 23); }
-// x with its lower 16 bits off; what is left of a finite x is exact
-__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-__device__ __forceinline__ float below(float x) {
-    const float r = x - upper(x);
-    return fabsf(x) < INFINITY ? r : 0.f;
-}
-
-// What is stored of a weighted sum v, the weights' sum and the largest score: zeros where there is no token
-__device__ __forceinline__ float kv8_quotient(float v, float sum, float top) { return sum == 0.f && top == -INFINITY ? 0.f : v / sum; }
 
 template <int D>
 struct Kv8Parts {   // of the waves

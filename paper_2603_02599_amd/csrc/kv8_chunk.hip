@@ -1,0 +1,594 @@
+// Attention of a chunk of new tokens of each request over the 8-bit paged cache.
+//
+// A request's query rows times the G = Hq / Hkv query heads of a KV head are the "places" of a product: place v is row v / G, head v % G.  With S^T = K Q^T and
+// O^T = V^T P^T on the 32x32x16 matrix instruction a lane has one place as its column throughout:
+//   scores  S^T = K Q^T: lane (c, h) gets scores of place c and the tokens of rows 8 a + 4 h + e; the row's token is chosen as 16 h + 4 a + e, so a lane's sixteen
+//           scores are those of one page's tokens in their order, and
+//   output  O^T = V^T P^T: the same lane is P's operand for those tokens, V [dim][token] gives lane (dim, h) the page's sixteen in one read.
+// No value moves between lanes but for the maximum of the two halves h.  Codes become bf16 exactly, a key's power is applied while its codes are converted (a lane has one
+// token's), a value's power to its weight.  bf16 queries enter as they are, 32-bit ones as three planes of 8 bits, exact; a weight of the softmax is bf16(p) in bf16 calls, three planes
+// (24 bits) in 32-bit ones.  Maximum, sum and output are in 32 bits, the sum over the weights as they are multiplied.
+// The reference that scores are taken against is raised to kHead above the maximum when a score passes it, so that it is raised seldom and a weight is never above 1.
+#include <float.h>
+#include <math.h>
+
+#include "kernels.hpp"
+#include "lowbit.hpp"
+
+namespace sun {
+
+constexpr int kTile = 128;           // places of a workgroup: 32 to a wave
+constexpr int kFew = 32;             // requests of so many places at most: the four waves share them and take tokens in turn
+constexpr int kWaves = 4;
+constexpr float kHead = 6.f;         // powers of two
+constexpr int kMinSplit = 256;       // tokens of a part at least
+constexpr int kMaxSplits = 64;
+constexpr int kGroupsWanted = 1024;  // workgroups that parts are made for
+
+struct ChunkArgs {
+    const uint8_t *codes, *scales;
+    int64_t k_page, k_head, v_off, v_page, v_head, s_page, s_head, vs_off;
+    const void* q;
+    const int32_t *row_starts, *page_tables, *n_tokens;
+    void* out;
+    float* partial;      // [slot][slot_rows][D], behind them (reference in powers of two, sum) pairs [slot][slot_rows]
+    int64_t slots;
+    int batch, rows, max_pages, n_pages, Hq, Hkv, window, splits, slot_rows;
+    float c;             // log2(e) / sqrt(D)
+};
+
+static __device__ uint32_t g_there[4] = {1, 1, 1, 1};
+
+// ---------------------------------------------------------------- what there is to do
+
+struct ChunkRequest { int start, count, n, tiles, splits; };
+__device__ __forceinline__ ChunkRequest chunk_request(const ChunkArgs& a, int b) {
+    ChunkRequest r{0, 0, 0, 0, 1};
+    if (b >= a.batch) return r;
+    r.start = min(max(a.row_starts[b], 0), a.rows);
+    r.count = max(min(a.row_starts[b + 1], a.rows) - r.start, 0);
+    r.n = (int)min((long long)max(a.n_tokens[b], 0), (long long)a.max_pages * kPageTokens);
+    const int places = r.count * (a.Hq / a.Hkv);
+    r.tiles = places <= kFew ? places > 0 : (places + kTile - 1) / kTile;
+    const long long first = a.window > 0 ? max((long long)r.n - r.count - a.window + 1, 0ll) : 0;
+    r.splits = max(1, min(a.splits, (int)((r.n - first + kMinSplit - 1) / kMinSplit)));
+    return r;
+}
+
+struct ChunkPlace {
+    ChunkRequest r;
+    int b, index;           // request (-1: behind the last), and which of its items or tiles
+    long long items;        // of the requests in front
+};
+// Item `index` of all requests' (a tile's part; TILES: a tile).  The whole wave calls it.
+template <bool TILES>
+__device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, int index) {
+    const int lane = threadIdx.x & 63;
+    long long items = 0;
+    int tiles = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        const ChunkRequest r = chunk_request(a, b0 + lane);
+        int t = r.tiles, s = r.tiles * r.splits;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int x = __shfl_up(t, o), y = __shfl_up(s, o);
+            if (lane >= o) t += x, s += y;
+        }
+        const long long mine = TILES ? (long long)tiles + t : items + s;
+        const uint64_t past = __ballot(mine > index);
+        if (past) {
+            const int l = __ffsll((unsigned long long)past) - 1;
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            ChunkPlace p;
+            p.r = ChunkRequest{of(r.start), of(r.count), of(r.n), of(r.tiles), of(r.splits)};
+            p.b = b0 + l;
+            const int before_t = of(t) - p.r.tiles, before_s = of(s) - p.r.tiles * p.r.splits;
+            p.items = items + before_s;
+            p.index = (int)(index - (TILES ? (long long)tiles + before_t : p.items));
+            return p;
+        }
+        tiles += __builtin_amdgcn_readlane(t, 63);
+        items += __builtin_amdgcn_readlane(s, 63);
+    }
+    ChunkPlace none{};
+    none.b = -1;
+    return none;
+}
+
+// ---------------------------------------------------------------- attention of one part
+
+// LDS: blocks of 32 tokens (two pages) of a KV head.  Keys [token][16-byte piece ^ key], values [page][dim][16 tokens], 256 bytes a page of powers
+// of keys and values and a word that says whether the page is there.
+template <int D>
+struct Block {
+    static constexpr int V = 32 * D, S = 64 * D, BYTES = 64 * D + 512, OPS = 2 * (D / 64) + 1;   // requests of a page
+    __device__ static int key(int token) { return D == 128 ? (token & 3) | (token >> 2 & 4) : (token >> 1 & 1) | (token >> 3 & 2); }
+};
+constexpr int kWideStages = 4, kFewStages = 2;
+template <int D>
+struct ChunkLds {
+    static constexpr int RING = kWaves * kFewStages * Block<D>::BYTES, WIDE = kWideStages * 2 * Block<D>::BYTES, SUMS = kWaves * 32 * (D + 4) * 4 + kWaves * 32 * 8;
+    static constexpr int BYTES = RING > WIDE ? (RING > SUMS ? RING : SUMS) : (WIDE > SUMS ? WIDE : SUMS);
+};
+
+// A page of a part's keys and values into half `half` of a block; one that is not there leaves zeros.
+template <int D>
+__device__ __forceinline__ void request_page(const ChunkArgs& a, int head, int page, int half, uint32_t block) {
+    const int lane = threadIdx.x & 63;
+    const bool there = (unsigned)page < (unsigned)a.n_pages;
+    const int64_t at = there ? page : 0;
+    const uint8_t* k = a.codes + at * a.k_page + head * a.k_head;
+    const uint8_t* v = a.codes + a.v_off + at * a.v_page + head * a.v_head;
+    constexpr int PIECES = D / 16, TOKENS = 64 / PIECES;   // of a token, of a request
+#pragma unroll
+    for (int j = 0; j < kPageTokens / TOKENS; ++j) {
+        const int token = j * TOKENS + lane / PIECES;
+        const uint8_t* p = k + token * D + ((lane % PIECES) ^ Block<D>::key(kPageTokens * half + token)) * 16;
+        lds_fetch16(there ? (const void*)p : &g_zeros, block + (kPageTokens * half + j * TOKENS) * D);
+    }
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+        lds_fetch16(there ? (const void*)(v + j * 1024 + lane * 16) : &g_zeros, block + Block<D>::V + half * 16 * D + j * 1024);
+    const uint8_t* s = a.scales + at * a.s_page + head * a.s_head + (lane & 3) * 4;
+    if (lane >= 4) s += a.vs_off;
+    if (lane >= 8) s = (const uint8_t*)&g_there[0];
+    lds_fetch4(there ? (const void*)s : &g_zeros, block + Block<D>::S + half * 256);
+}
+
+// A wave's 32 places: operands, and what has been summed up
+template <class T, int D>
+struct Places {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int P = F32 ? 3 : 1, KS = D / 16, NB = D / 32;   // planes, steps of 16 dims, blocks of 32 dims
+    bf16x8 q[P][KS];
+    f32x16 o[NB];
+    float m, l;        // the reference in powers of two, the lane's half of the sum
+    int lo, hi;        // positions that the lane's place sees: lo .. hi
+    uint32_t had;      // not 0: one of them was there
+
+    __device__ __forceinline__ void load(const ChunkArgs& a, const ChunkRequest& r, int head, int v) {
+        const int G = a.Hq / a.Hkv, h = (threadIdx.x & 63) >> 5;
+        const bool on = v < r.count * G;
+        const int row = on ? v / G : 0, pos = r.n - r.count + row;
+        hi = on ? pos : -1;
+        lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+        const T* p = (const T*)a.q + ((int64_t)(r.start + row) * a.Hq + head * G + (on ? v % G : 0)) * D + 16 * h;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if constexpr (F32) {
+                float x[8];
+                bf16x8 planes[3];
+                load8(p + 32 * (s / 2) + 8 * (s % 2), x);
+                three_planes(x, planes);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) q[i][s] = planes[i];
+            } else {
+                q[0][s] = *reinterpret_cast<const bf16x8*>(p + 32 * (s / 2) + 8 * (s % 2));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+        m = -INFINITY;
+        l = 0.f;
+        had = 0;
+    }
+
+    // Tokens at .. at + 31, of which those from n on have not been written.  whole: every place of the wave sees all of them
+    __device__ __forceinline__ void step(const ChunkArgs& a, const uint8_t* block, int at, int n, bool whole) {
+        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        {
+            const int token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+            const float scale = __uint_as_float((uint32_t)block[Block<D>::S + (token >> 4) * 256 + (token & 15)] << 23);
+            const uint8_t* k = block + token * D;
+            auto read = [&](int w) { return *reinterpret_cast<const u32x4_s*>(k + ((2 * w + h) ^ Block<D>::key(token)) * 16); };
+            u32x4_s next = read(0);
+#pragma unroll
+            for (int w = 0; w < KS / 2; ++w) {
+                const u32x4_s codes = next;
+                if (w + 1 < KS / 2) next = read(w + 1);
+                __builtin_amdgcn_sched_barrier(0);   // codes are converted where they are used: all at once they take the registers
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bf16x8 x = codes_to_bf16(codes[2 * u], codes[2 * u + 1], scale);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][2 * w + u], s, 0, 0, 0);
+                }
+            }
+        }
+        u32x4_s vs = *reinterpret_cast<const u32x4_s*>(block + Block<D>::S + h * 256 + 16);
+        uint32_t live = 0xffff;          // of the lane's sixteen tokens, which its place sees
+        const int mine = at + 16 * h;
+        if (!whole) {
+            const bool there = *reinterpret_cast<const uint32_t*>(block + Block<D>::S + h * 256 + 32) != 0;
+            const int from = max(lo - mine, 0), to = min(hi - mine, 15);
+            live = there && from <= to ? (0xffffu >> (15 - to)) & (0xffffu << from) : 0u;
+            had |= live;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(live >> i & 1)) s[i] = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {   // powers that nobody has written are not used
+                const uint32_t b = live >> (4 * j) & 15;
+                vs[j] &= ((b & 1) * 0xffu) | ((b >> 1 & 1) * 0xff00u) | ((b >> 2 & 1) * 0xff0000u) | ((b >> 3) * 0xff000000u);
+            }
+        } else {
+            had = 1;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        {
+            float x = top, y = top;
+            swap_rows<32>(x, y);
+            top = fmaxf(x, y) * a.c;
+        }
+        if (__any(top > m)) {
+            const float grown = top > m ? top + kHead : m;
+            const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
+            m = grown;
+            l *= f;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[j][i] *= f;
+        }
+        const uint8_t* v = block + Block<D>::V + h * 16 * D + c * 16;
+        u32x4_s codes[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) codes[j] = *reinterpret_cast<const u32x4_s*>(v + j * 512);
+        const float ref = m == -INFINITY ? 0.f : m;
+        bf16x8 w[P][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            u32x4_s words[P];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int i = 8 * u + 2 * j + e;
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -ref));
+                    l += p;
+                    x[e] = p * power(vs[i >> 2], i & 3);
+                }
+                words[0][j] = pack_bf16(x[0], x[1]);
+                if constexpr (F32) {
+                    x[0] -= bf16_lo(words[0][j]), x[1] -= bf16_hi(words[0][j]);
+                    words[1][j] = pack_bf16(x[0], x[1]);
+                    words[2][j] = pack_bf16(x[0] - bf16_lo(words[1][j]), x[1] - bf16_hi(words[1][j]));
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) w[p][u] = __builtin_bit_cast(bf16x8, words[p]);
+        }
+        if (!whole) {
+            // Values that nobody has written are not used; a not-a-number in one that a place does not see must not reach it, though its weight is 0.
+            bool odd = false;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int written = min(max(n - mine - 4 * e, 0), 4);
+                    codes[j][e] &= written == 4 ? ~0u : (1u << (8 * written)) - 1;
+                    odd |= (((codes[j][e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                }
+            if (__any(odd)) {   // marked where a place sees one, by a product of ones, and left out below
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    f32x16 d;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) d[i] = 0.f;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        u32x4_s one, sees;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t bad = (((codes[j][2 * u + (e >> 1)] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> (16 * (e & 1));
+                            one[e] = (bad & 0x80u ? 0x3f80u : 0u) | (bad & 0x8000u ? 0x3f800000u : 0u);
+                            sees[e] = (live >> (8 * u + 2 * e) & 1 ? 0x3f80u : 0u) | (live >> (8 * u + 2 * e + 1) & 1 ? 0x3f800000u : 0u);
+                        }
+                        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, one), __builtin_bit_cast(bf16x8, sees), d, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (d[i] > 0.f) o[j][i] = NAN;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) codes[j][e] &= ~(((((codes[j][e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8 x = codes_to_bf16(codes[j][2 * u], codes[j][2 * u + 1]);
+#pragma unroll
+                for (int p = 0; p < P; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, w[p][u], o[j], 0, 0, 0);
+            }
+        }
+    }
+
+    // The two halves' sums, and a reference that says whether there was a token
+    __device__ __forceinline__ void close() {
+        float x = l, y = l;
+        swap_rows<32>(x, y);
+        l = x + y;
+        uint32_t u = had, w = had;
+        swap_rows<32>(u, w);
+        had = u | w;
+        if (m == -INFINITY && had) m = -FLT_MAX;
+    }
+};
+
+// The range of a tile's part
+struct ChunkRange { int begin, end; };
+__device__ __forceinline__ ChunkRange chunk_range(const ChunkArgs& a, const ChunkRequest& r, int places0, int places, int split, int step) {
+    const int G = a.Hq / a.Hkv, last = min(places0 + places, r.count * G) - 1;
+    const int hi = r.n - r.count + last / G + 1, low = a.window > 0 ? max(r.n - r.count + places0 / G - a.window + 1, 0) : 0;
+    const int first = low / kPageTokens * kPageTokens, span = max(hi - first, 0);
+    const int per = ((span + r.splits - 1) / r.splits + step - 1) / step * step;
+    const long long begin = first + (long long)split * per;
+    return ChunkRange{(int)min(begin, (long long)max(hi, 0)), (int)min(begin + per, (long long)max(hi, 0))};
+}
+
+// Four waves of 32 places each over the same tokens, 64 a step: wave w requests the step's page w.
+template <class T, int D>
+__device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace& p, int head, int tile, int split, int64_t slot, uint8_t* lds) {
+    constexpr int ST = kWideStages, STAGE = 2 * Block<D>::BYTES, OPS = Block<D>::OPS;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+    const int G = a.Hq / a.Hkv, v0 = tile * kTile + 32 * wave, live = p.r.count * G;
+    const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
+    const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    // positions that all of the wave's places see, and that any does
+    const int base = p.r.n - p.r.count, low = base + v0 / G, high = base + (min(v0 + 32, live) - 1) / G;
+    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0, any_from = a.window > 0 ? max(low - a.window + 1, 0) : 0;
+    Places<T, D> w;
+    w.load(a, p.r, head, v0 + c);
+    auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
+    int ahead = range.begin + wave * kPageTokens, fill = 0;
+    int page = page_at(ahead);
+    auto request = [&]() {
+        request_page<D>(a, head, page, wave & 1, lds0 + fill * STAGE + (wave >> 1) * Block<D>::BYTES);
+        ahead += 64;
+        page = page_at(ahead);
+        if (++fill == ST) fill = 0;
+    };
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) request();
+    int at = 0;
+    for (int token = range.begin; token < range.end; token += 64) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(OPS * (ST - 2)) : "memory");   // the step has landed for every wave, and all are done with the one before
+        request();
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            const int from = token + 32 * half;
+            const uint8_t* block = lds + at * STAGE + half * Block<D>::BYTES;
+            if (v0 >= live || from > high || from + 31 < any_from) continue;
+            const bool there = *reinterpret_cast<const uint32_t*>(block + Block<D>::S + h * 256 + 32) != 0;
+            w.step(a, block, from, p.r.n, from >= all_from && from + 31 <= low && __all(there));
+        }
+        if (++at == ST) at = 0;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    w.close();
+    const int v = v0 + c;
+    if (v < live) {
+        if (p.r.splits == 1) {
+            const int row = p.r.start + v / G;
+            T* out = (T*)a.out + ((int64_t)row * a.Hq + head * G + v % G) * D;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = kv8_quotient(w.o[j][4 * e + i], w.l, w.m);
+                    T* to = out + 32 * j + 8 * e + 4 * h;
+                    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+                    else *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+                }
+        } else {
+            const int64_t place = slot * a.slot_rows + 32 * wave + c;
+            float* out = a.partial + place * D;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<f32x4*>(out + 32 * j + 8 * e + 4 * h) = f32x4{w.o[j][4 * e], w.o[j][4 * e + 1], w.o[j][4 * e + 2], w.o[j][4 * e + 3]};
+            if (h == 0) reinterpret_cast<float2*>(a.partial + a.slots * a.slot_rows * D)[place] = float2{w.m, w.l};
+        }
+    }
+}
+
+// Up to 32 places: each wave has all of them, and every fourth 32 tokens, which it requests for itself.
+template <class T, int D>
+__device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& p, int head, int split, int64_t slot, uint8_t* lds) {
+    constexpr int ST = kFewStages, STAGE = Block<D>::BYTES, OPS = 2 * Block<D>::OPS, LD = D + 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
+    const int G = a.Hq / a.Hkv, live = p.r.count * G;
+    const ChunkRange range = chunk_range(a, p.r, 0, kFew, split, 32 * kWaves);
+    const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * ST * STAGE;
+    const int low = p.r.n - p.r.count, high = p.r.n - 1;
+    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
+    Places<T, D> w;
+    w.load(a, p.r, head, c);
+    auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
+    int ahead = range.begin + 32 * wave, fill = 0;
+    int page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
+    auto request = [&]() {
+        request_page<D>(a, head, page0, 0, lds0 + fill * STAGE);
+        request_page<D>(a, head, page1, 1, lds0 + fill * STAGE);
+        ahead += 32 * kWaves;
+        page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
+        if (++fill == ST) fill = 0;
+    };
+#pragma unroll
+    for (int s = 0; s < ST - 1; ++s) request();
+    int at = 0;
+    for (int from = range.begin + 32 * wave; from < range.end; from += 32 * kWaves) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OPS * (ST - 2)) : "memory");
+        request();
+        const uint8_t* block = lds + (wave * ST + at) * STAGE;
+        const bool there = *reinterpret_cast<const uint32_t*>(block + Block<D>::S + h * 256 + 32) != 0;
+        w.step(a, block, from, p.r.n, from >= all_from && from + 31 <= low && __all(there));
+        if (++at == ST) at = 0;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    w.close();
+    __syncthreads();   // every wave is done with its ring
+    float* sums = reinterpret_cast<float*>(lds);
+    float2* ml = reinterpret_cast<float2*>(lds + kWaves * 32 * LD * 4);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<f32x4*>(sums + (wave * 32 + c) * LD + 32 * j + 8 * e + 4 * h) = f32x4{w.o[j][4 * e], w.o[j][4 * e + 1], w.o[j][4 * e + 2], w.o[j][4 * e + 3]};
+    if (h == 0) ml[wave * 32 + c] = float2{w.m, w.l};
+    __syncthreads();
+    for (int u = threadIdx.x; u < live * (D / 4); u += 64 * kWaves) {
+        const int v = u / (D / 4), d = u % (D / 4) * 4;
+        float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i * 32 + v].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            const float2 y = ml[i * 32 + v];
+            const float f = __builtin_amdgcn_exp2f(y.x - ref);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(sums + (i * 32 + v) * LD + d);
+            sum += f * y.y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] += f * o[e];
+        }
+        if (p.r.splits == 1) {
+            T* to = (T*)a.out + ((int64_t)(p.r.start + v / G) * a.Hq + head * G + v % G) * D + d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = kv8_quotient(x[e], sum, top);
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+            else *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        } else {
+            const int64_t place = slot * a.slot_rows + v;
+            *reinterpret_cast<f32x4*>(a.partial + place * D + d) = f32x4{x[0], x[1], x[2], x[3]};
+            if (d == 0) reinterpret_cast<float2*>(a.partial + a.slots * a.slot_rows * D)[place] = float2{top, sum};
+        }
+    }
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ChunkLds<D>::BYTES];
+    const int head = blockIdx.x % a.Hkv;
+    for (int item = blockIdx.x / a.Hkv;; item += gridDim.x / a.Hkv) {
+        const ChunkPlace p = chunk_find<false>(a, item);
+        if (p.b < 0) return;
+        const int split = p.index % p.r.splits, tile = p.r.tiles - 1 - p.index / p.r.splits;   // the longest first
+        const int64_t slot = (p.items + (int64_t)tile * p.r.splits + split) * a.Hkv + head;
+        if (p.r.splits == 1 || slot < a.slots) {   // row starts that are none could name more
+            if (p.r.count * (a.Hq / a.Hkv) <= kFew) chunk_few<T, D>(a, p, head, split, slot, lds);
+            else chunk_wide<T, D>(a, p, head, tile, split, slot, lds);
+        }
+        __syncthreads();
+    }
+}
+
+// out = sum over a tile's parts, a wave a place at a time
+template <class T, int D>
+__global__ __launch_bounds__(64 * kWaves) void kv8_chunk_join_kernel(ChunkArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.Hq / a.Hkv;
+    const int head = blockIdx.x % a.Hkv;
+    const ChunkPlace p = chunk_find<true>(a, blockIdx.x / a.Hkv);
+    if (p.b < 0 || p.r.splits == 1) return;
+    const int tile = p.index, places = p.r.count * G <= kFew ? kFew : kTile, live = min(p.r.count * G - tile * places, places);
+    const int64_t slot = (p.items + (int64_t)tile * p.r.splits) * a.Hkv + head;
+    if (slot + (int64_t)(p.r.splits - 1) * a.Hkv >= a.slots) return;
+    const float2* ml = reinterpret_cast<const float2*>(a.partial + a.slots * a.slot_rows * D);
+    constexpr int E = D / 64;
+    for (int v = blockIdx.y * kWaves + wave; v < live; v += kWaves * gridDim.y) {
+        const int64_t at0 = slot * a.slot_rows + v, step = (int64_t)a.Hkv * a.slot_rows;
+        const float2 mine = lane < p.r.splits ? ml[at0 + lane * step] : float2{-INFINITY, 0.f};
+        const float top = wave_max(mine.x), ref = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(mine.x - ref), sum = wave_sum(f * mine.y);
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = 0.f;
+        for (int s = 0; s < p.r.splits; ++s) {
+            const float g = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s));
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] += g * a.partial[(at0 + s * step) * D + 64 * e + lane];
+        }
+        const int place = tile * places + v;
+        T* to = (T*)a.out + ((int64_t)(p.r.start + place / G) * a.Hq + head * G + place % G) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) store_as(to + 64 * e + lane, kv8_quotient(x[e], sum, top));
+    }
+}
+
+// ---------------------------------------------------------------- the call
+
+static int64_t chunk_tiles(const sun_model_cfg& c, int batch, int rows) {   // no fewer than there can be
+    const int G = c.n_q_heads / c.n_kv_heads;
+    return (int64_t)rows * G / kTile + std::min(batch, rows);
+}
+static int chunk_splits(const sun_model_cfg& c, int batch, int rows, int max_pages) {
+    const int64_t groups = chunk_tiles(c, batch, rows) * c.n_kv_heads, longest = ((int64_t)max_pages * kPageTokens + kMinSplit - 1) / kMinSplit;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({kMaxSplits, longest, (kGroupsWanted + groups - 1) / groups}));
+}
+static int chunk_slot_rows(const sun_model_cfg& c, int rows) {
+    return (int)std::min<int64_t>(kTile, ((int64_t)rows * (c.n_q_heads / c.n_kv_heads) + 31) / 32 * 32);
+}
+static size_t chunk_bytes(const sun_model_cfg& c, int64_t slots, int slot_rows) { return (size_t)slots * slot_rows * (c.head_dim + 2) * 4; }
+
+int64_t kv8_chunk_groups(const sun_model_cfg& c, int batch, int rows) { return chunk_tiles(c, batch, rows) * c.n_kv_heads; }
+size_t kv8_chunk_workspace(const sun_model_cfg& c, int batch, int rows, int max_pages) {
+    const int splits = chunk_splits(c, batch, rows, max_pages);
+    return splits == 1 ? 0 : chunk_bytes(c, chunk_tiles(c, batch, rows) * c.n_kv_heads * splits, chunk_slot_rows(c, rows));
+}
+// No less than what any fewer rows of any fewer requests take: g workgroups without parts are given ceil(wanted / g) of them each at most, fewer than wanted + g in all
+size_t kv8_chunk_workspace_up_to(const sun_model_cfg& c, int batch, int rows, int max_pages) {
+    const int64_t groups = kv8_chunk_groups(c, batch, rows), splits = std::min<int64_t>(kMaxSplits, ((int64_t)max_pages * kPageTokens + kMinSplit - 1) / kMinSplit);
+    if (splits == 1) return 0;
+    return chunk_bytes(c, std::min<int64_t>(groups * splits, kGroupsWanted + std::min<int64_t>(groups, kGroupsWanted)), chunk_slot_rows(c, rows));
+}
+
+template <class T, int D>
+static hipError_t chunk_attend(const ChunkArgs& a, int64_t tiles, hipStream_t st) {
+    const int64_t items = tiles * a.splits;
+    const unsigned grid = (unsigned)(std::min<int64_t>(items, std::max<int64_t>(8192 / a.Hkv, 1)) * a.Hkv);
+    hipLaunchKernelGGL((kv8_chunk_kernel<T, D>), dim3(grid), dim3(64 * kWaves), 0, st, a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)(a.slot_rows / 8)), dim3(64 * kWaves), 0, st, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv8_chunk_attention(const Kv8Pool& pool, int layer, int batch, int rows, const void* q, bool f32, const int32_t* row_starts, const int32_t* page_tables,
+                                      int max_pages, const int32_t* n_tokens, int window, void* out, float* partial, hipStream_t st) {
+    const sun_model_cfg& c = pool.cfg;
+    const sun_kv8_layout& L = pool.lay;
+    ChunkArgs a{};
+    a.codes = pool.base + L.k_off + layer * L.k_layer;
+    a.scales = pool.base + L.ks_off + layer * L.s_layer;
+    a.k_page = L.k_page, a.k_head = L.k_head;
+    a.v_off = L.v_off - L.k_off, a.v_page = L.v_page, a.v_head = L.v_head;
+    a.s_page = L.s_page, a.s_head = L.s_head, a.vs_off = L.vs_off - L.ks_off;
+    a.q = q, a.row_starts = row_starts, a.page_tables = page_tables, a.n_tokens = n_tokens, a.out = out, a.partial = partial;
+    a.batch = batch, a.rows = rows, a.max_pages = max_pages, a.n_pages = (int)L.n_pages;
+    a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads, a.window = window;
+    a.splits = chunk_splits(c, batch, rows, max_pages);
+    a.slot_rows = chunk_slot_rows(c, rows);
+    const int64_t tiles = chunk_tiles(c, batch, rows);
+    a.slots = a.splits > 1 ? tiles * a.Hkv * a.splits : 0;
+    a.c = 1.4426950408889634f / sqrtf((float)c.head_dim);
+    if (f32) return c.head_dim == 128 ? chunk_attend<float, 128>(a, tiles, st) : chunk_attend<float, 64>(a, tiles, st);
+    return c.head_dim == 128 ? chunk_attend<uint16_t, 128>(a, tiles, st) : chunk_attend<uint16_t, 64>(a, tiles, st);
+}
+
+}  // namespace sun

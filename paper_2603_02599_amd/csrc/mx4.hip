@@ -4,21 +4,12 @@
 #include <math.h>
 
 #include "kernels.hpp"
+#include "lowbit.hpp"
 
 namespace sun {
 
 constexpr int kMxBlock = 32;
 
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
-    const u32x4_s w = *reinterpret_cast<const u32x4_s*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
-}
 // A lane takes eight columns, four lanes a block: reads and writes are contiguous over the wave.  The matrix is contiguous, so
 // rows do not matter.  A workgroup has R runs of 256 octets under way.  The converter rounds to the nearest even code and stops at 6.
 // Memory bounds it: 28672 x 4096 in bf16 (297 MB in and out) 48 us, 6.2 TB/s.
@@ -151,42 +142,6 @@ struct Mx4Args {
     int splits;
 };
 
-// Eight 32-bit activations as their three planes.  What is not finite has its value in the first plane and zeros in the others.
-__device__ __forceinline__ void mx4_planes(const float (&v)[8], bf16x8 (&planes)[3]) {
-    u32x4_s w[3];
-    float r[8];
-    bool finite = true;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        r[i] = v[i];
-        finite &= fabsf(v[i]) < INFINITY;
-    }
-    auto cut = [](float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
-    auto plane = [&](int p) {   // the upper halves of two values a word
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[p][j] = __builtin_amdgcn_perm(__float_as_uint(r[2 * j + 1]), __float_as_uint(r[2 * j]), 0x07060302u);
-    };
-    if (!finite) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (v[i] != v[i]) r[i] = __uint_as_float(0x7fc00000u);   // a not-a-number that its upper half says
-    }
-    plane(0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = cut(r[i]);
-    if (!finite) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (!(fabsf(v[i]) < INFINITY)) r[i] = 0.f;
-    }
-    plane(1);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = cut(r[i]);
-    plane(2);
-#pragma unroll
-    for (int p = 0; p < 3; ++p) planes[p] = __builtin_bit_cast(bf16x8, w[p]);
-}
-
 // The planes of 32-bit activations for more than sixteen rows, once for all workgroups.  A lane takes eight.  150 x 13824: 6 us.
 __global__ __launch_bounds__(256) void mx4_planes_kernel(const float* x, int64_t ld_x, int rows, int K, uint16_t* planes, int64_t plane) {
     const int64_t octets = (int64_t)rows * (K / 8), stride = (int64_t)gridDim.x * 256;
@@ -195,7 +150,7 @@ __global__ __launch_bounds__(256) void mx4_planes_kernel(const float* x, int64_t
         float v[8];
         load8(x + row * ld_x + k, v);
         bf16x8 w[3];
-        mx4_planes(v, w);
+        three_planes(v, w);
 #pragma unroll
         for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(planes + p * plane + row * K + k) = w[p];
     }
@@ -211,20 +166,6 @@ __device__ __forceinline__ bf16x8 mx4_values(uint32_t w, float scale) {
 }
 // the converter reads the power's exponent field: all ones is not-a-number
 __device__ __forceinline__ float mx4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-__device__ u32x4_s g_mx4_zeros = {0, 0, 0, 0};   // what lanes behind the last column are given
-
-// Requests from memory straight into LDS, the address a lane's own: 16 bytes a lane (lane i's land at lds_byte + 16 i), or a byte, which
-// lands as a word (at lds_byte + 4 i).  Whoever reads the place waits for vmcnt and the barrier by hand.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"   // m0 is a reserved register, see lds_dma16
-__device__ __forceinline__ void lds_fetch16(const void* p, uint32_t lds_byte) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");
-}
-__device__ __forceinline__ void lds_fetch1(const void* p, uint32_t lds_byte) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 
 // Four consecutive columns of one row
 template <class T>
@@ -268,8 +209,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int64_t at = (int64_t)min(n0 + 16 * t + row16, a.N - 1) * blocks + chunk * 4;
-                lds_fetch16(chunk * 4 + piece < blocks ? (const void*)(a.codes + (at + piece) * 16) : &g_mx4_zeros, to + (u * NT + t) * 1024);
-                lds_fetch1(chunk * 4 + (lane & 3) < blocks ? (const void*)(a.scales + at + (lane & 3)) : &g_mx4_zeros, to + U * NT * 1024 + (u * NT + t) * 256);
+                lds_fetch16(chunk * 4 + piece < blocks ? (const void*)(a.codes + (at + piece) * 16) : &g_zeros, to + (u * NT + t) * 1024);
+                lds_fetch1(chunk * 4 + (lane & 3) < blocks ? (const void*)(a.scales + at + (lane & 3)) : &g_zeros, to + U * NT * 1024 + (u * NT + t) * 256);
             }
         }
         u32x4_s x[U][4][P == 3 ? 2 : 1];
@@ -303,7 +244,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void mx4_few_kernel(Mx4Args a) {
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x[u][j][e >> 2][e & 3]);
-                    mx4_planes(v, planes);
+                    three_planes(v, planes);
                 } else {
                     planes[0] = __builtin_bit_cast(bf16x8, x[u][j][0]);
                 }
@@ -386,15 +327,15 @@ __global__ __launch_bounds__(512) void mx4_stream_kernel(Mx4Args a) {
         if (i < XW) {
             const int f = wq * XW + i;
             src = x[i] + (plane * a.plane + (int64_t)chunk * 128);
-            if (!full && chunk * 4 + (f & 3) >= end) src = &g_mx4_zeros;
+            if (!full && chunk * 4 + (f & 3) >= end) src = &g_zeros;
             lds_fetch16(src, to + f * 1024);
         } else if (i < XW + CW) {
             src = code[i - XW] + (int64_t)chunk * 64;
-            if (!full && chunk * 4 + piece >= end) src = &g_mx4_zeros;
+            if (!full && chunk * 4 + piece >= end) src = &g_zeros;
             lds_fetch16(src, to + C0 + (wq * CW + i - XW) * 1024);
         } else {
             src = power[i - XW - CW] + chunk * 4;
-            if (!full && chunk * 4 + (lane & 3) >= end) src = &g_mx4_zeros;
+            if (!full && chunk * 4 + (lane & 3) >= end) src = &g_zeros;
             lds_fetch1(src, to + S0 + (wq * CW + i - XW - CW) * 256);
         }
     };
@@ -549,16 +490,16 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
         const void* src;
         if (i < CW) {
             src = code[i] + (int64_t)chunk * 64;
-            if (!full && chunk * 4 + piece >= end) src = &g_mx4_zeros;
+            if (!full && chunk * 4 + piece >= end) src = &g_zeros;
             lds_fetch16(src, lds0 + C0 + (wave * CW + i) * 1024);
         } else if (i < 2 * CW) {
             src = power[i - CW] + chunk * 4;
-            if (!full && chunk * 4 + (lane & 3) >= end) src = &g_mx4_zeros;
+            if (!full && chunk * 4 + (lane & 3) >= end) src = &g_zeros;
             lds_fetch1(src, lds0 + S0 + (wave * CW + i - CW) * 256);
         } else {
             const int f = wave * XW + i - 2 * CW;
             src = x[i - 2 * CW] + (plane * a.plane + (int64_t)chunk * 128);
-            if (!full && chunk * 4 + (f & 3) >= end) src = &g_mx4_zeros;
+            if (!full && chunk * 4 + (f & 3) >= end) src = &g_zeros;
             lds_fetch16(src, lds0 + fill * (XF * 1024) + f * 1024);
         }
     };
