@@ -57,6 +57,9 @@ enum {
 
 enum { SUN_F32 = 0, SUN_BF16 = 1 };
 
+/* Activations: x; x / (1 + e^-x); x (1 + erf(x / sqrt 2)) / 2; x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+enum { SUN_ACT_NONE = 0, SUN_ACT_SILU = 1, SUN_ACT_GELU = 2, SUN_ACT_GELU_TANH = 3 };
+
 /* step flags */
 enum {
     SUN_VALIDATE = 1u, /* copy token ids, lengths, page tables and model ids to the host
@@ -634,6 +637,32 @@ size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows);
  */
 int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x,
                    void* out, int out_dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * out[b, n] = act(sum_k W[n, k] x[b, k] + bias[n]) + residual[b, n]: sun_mx4_linear with what stands behind a projection in its epilogue, the product in its
+ * arithmetic, the rest in 32 bits, rounded once.  Workspace: sun_mx4_linear_workspace_bytes.
+ *   bias        dev [N], of out's type, or NULL
+ *   activation  SUN_ACT_*
+ *   residual    dev [rows, N], of out's type, row stride ld_residual elements, or NULL; may be out itself at out's stride, and must not overlap
+ *               it in any other way
+ * Errors: those of sun_mx4_linear; SUN_ERR_SHAPE also for another activation, a bias or residual not aligned to its type, ld_residual < N, a
+ * residual that is out at another stride.
+ */
+int sun_mx4_linear_fused(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x, const void* bias,
+                         int activation, const void* residual, int64_t ld_residual, void* out, int out_dtype, int64_t ld_out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace sun_mx4_gated needs for a pair of matrices [N, K] and up to `rows` rows, any types; 0 for sizes that it refuses. */
+size_t sun_mx4_gated_workspace_bytes(int N, int K, int rows);
+
+/*
+ * out[b, n] = act(sum_k Wg[n, k] x[b, k]) * (sum_k Wu[n, k] x[b, k]): the first half of a gated feed-forward block in one kernel, Wg and Wu [N, K] in the
+ * format above, separate or the halves of one array.  Arithmetic, types, strides and refusals as in sun_mx4_linear (N at most 2^27, 2 N columns against its limits); the
+ * activation and the product are in 32 bits, rounded once.
+ */
+int sun_mx4_gated(const void* gate_codes, const void* gate_scales, const void* up_codes, const void* up_scales, int N, int K, int rows,
+                  const void* x, int x_dtype, int64_t ld_x, int activation, void* out, int out_dtype, int64_t ld_out, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ single operations */
 

@@ -15,6 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("SUN_LIB_PATH", os.path.join(_HERE, "libsun.so"))  # override: another build of libsun
 
 SUN_F32, SUN_BF16 = 0, 1
+SUN_ACT_NONE, SUN_ACT_SILU, SUN_ACT_GELU, SUN_ACT_GELU_TANH = 0, 1, 2, 3
 SUN_VALIDATE, SUN_PROFILE, SUN_SERVE_RESET = 1, 2, 4
 
 
@@ -40,6 +41,7 @@ EXPORTS = [
     "sun_kv8_attention", "sun_kv8_attention_workspace_bytes", "sun_kv8_attention_window_workspace_bytes",
     "sun_kv8_chunk_attention", "sun_kv8_chunk_attention_workspace_bytes",
     "sun_mx4_quantize", "sun_mx4_dequantize", "sun_mx4_linear", "sun_mx4_linear_workspace_bytes",
+    "sun_mx4_linear_fused", "sun_mx4_gated", "sun_mx4_gated_workspace_bytes",
     "sun_hbm_read_probe", "sun_profile_read", "sun_profile_reset", "sun_last_error", "sun_version",
 ]
 
@@ -116,7 +118,8 @@ def lib() -> C.CDLL:
         for f in ("sun_kv_pool_bytes", "sun_weights_pack_bytes", "sun_qweights_pack_bytes", "sun_workspace_bytes",
                   "sun_prefill_workspace_bytes", "sun_serve_workspace_bytes", "sun_paged_attention_static_bytes",
                   "sun_paged_attention_static_limit", "sun_kv8_pool_bytes", "sun_kv8_attention_workspace_bytes",
-                  "sun_kv8_attention_window_workspace_bytes", "sun_kv8_chunk_attention_workspace_bytes", "sun_mx4_linear_workspace_bytes"):
+                  "sun_kv8_attention_window_workspace_bytes", "sun_kv8_chunk_attention_workspace_bytes", "sun_mx4_linear_workspace_bytes",
+                  "sun_mx4_gated_workspace_bytes"):
             getattr(L, f).restype = C.c_size_t
         L.sun_kv_pool_bytes.argtypes = [C.POINTER(ModelCfg), C.c_int64, C.c_int]
         L.sun_kv_pool_create.argtypes = [C.POINTER(ModelCfg), C.c_void_p, C.c_size_t, C.c_int, C.c_int,
@@ -179,6 +182,11 @@ def lib() -> C.CDLL:
         L.sun_mx4_linear_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
         L.sun_mx4_linear.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int64,
                                      C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sun_mx4_linear_fused.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int,
+                                           C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.sun_mx4_gated_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
+        L.sun_mx4_gated.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int64, C.c_int,
+                                    C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
         L.sun_hbm_read_probe.argtypes = [C.c_void_p, C.c_size_t, C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
         L.sun_profile_read.argtypes = [C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.sun_profile_reset.restype = None
@@ -741,6 +749,42 @@ def sun_mx4_linear(codes, scales, x, out, workspace, stream=None):
     _int32(rows=rows)
     _call(dev, stream, lib().sun_mx4_linear, (
         pc, ps, n, k, rows, _want("x", x, dev, tx, (rows, k), True), _dtype(x, "x"), _row_stride(x),
+        _want("out", out, dev, to, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev)))
+
+
+def sun_mx4_linear_fused(codes, scales, x, out, workspace, bias=None, activation: int = SUN_ACT_NONE, residual=None, stream=None):
+    """out [rows, N] = act(x [rows, K] W^T + bias [N]) + residual [rows, N]; bias and residual of out's type, or None; rows at any stride, a residual may be
+    out itself."""
+    dev = _gpu(codes)
+    pc, ps, n, k = _mx4(codes, scales, dev)
+    if x.dim() != 2:
+        _refuse("x must be [rows, K]")
+    rows, tx, to = x.shape[0], x.dtype, out.dtype
+    _int32(rows=rows, activation=activation)
+    _call(dev, stream, lib().sun_mx4_linear_fused, (
+        pc, ps, n, k, rows, _want("x", x, dev, tx, (rows, k), True), _dtype(x, "x"), _row_stride(x),
+        None if bias is None else _want("bias", bias, dev, to, (n,)), activation,
+        None if residual is None else _want("residual", residual, dev, to, (rows, n), True), 0 if residual is None else _row_stride(residual),
+        _want("out", out, dev, to, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev)))
+
+
+def sun_mx4_gated_workspace_bytes(N: int, K: int, rows: int) -> int:
+    return int(lib().sun_mx4_gated_workspace_bytes(N, K, rows)) if _fits(N, K, rows) else 0
+
+
+def sun_mx4_gated(gate_codes, gate_scales, up_codes, up_scales, x, out, workspace, activation: int = SUN_ACT_SILU, stream=None):
+    """out [rows, N] = act(x [rows, K] Wg^T) * (x Wu^T); x and out float32 or bfloat16 each, rows at any stride."""
+    dev = _gpu(gate_codes)
+    pg, sg, n, k = _mx4(gate_codes, gate_scales, dev)
+    if up_codes.shape != gate_codes.shape:
+        _refuse(f"up_codes must be {tuple(gate_codes.shape)} as gate_codes, is {tuple(up_codes.shape)}")
+    pu, su, _, _ = _mx4(up_codes, up_scales, dev)
+    if x.dim() != 2:
+        _refuse("x must be [rows, K]")
+    rows, tx, to = x.shape[0], x.dtype, out.dtype
+    _int32(rows=rows, activation=activation)
+    _call(dev, stream, lib().sun_mx4_gated, (
+        pg, sg, pu, su, n, k, rows, _want("x", x, dev, tx, (rows, k), True), _dtype(x, "x"), _row_stride(x), activation,
         _want("out", out, dev, to, (rows, n), True), _dtype(out, "out"), _row_stride(out), *_workspace(workspace, dev)))
 
 

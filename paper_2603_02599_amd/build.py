@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsun.so")
-SOURCES = ["api.hip", "proj.hip", "attention.hip", "layers.hip", "misc.hip", "kv8.hip", "kv8_chunk.hip", "mx4.hip"]
+SOURCES = ["api.hip", "proj.hip", "attention.hip", "layers.hip", "misc.hip", "kv8.hip", "kv8_chunk.hip", "mx4.hip", "mx4_fused.hip",
+           "mx4_gated.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 ALU forms are kept out of the generated code on purpose
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -40,7 +41,7 @@ def build_lib(force: bool = False, verbose: bool = False) -> str:
             print(out)
         return obj
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=6) as ex:
         objs = list(ex.map(compile_one, SOURCES))
     r = subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs],
                        stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -1696,20 +1696,54 @@ size_t sun_mx4_linear_workspace_bytes(int N, int K, int rows) {
     return align_up(std::max<size_t>(mx4_linear_workspace_up_to(N, K, rows), 1));
 }
 
+static bool is_activation(int act) { return act >= SUN_ACT_NONE && act <= SUN_ACT_GELU_TANH; }
+
+// The checks that the products share; columns: of all matrices together
+static int run_mx4_linear(const Mx4Linear& m, int64_t columns, int x_dtype, int out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!m.out || !workspace) return fail(SUN_ERR_NULL, "NULL argument");
+    if (!is_dtype(out_dtype) || m.rows < 1) return fail(SUN_ERR_SHAPE, "out_dtype must be SUN_F32 or SUN_BF16, rows >= 1");
+    if (m.ld_x < m.K || m.ld_x % (16 / dtype_bytes(x_dtype)) || m.ld_out < m.N || (uintptr_t)m.out % dtype_bytes(out_dtype))
+        return fail(SUN_ERR_SHAPE, "ld_x must be >= K and a multiple of 16 bytes, ld_out >= N, out aligned to its type");
+    if (!mx4_linear_fits(columns, m.K, m.rows)) return fail(SUN_ERR_SHAPE, "%lld x %d by %d rows is more than one launch takes", (long long)columns, m.K, m.rows);
+    if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    const size_t need = mx4_linear_workspace((int)columns, m.K, m.rows, m.x_f32);
+    if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
+    SUN_HIP_CHECK(launch_mx4_linear(m, workspace, (hipStream_t)stream));
+    return SUN_OK;
+}
+
 int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x,
                    void* out, int out_dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream) {
     if (int rc = check_mx4(codes, scales, N, K, x, x_dtype)) return rc;
-    if (!out || !workspace) return fail(SUN_ERR_NULL, "NULL argument");
-    if (!is_dtype(out_dtype) || rows < 1) return fail(SUN_ERR_SHAPE, "out_dtype must be SUN_F32 or SUN_BF16, rows >= 1");
-    if (ld_x < K || ld_x % (16 / dtype_bytes(x_dtype)) || ld_out < N || (uintptr_t)out % dtype_bytes(out_dtype))
-        return fail(SUN_ERR_SHAPE, "ld_x must be >= K and a multiple of 16 bytes, ld_out >= N, out aligned to its type");
-    if (!mx4_linear_fits(N, K, rows)) return fail(SUN_ERR_SHAPE, "%d x %d by %d rows is more than one launch takes", N, K, rows);
-    if ((uintptr_t)workspace % 256) return fail(SUN_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    const size_t need = mx4_linear_workspace(N, K, rows, x_dtype == SUN_F32);
-    if (need > workspace_bytes) return fail(SUN_ERR_WORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
     const Mx4Linear m{(const uint8_t*)codes, (const uint8_t*)scales, N, K, rows, x, ld_x, x_dtype == SUN_F32, out, ld_out, out_dtype == SUN_F32};
-    SUN_HIP_CHECK(launch_mx4_linear(m, workspace, (hipStream_t)stream));
-    return SUN_OK;
+    return run_mx4_linear(m, N, x_dtype, out_dtype, workspace, workspace_bytes, stream);
+}
+
+int sun_mx4_linear_fused(const void* codes, const void* scales, int N, int K, int rows, const void* x, int x_dtype, int64_t ld_x, const void* bias,
+                         int activation, const void* residual, int64_t ld_residual, void* out, int out_dtype, int64_t ld_out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    if (int rc = check_mx4(codes, scales, N, K, x, x_dtype)) return rc;
+    if (!is_activation(activation)) return fail(SUN_ERR_SHAPE, "activation %d", activation);
+    if (!is_dtype(out_dtype)) return fail(SUN_ERR_SHAPE, "out_dtype must be SUN_F32 or SUN_BF16");
+    if (((uintptr_t)bias | (uintptr_t)residual) % dtype_bytes(out_dtype) || (residual && ld_residual < N))
+        return fail(SUN_ERR_SHAPE, "bias and residual must be aligned to their type, ld_residual >= N");
+    if (residual && residual == out && ld_residual != ld_out) return fail(SUN_ERR_SHAPE, "a residual that is out must have its row stride");
+    const Mx4Linear m{(const uint8_t*)codes, (const uint8_t*)scales, N, K, rows, x, ld_x, x_dtype == SUN_F32, out, ld_out, out_dtype == SUN_F32,
+                      activation, bias, residual, residual ? ld_residual : 0};
+    return run_mx4_linear(m, N, x_dtype, out_dtype, workspace, workspace_bytes, stream);
+}
+
+size_t sun_mx4_gated_workspace_bytes(int N, int K, int rows) { return N > 1 << 30 ? 0 : sun_mx4_linear_workspace_bytes(2 * N, K, rows); }
+
+int sun_mx4_gated(const void* gate_codes, const void* gate_scales, const void* up_codes, const void* up_scales, int N, int K, int rows,
+                  const void* x, int x_dtype, int64_t ld_x, int activation, void* out, int out_dtype, int64_t ld_out, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+    if (int rc = check_mx4(gate_codes, gate_scales, N, K, x, x_dtype)) return rc;
+    if (int rc = check_mx4(up_codes, up_scales, N, K, x, x_dtype)) return rc;
+    if (!is_activation(activation)) return fail(SUN_ERR_SHAPE, "activation %d", activation);
+    const Mx4Linear m{(const uint8_t*)gate_codes, (const uint8_t*)gate_scales, N, K, rows, x, ld_x, x_dtype == SUN_F32, out, ld_out, out_dtype == SUN_F32,
+                      activation, nullptr, nullptr, 0, (const uint8_t*)up_codes, (const uint8_t*)up_scales};
+    return run_mx4_linear(m, 2ll * N, x_dtype, out_dtype, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

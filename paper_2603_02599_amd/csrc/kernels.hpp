@@ -134,10 +134,17 @@ struct Mx4Linear {
     void* out;
     int64_t ld_out;
     bool out_f32;
+    // the epilogue; with an up matrix x goes through both, and out is act(gate) * up (sizes of its workspace: those of 2 N columns)
+    int act = SUN_ACT_NONE;
+    const void *bias = nullptr, *residual = nullptr;
+    int64_t ld_residual = 0;
+    const uint8_t *up_codes = nullptr, *up_scales = nullptr;
 };
 size_t mx4_linear_workspace(int N, int K, int rows, bool x_f32);
 size_t mx4_linear_workspace_up_to(int N, int K, int rows);
 hipError_t launch_mx4_linear(const Mx4Linear& a, void* workspace, hipStream_t st);
+hipError_t launch_mx4_gated(const Mx4Linear& a, void* workspace, hipStream_t st);   // mx4_gated.hip
+hipError_t launch_mx4_fused(const Mx4Linear& a, void* workspace, hipStream_t st);   // mx4_fused.hip
 
 // ---------------- all layers of a small batch in one launch (layers.hip) ----------------
 constexpr int kLayersRows = 16;    // rows of such a step at most; measured in layers.hip
