@@ -37,8 +37,6 @@ struct ChunkArgs {
     float c;             // log2(e) / sqrt(D)
 };
 
-static __device__ uint32_t g_there[4] = {1, 1, 1, 1};
-
 // ---------------------------------------------------------------- what there is to do
 
 struct ChunkRequest { int start, count, n, tiles, splits; };
@@ -97,11 +95,11 @@ __device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, int index) 
 
 // ---------------------------------------------------------------- attention of one part
 
-// LDS: blocks of 32 tokens (two pages) of a KV head.  Keys [token][16-byte piece ^ key], values [page][dim][16 tokens], 256 bytes a page of powers
-// of keys and values and a word that says whether the page is there.
+// LDS: blocks of 32 tokens (two pages) of a KV head.  Keys [token][16-byte piece ^ key], values [page][dim][16 tokens], and 256 bytes a page: 16 powers of keys and 16 of
+// values; when they have landed the wave that requested the page writes behind them a word that says whether it is there, and the powers as floats, values first.
 template <int D>
 struct Block {
-    static constexpr int V = 32 * D, S = 64 * D, BYTES = 64 * D + 512, OPS = 2 * (D / 64) + 1;   // requests of a page
+    static constexpr int V = 32 * D, S = 64 * D, THERE = 32, VALUES = 64, KEYS = 128, BYTES = 64 * D + 512, OPS = 2 * (D / 64) + 1;   // requests of a page
     __device__ static int key(int token) { return D == 128 ? (token & 3) | (token >> 2 & 4) : (token >> 1 & 1) | (token >> 3 & 2); }
 };
 constexpr int kWideStages = 4, kFewStages = 2;
@@ -111,29 +109,52 @@ struct ChunkLds {
     static constexpr int BYTES = RING > WIDE ? (RING > SUMS ? RING : SUMS) : (WIDE > SUMS ? WIDE : SUMS);
 };
 
-// A page of a part's keys and values into half `half` of a block; one that is not there leaves zeros.
+// What lanes are given of a page that is not there: a block of keys, one of values, powers
+static __device__ uint32_t g_no_page[512] = {};
+
+// Requests of pages.  The addresses' lane parts are the same for all pages, so that a page takes scalar instructions alone.
 template <int D>
-__device__ __forceinline__ void request_page(const ChunkArgs& a, int head, int page, int half, uint32_t block) {
-    const int lane = threadIdx.x & 63;
-    const bool there = (unsigned)page < (unsigned)a.n_pages;
-    const int64_t at = there ? page : 0;
-    const uint8_t* k = a.codes + at * a.k_page + head * a.k_head;
-    const uint8_t* v = a.codes + a.v_off + at * a.v_page + head * a.v_head;
-    constexpr int PIECES = D / 16, TOKENS = 64 / PIECES;   // of a token, of a request
+struct PageRequests {
+    const uint8_t *codes, *scales;   // the head's
+    int64_t k_page, v_off, v_page, s_page;
+    int n_pages;
+    uint32_t k_lane[2], v_lane, s_lane;   // keys by half of the block
+    uint32_t there;                       // bit i: whether the page that was requested i pages ago is
+
+    __device__ __forceinline__ void init(const ChunkArgs& a, int head) {
+        const int lane = threadIdx.x & 63;
+        codes = a.codes + head * a.k_head;
+        scales = a.scales + head * a.s_head;
+        k_page = a.k_page, v_off = a.v_off + head * (a.v_head - a.k_head), v_page = a.v_page, s_page = a.s_page;
+        n_pages = a.n_pages;
+        constexpr int PIECES = D / 16;
+        const int token = lane / PIECES;   // more tokens of a page have the same key
 #pragma unroll
-    for (int j = 0; j < kPageTokens / TOKENS; ++j) {
-        const int token = j * TOKENS + lane / PIECES;
-        const uint8_t* p = k + token * D + ((lane % PIECES) ^ Block<D>::key(kPageTokens * half + token)) * 16;
-        lds_fetch16(there ? (const void*)p : &g_zeros, block + (kPageTokens * half + j * TOKENS) * D);
+        for (int half = 0; half < 2; ++half) k_lane[half] = token * D + ((lane % PIECES) ^ Block<D>::key(kPageTokens * half + token)) * 16;
+        v_lane = lane * 16;
+        s_lane = (lane & 3) * 4 + (lane & 4 ? (uint32_t)a.vs_off : 0u);   // sixteen powers of keys, sixteen of values, again and again
+        there = 0;
     }
+    __device__ __forceinline__ void request(int page, int half, uint32_t block) {
+        const bool on = (unsigned)page < (unsigned)n_pages;
+        there = there << 1 | (on ? 1u : 0u);
+        const uint8_t* k = on ? codes + page * k_page : (const uint8_t*)g_no_page;
+        const uint8_t* v = on ? codes + v_off + page * v_page : (const uint8_t*)g_no_page;
+        const uint8_t* s = on ? scales + page * s_page : (const uint8_t*)g_no_page;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j)
-        lds_fetch16(there ? (const void*)(v + j * 1024 + lane * 16) : &g_zeros, block + Block<D>::V + half * 16 * D + j * 1024);
-    const uint8_t* s = a.scales + at * a.s_page + head * a.s_head + (lane & 3) * 4;
-    if (lane >= 4) s += a.vs_off;
-    if (lane >= 8) s = (const uint8_t*)&g_there[0];
-    lds_fetch4(there ? (const void*)s : &g_zeros, block + Block<D>::S + half * 256);
-}
+        for (int j = 0; j < D / 64; ++j) lds_dma16(k + j * 1024, half ? k_lane[1] : k_lane[0], block + half * 16 * D + j * 1024);
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) lds_dma16(v + j * 1024, v_lane, block + Block<D>::V + half * 16 * D + j * 1024);
+        lds_dma4(s, s_lane, block + Block<D>::S + half * 256);
+    }
+    // The powers of a page that has landed, as floats, and whether it is there; `ago`: pages requested since
+    __device__ __forceinline__ void widen(uint8_t* page, int ago) const {
+        const int lane = threadIdx.x & 63;
+        if (lane < 32) *reinterpret_cast<uint32_t*>(page + Block<D>::VALUES + lane * 4) = (uint32_t)page[lane ^ 16] << 23;
+        if (lane == 32) *reinterpret_cast<uint32_t*>(page + Block<D>::THERE) = there >> ago & 1;
+    }
+};
+__device__ __forceinline__ bool page_there(const uint8_t* page) { return *reinterpret_cast<const uint32_t*>(page + 32) != 0; }
 
 // A wave's 32 places: operands, and what has been summed up
 template <class T, int D>
@@ -175,47 +196,71 @@ struct Places {
         had = 0;
     }
 
-    // Tokens at .. at + 31, of which those from n on have not been written.  whole: every place of the wave sees all of them
-    __device__ __forceinline__ void step(const ChunkArgs& a, const uint8_t* block, int at, int n, bool whole) {
-        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+    // A block's keys on their way into operands
+    struct Keys {
+        u32x4_s codes[KS / 2];
+        float scale;
+        __device__ __forceinline__ void read(const uint8_t* block) {
+            const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+#pragma unroll
+            for (int w = 0; w < KS / 2; ++w) codes[w] = *reinterpret_cast<const u32x4_s*>(block + token * D + ((2 * w + h) ^ Block<D>::key(token)) * 16);
+            scale = *reinterpret_cast<const float*>(block + Block<D>::S + (token >> 4) * 256 + Block<D>::KEYS + (token & 15) * 4);
+        }
+        __device__ __forceinline__ bf16x8 operand(int s) const { return codes_to_bf16(codes[s >> 1][2 * (s & 1)], codes[s >> 1][2 * (s & 1) + 1], scale); }
+    };
+    __device__ __forceinline__ void scores(const Keys& k, int s, f32x16& out) const {   // one step of 16 dims
+        const bf16x8 x = k.operand(s);
+#pragma unroll
+        for (int p = 0; p < P; ++p) out = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][s], out, 0, 0, 0);
+    }
+    __device__ __forceinline__ f32x16 scores(const uint8_t* block) const {
+        Keys k;
+        k.read(block);
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
-        {
-            const int token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
-            const float scale = __uint_as_float((uint32_t)block[Block<D>::S + (token >> 4) * 256 + (token & 15)] << 23);
-            const uint8_t* k = block + token * D;
-            auto read = [&](int w) { return *reinterpret_cast<const u32x4_s*>(k + ((2 * w + h) ^ Block<D>::key(token)) * 16); };
-            u32x4_s next = read(0);
 #pragma unroll
-            for (int w = 0; w < KS / 2; ++w) {
-                const u32x4_s codes = next;
-                if (w + 1 < KS / 2) next = read(w + 1);
-                __builtin_amdgcn_sched_barrier(0);   // codes are converted where they are used: all at once they take the registers
+        for (int i = 0; i < KS; ++i) scores(k, i, s);
+        return s;
+    }
+
+    // Scores s of the block of tokens at .. at + 31, of which those from n on have not been written, into weights and the output; meanwhile the scores s2 of
+    // `next`, if there is one, products and weights in turn.  whole: every place of the wave sees all of the tokens
+    template <bool NEXT = true>
+    __device__ __forceinline__ void step(const ChunkArgs& a, f32x16& s, const uint8_t* block, int at, int n, bool whole, const uint8_t* next, f32x16& s2) {
+        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+        Keys k;
+        if constexpr (NEXT) k.read(next);
+        float vs[16];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bf16x8 x = codes_to_bf16(codes[2 * u], codes[2 * u + 1], scale);
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(block + Block<D>::S + h * 256 + Block<D>::VALUES + 16 * i);
 #pragma unroll
-                    for (int p = 0; p < P; ++p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][2 * w + u], s, 0, 0, 0);
-                }
-            }
+            for (int e = 0; e < 4; ++e) vs[4 * i + e] = x[e];
         }
-        u32x4_s vs = *reinterpret_cast<const u32x4_s*>(block + Block<D>::S + h * 256 + 16);
-        uint32_t live = 0xffff;          // of the lane's sixteen tokens, which its place sees
+        const uint8_t* v = block + Block<D>::V + h * 16 * D + c * 16;
+        u32x4_s codes[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) codes[j] = *reinterpret_cast<const u32x4_s*>(v + j * 512);
         const int mine = at + 16 * h;
         if (!whole) {
-            const bool there = *reinterpret_cast<const uint32_t*>(block + Block<D>::S + h * 256 + 32) != 0;
             const int from = max(lo - mine, 0), to = min(hi - mine, 15);
-            live = there && from <= to ? (0xffffu >> (15 - to)) & (0xffffu << from) : 0u;
+            const uint32_t live = page_there(block + Block<D>::S + h * 256) && from <= to ? (0xffffu >> (15 - to)) & (0xffffu << from) : 0u;   // tokens that the lane's place sees
             had |= live;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (!(live >> i & 1)) s[i] = -INFINITY;
+                if (!(live >> i & 1)) s[i] = -INFINITY, vs[i] = 0.f;   // a power that nobody has written is not used
+            // Values that nobody has written are not used; a not-a-number in one that a place does not see must not reach it, though its weight is 0.
+            bool odd = false;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {   // powers that nobody has written are not used
-                const uint32_t b = live >> (4 * j) & 15;
-                vs[j] &= ((b & 1) * 0xffu) | ((b >> 1 & 1) * 0xff00u) | ((b >> 2 & 1) * 0xff0000u) | ((b >> 3) * 0xff000000u);
-            }
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int written = min(max(n - mine - 4 * e, 0), 4);
+                    codes[j][e] &= written == 4 ? ~0u : (1u << (8 * written)) - 1;
+                    odd |= not_a_number(codes[j][e]) != 0;
+                }
+            if (__any(odd)) mark(codes, live);
         } else {
             had = 1;
         }
@@ -237,81 +282,67 @@ struct Places {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[j][i] *= f;
         }
-        const uint8_t* v = block + Block<D>::V + h * 16 * D + c * 16;
-        u32x4_s codes[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) codes[j] = *reinterpret_cast<const u32x4_s*>(v + j * 512);
         const float ref = m == -INFINITY ? 0.f : m;
-        bf16x8 w[P][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            u32x4_s words[P];
+        for (int i = 0; i < 16; ++i) s2[i] = 0.f;
+        u32x4_s words[P][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int i = 8 * u + 2 * j + e;
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -ref));
-                    l += p;
-                    x[e] = p * power(vs[i >> 2], i & 3);
-                }
-                words[0][j] = pack_bf16(x[0], x[1]);
-                if constexpr (F32) {
-                    x[0] -= bf16_lo(words[0][j]), x[1] -= bf16_hi(words[0][j]);
-                    words[1][j] = pack_bf16(x[0], x[1]);
-                    words[2][j] = pack_bf16(x[0] - bf16_lo(words[1][j]), x[1] - bf16_hi(words[1][j]));
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < P; ++p) w[p][u] = __builtin_bit_cast(bf16x8, words[p]);
-        }
-        if (!whole) {
-            // Values that nobody has written are not used; a not-a-number in one that a place does not see must not reach it, though its weight is 0.
-            bool odd = false;
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int written = min(max(n - mine - 4 * e, 0), 4);
-                    codes[j][e] &= written == 4 ? ~0u : (1u << (8 * written)) - 1;
-                    odd |= (((codes[j][e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
-                }
-            if (__any(odd)) {   // marked where a place sees one, by a product of ones, and left out below
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    f32x16 d;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) d[i] = 0.f;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        u32x4_s one, sees;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t bad = (((codes[j][2 * u + (e >> 1)] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> (16 * (e & 1));
-                            one[e] = (bad & 0x80u ? 0x3f80u : 0u) | (bad & 0x8000u ? 0x3f800000u : 0u);
-                            sees[e] = (live >> (8 * u + 2 * e) & 1 ? 0x3f80u : 0u) | (live >> (8 * u + 2 * e + 1) & 1 ? 0x3f800000u : 0u);
-                        }
-                        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, one), __builtin_bit_cast(bf16x8, sees), d, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (d[i] > 0.f) o[j][i] = NAN;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) codes[j][e] &= ~(((((codes[j][e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
+        for (int j = 0; j < 8; ++j) {
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (NEXT)
+                if (j % (8 / KS) == 0) scores(k, j / (8 / KS), s2);
+            float x[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = 2 * j + e;
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -ref));
+                l += p;
+                x[e] = p * vs[i];
+            }
+            words[0][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
+            if constexpr (F32) {
+                x[0] -= bf16_lo(words[0][j >> 2][j & 3]), x[1] -= bf16_hi(words[0][j >> 2][j & 3]);
+                words[1][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
+                words[2][j >> 2][j & 3] = pack_bf16(x[0] - bf16_lo(words[1][j >> 2][j & 3]), x[1] - bf16_hi(words[1][j >> 2][j & 3]));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
                 const bf16x8 x = codes_to_bf16(codes[j][2 * u], codes[j][2 * u + 1]);
 #pragma unroll
-                for (int p = 0; p < P; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, w[p][u], o[j], 0, 0, 0);
+                for (int p = 0; p < P; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, words[p][u]), o[j], 0, 0, 0);
             }
+    }
+
+    __device__ static uint32_t not_a_number(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }   // the upper bit of each that is
+
+    // Values that are not numbers: marked in the output where a place sees one, by a product of ones, and taken out
+    __device__ __forceinline__ void mark(u32x4_s (&codes)[NB], uint32_t live) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            f32x16 d;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) d[i] = 0.f;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                u32x4_s one, sees;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t bad = not_a_number(codes[j][2 * u + (e >> 1)]) >> (16 * (e & 1));
+                    one[e] = (bad & 0x80u ? 0x3f80u : 0u) | (bad & 0x8000u ? 0x3f800000u : 0u);
+                    sees[e] = (live >> (8 * u + 2 * e) & 1 ? 0x3f80u : 0u) | (live >> (8 * u + 2 * e + 1) & 1 ? 0x3f800000u : 0u);
+                }
+                d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, one), __builtin_bit_cast(bf16x8, sees), d, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (d[i] > 0.f) o[j][i] = NAN;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) codes[j][e] &= ~((not_a_number(codes[j][e]) >> 7) * 0xffu);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -347,35 +378,50 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    // positions that all of the wave's places see, and that any does
+    // positions from all_from to low are seen by all of the wave's places
     const int base = p.r.n - p.r.count, low = base + v0 / G, high = base + (min(v0 + 32, live) - 1) / G;
-    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0, any_from = a.window > 0 ? max(low - a.window + 1, 0) : 0;
+    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
     Places<T, D> w;
     w.load(a, p.r, head, v0 + c);
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
     int ahead = range.begin + wave * kPageTokens, fill = 0;
     int page = page_at(ahead);
+    PageRequests<D> pages;
+    pages.init(a, head);
     auto request = [&]() {
-        request_page<D>(a, head, page, wave & 1, lds0 + fill * STAGE + (wave >> 1) * Block<D>::BYTES);
+        pages.request(page, wave & 1, lds0 + fill * STAGE + (wave >> 1) * Block<D>::BYTES);
         ahead += 64;
         page = page_at(ahead);
         if (++fill == ST) fill = 0;
     };
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) request();
+    uint8_t* const own = lds + (wave >> 1) * Block<D>::BYTES + Block<D>::S + (wave & 1) * 256;   // the wave's page of a stage
+    auto block_at = [&](int stage, int half) { return lds + stage * STAGE + half * Block<D>::BYTES; };
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 2)) : "memory");
+    pages.widen(own, ST - 2);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     int at = 0;
-    for (int token = range.begin; token < range.end; token += 64) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(OPS * (ST - 2)) : "memory");   // the step has landed for every wave, and all are done with the one before
+    // The next step has landed for every wave, and all are done with the one before this, whose place is filled again
+    auto turn = [&](int next) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 3)) : "memory");
+        pages.widen(own + next * STAGE, ST - 3);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         request();
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-            const int from = token + 32 * half;
-            const uint8_t* block = lds + at * STAGE + half * Block<D>::BYTES;
-            if (v0 >= live || from > high || from + 31 < any_from) continue;
-            const bool there = *reinterpret_cast<const uint32_t*>(block + Block<D>::S + h * 256 + 32) != 0;
-            w.step(a, block, from, p.r.n, from >= all_from && from + 31 <= low && __all(there));
+    };
+    auto after = [&](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
+    if (v0 < live) {
+        f32x16 s = w.scores(block_at(0, 0)), s2;
+        for (int token = range.begin; token < range.end; token += 64) {
+            const int next = after(at);
+            const uint8_t *first = block_at(at, 0), *second = block_at(at, 1);
+            w.step(a, s, first, token, p.r.n, token >= all_from && token + 31 <= low && __all(page_there(first + Block<D>::S + h * 256)), second, s2);
+            turn(next);
+            w.step(a, s2, second, token + 32, p.r.n, token + 32 >= all_from && token + 63 <= low && __all(page_there(second + Block<D>::S + h * 256)), block_at(next, 0), s);
+            at = next;
         }
-        if (++at == ST) at = 0;
+    } else {   // requests for the others
+        for (int token = range.begin; token < range.end; token += 64) turn(at = after(at));
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     w.close();
@@ -417,6 +463,7 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
     const ChunkRange range = chunk_range(a, p.r, 0, kFew, split, 32 * kWaves);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * ST * STAGE;
+    uint8_t* const ring = lds + wave * ST * STAGE;
     const int low = p.r.n - p.r.count, high = p.r.n - 1;
     const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
     Places<T, D> w;
@@ -424,9 +471,11 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
     int ahead = range.begin + 32 * wave, fill = 0;
     int page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
+    PageRequests<D> pages;
+    pages.init(a, head);
     auto request = [&]() {
-        request_page<D>(a, head, page0, 0, lds0 + fill * STAGE);
-        request_page<D>(a, head, page1, 1, lds0 + fill * STAGE);
+        pages.request(page0, 0, lds0 + fill * STAGE);
+        pages.request(page1, 1, lds0 + fill * STAGE);
         ahead += 32 * kWaves;
         page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
         if (++fill == ST) fill = 0;
@@ -437,9 +486,12 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
     for (int from = range.begin + 32 * wave; from < range.end; from += 32 * kWaves) {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OPS * (ST - 2)) : "memory");
         request();
-        const uint8_t* block = lds + (wave * ST + at) * STAGE;
-        const bool there = *reinterpret_cast<const uint32_t*>(block + Block<D>::S + h * 256 + 32) != 0;
-        w.step(a, block, from, p.r.n, from >= all_from && from + 31 <= low && __all(there));
+        const uint8_t* block = ring + at * STAGE;
+        pages.widen(ring + at * STAGE + Block<D>::S, 2 * (ST - 1) + 1);
+        pages.widen(ring + at * STAGE + Block<D>::S + 256, 2 * (ST - 1));
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        f32x16 s = w.scores(block), none;
+        w.template step<false>(a, s, block, from, p.r.n, from >= all_from && from + 31 <= low && __all(page_there(block + Block<D>::S + h * 256)), nullptr, none);
         if (++at == ST) at = 0;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
