@@ -95,18 +95,28 @@ __device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, int index) 
 
 // ---------------------------------------------------------------- attention of one part
 
-// LDS: blocks of 32 tokens (two pages) of a KV head.  Keys [token][16-byte piece ^ key], values [page][dim][16 tokens], and 256 bytes a page: 16 powers of keys and 16 of
-// values; when they have landed the wave that requested the page writes behind them a word that says whether it is there, and the powers as floats, values first.
+// LDS: blocks of 32 tokens (two pages) of a KV head.  Keys [token][16-byte piece ^ key], values [page][dim][16 tokens], 256 bytes a page of powers (16 of keys, 16 of
+// values), and a page's notes, which the wave that requested it writes when it has landed: the powers as floats, whether it is there, and which of its values are not numbers.
+struct Notes {
+    float powers[32];         // of values, and behind them of keys
+    uint32_t there, odd;      // odd: `bad` is to be looked at
+    uint32_t unused[14];
+    uint16_t bad[128];        // of a dim: its tokens, a bit each
+    __device__ bool plain() const { return there && !odd; }
+};
 template <int D>
 struct Block {
-    static constexpr int V = 32 * D, S = 64 * D, THERE = 32, VALUES = 64, KEYS = 128, BYTES = 64 * D + 512, OPS = 2 * (D / 64) + 1;   // requests of a page
+    static constexpr int V = 32 * D, S = 64 * D, N = S + 512, BYTES = N + 2 * (int)sizeof(Notes), OPS = 2 * (D / 64) + 1;   // requests of a page
     __device__ static int key(int token) { return D == 128 ? (token & 3) | (token >> 2 & 4) : (token >> 1 & 1) | (token >> 3 & 2); }
+    __device__ static const Notes& notes(const uint8_t* block, int half) { return reinterpret_cast<const Notes*>(block + N)[half]; }
 };
-constexpr int kWideStages = 4, kFewStages = 2;
+__device__ __forceinline__ uint32_t not_a_number(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }   // the upper bit of each that is
+constexpr int kWideStages = 4;
 template <int D>
-struct ChunkLds {
-    static constexpr int RING = kWaves * kFewStages * Block<D>::BYTES, WIDE = kWideStages * 2 * Block<D>::BYTES, SUMS = kWaves * 32 * (D + 4) * 4 + kWaves * 32 * 8;
-    static constexpr int BYTES = RING > WIDE ? (RING > SUMS ? RING : SUMS) : (WIDE > SUMS ? WIDE : SUMS);
+struct ChunkLds {   // two workgroups on a compute unit
+    static constexpr int WIDE = kWideStages * 2 * Block<D>::BYTES, FEW = kWaves * Block<D>::BYTES, SUMS = kWaves * 32 * (D / 2 + 4) * 4 + kWaves * 32 * 8;
+    static constexpr int BYTES = WIDE;
+    static_assert(WIDE >= FEW && WIDE >= SUMS && 2 * WIDE <= 160 * 1024, "");
 };
 
 // What lanes are given of a page that is not there: a block of keys, one of values, powers
@@ -147,14 +157,37 @@ struct PageRequests {
         for (int j = 0; j < D / 64; ++j) lds_dma16(v + j * 1024, v_lane, block + Block<D>::V + half * 16 * D + j * 1024);
         lds_dma4(s, s_lane, block + Block<D>::S + half * 256);
     }
-    // The powers of a page that has landed, as floats, and whether it is there; `ago`: pages requested since
-    __device__ __forceinline__ void widen(uint8_t* page, int ago) const {
+    // Notes of a page that has landed, requested `ago` pages ago, whose first token is `at`.  Powers and values from token n on, which nobody has written, become zeros; where some places see
+    // a token and others do not (`partly`), values that are not numbers are noted and become zeros: their product with a weight of 0 would not be.
+    __device__ __forceinline__ void note(uint8_t* block, int half, int ago, int at, int n, bool partly) const {
         const int lane = threadIdx.x & 63;
-        if (lane < 32) *reinterpret_cast<uint32_t*>(page + Block<D>::VALUES + lane * 4) = (uint32_t)page[lane ^ 16] << 23;
-        if (lane == 32) *reinterpret_cast<uint32_t*>(page + Block<D>::THERE) = there >> ago & 1;
+        Notes& notes = reinterpret_cast<Notes*>(block + Block<D>::N)[half];
+        const uint8_t* s = block + Block<D>::S + half * 256;
+        if (lane < 32) notes.powers[lane] = at + (lane & 15) < n ? __uint_as_float((uint32_t)s[lane ^ 16] << 23) : 0.f;   // keys behind values
+        bool any = false;
+        if (partly) {
+#pragma unroll 1
+            for (int dim = lane; dim < D; dim += 64) {
+                u32x4_s* p = reinterpret_cast<u32x4_s*>(block + Block<D>::V + half * 16 * D + dim * 16);
+                u32x4_s x = *p;
+                uint32_t mask = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int written = min(max(n - at - 4 * e, 0), 4);
+                    x[e] &= written == 4 ? ~0u : (1u << (8 * written)) - 1;
+                    const uint32_t bad = not_a_number(x[e]);
+                    x[e] &= ~((bad >> 7) * 0xffu);
+                    mask |= ((bad >> 7 & 1) | (bad >> 14 & 2) | (bad >> 21 & 4) | (bad >> 28 & 8)) << (4 * e);
+                }
+                any |= mask != 0;
+                notes.bad[dim] = (uint16_t)mask;
+                *p = x;
+            }
+        }
+        const uint32_t odd = __any(any) ? 1u : 0u;
+        if (lane == 0) notes.there = there >> ago & 1, notes.odd = odd;
     }
 };
-__device__ __forceinline__ bool page_there(const uint8_t* page) { return *reinterpret_cast<const uint32_t*>(page + 32) != 0; }
 
 // A wave's 32 places: operands, and what has been summed up
 template <class T, int D>
@@ -196,74 +229,40 @@ struct Places {
         had = 0;
     }
 
-    // A block's keys on their way into operands
-    struct Keys {
-        u32x4_s codes[KS / 2];
-        float scale;
-        __device__ __forceinline__ void read(const uint8_t* block) {
-            const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
-#pragma unroll
-            for (int w = 0; w < KS / 2; ++w) codes[w] = *reinterpret_cast<const u32x4_s*>(block + token * D + ((2 * w + h) ^ Block<D>::key(token)) * 16);
-            scale = *reinterpret_cast<const float*>(block + Block<D>::S + (token >> 4) * 256 + Block<D>::KEYS + (token & 15) * 4);
-        }
-        __device__ __forceinline__ bf16x8 operand(int s) const { return codes_to_bf16(codes[s >> 1][2 * (s & 1)], codes[s >> 1][2 * (s & 1) + 1], scale); }
-    };
-    __device__ __forceinline__ void scores(const Keys& k, int s, f32x16& out) const {   // one step of 16 dims
-        const bf16x8 x = k.operand(s);
-#pragma unroll
-        for (int p = 0; p < P; ++p) out = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][s], out, 0, 0, 0);
-    }
-    __device__ __forceinline__ f32x16 scores(const uint8_t* block) const {
-        Keys k;
-        k.read(block);
+    // The block of tokens at .. at + 31.  whole: every place of the wave sees all of them, and nothing has been taken out of it
+    __device__ __forceinline__ void step(const ChunkArgs& a, const uint8_t* block, int at, bool whole) {
+        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+        const Notes& notes = Block<D>::notes(block, h);
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        {
+            const int token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+            const float scale = Block<D>::notes(block, token >> 4).powers[16 + (token & 15)];
+            auto read = [&](int w) { return *reinterpret_cast<const u32x4_s*>(block + token * D + ((2 * w + h) ^ Block<D>::key(token)) * 16); };
+            u32x4_s next = read(0);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) scores(k, i, s);
-        return s;
-    }
-
-    // Scores s of the block of tokens at .. at + 31, of which those from n on have not been written, into weights and the output; meanwhile the scores s2 of
-    // `next`, if there is one, products and weights in turn.  whole: every place of the wave sees all of the tokens
-    template <bool NEXT = true>
-    __device__ __forceinline__ void step(const ChunkArgs& a, f32x16& s, const uint8_t* block, int at, int n, bool whole, const uint8_t* next, f32x16& s2) {
-        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
-        Keys k;
-        if constexpr (NEXT) k.read(next);
-        float vs[16];
+            for (int w = 0; w < KS / 2; ++w) {
+                const u32x4_s codes = next;
+                if (w + 1 < KS / 2) next = read(w + 1);
+                __builtin_amdgcn_sched_barrier(0);   // codes are converted where they are used: all at once they take the registers
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(block + Block<D>::S + h * 256 + Block<D>::VALUES + 16 * i);
+                for (int u = 0; u < 2; ++u) {
+                    const bf16x8 x = codes_to_bf16(codes[2 * u], codes[2 * u + 1], scale);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vs[4 * i + e] = x[e];
-        }
-        const uint8_t* v = block + Block<D>::V + h * 16 * D + c * 16;
-        u32x4_s codes[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) codes[j] = *reinterpret_cast<const u32x4_s*>(v + j * 512);
-        const int mine = at + 16 * h;
-        if (!whole) {
-            const int from = max(lo - mine, 0), to = min(hi - mine, 15);
-            const uint32_t live = page_there(block + Block<D>::S + h * 256) && from <= to ? (0xffffu >> (15 - to)) & (0xffffu << from) : 0u;   // tokens that the lane's place sees
-            had |= live;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (!(live >> i & 1)) s[i] = -INFINITY, vs[i] = 0.f;   // a power that nobody has written is not used
-            // Values that nobody has written are not used; a not-a-number in one that a place does not see must not reach it, though its weight is 0.
-            bool odd = false;
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int written = min(max(n - mine - 4 * e, 0), 4);
-                    codes[j][e] &= written == 4 ? ~0u : (1u << (8 * written)) - 1;
-                    odd |= not_a_number(codes[j][e]) != 0;
+                    for (int p = 0; p < P; ++p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][2 * w + u], s, 0, 0, 0);
                 }
-            if (__any(odd)) mark(codes, live);
-        } else {
-            had = 1;
+            }
         }
+        uint32_t live = 0xffff;   // tokens that the lane's place sees
+        if (!whole) {
+            const int mine = at + 16 * h, from = max(lo - mine, 0), to = min(hi - mine, 15);
+            live = notes.there && from <= to ? (0xffffu >> (15 - to)) & (0xffffu << from) : 0u;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = live >> i & 1 ? s[i] : -INFINITY;
+            if (__any(notes.odd != 0)) mark(block, live);
+        }
+        had |= live;
         float top = s[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
@@ -283,29 +282,29 @@ struct Places {
                 for (int i = 0; i < 16; ++i) o[j][i] *= f;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s2[i] = 0.f;
+        const uint8_t* v = block + Block<D>::V + h * 16 * D + c * 16;
+        u32x4_s codes[NB];
         u32x4_s words[P][2];
+        f32x4 vs;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (NEXT)
-                if (j % (8 / KS) == 0) scores(k, j / (8 / KS), s2);
+            if (j % 2 == 0) vs = *reinterpret_cast<const f32x4*>(notes.powers + 2 * j);
             float x[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int i = 2 * j + e;
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.c, -ref));
-                l += p;
-                x[e] = p * vs[i];
-            }
+            for (int e = 0; e < 2; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * j + e], a.c, -ref));
+            l += x[0] + x[1];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[e] *= vs[(2 * j + e) & 3];
             words[0][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
             if constexpr (F32) {
                 x[0] -= bf16_lo(words[0][j >> 2][j & 3]), x[1] -= bf16_hi(words[0][j >> 2][j & 3]);
                 words[1][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
                 words[2][j >> 2][j & 3] = pack_bf16(x[0] - bf16_lo(words[1][j >> 2][j & 3]), x[1] - bf16_hi(words[1][j >> 2][j & 3]));
             }
+            if (j >= 8 - NB) codes[j - 8 + NB] = *reinterpret_cast<const u32x4_s*>(v + (j - 8 + NB) * 512);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        asm volatile("" : "+v"(l));   // summed here: left to itself the compiler sums later, all in a row
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -317,33 +316,19 @@ struct Places {
             }
     }
 
-    __device__ static uint32_t not_a_number(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }   // the upper bit of each that is
-
-    // Values that are not numbers: marked in the output where a place sees one, by a product of ones, and taken out
-    __device__ __forceinline__ void mark(u32x4_s (&codes)[NB], uint32_t live) {
+    // Not-a-numbers among a block's values into the output of the places that see them
+    __device__ __forceinline__ void mark(const uint8_t* block, uint32_t live) {
+        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+        const Notes &first = Block<D>::notes(block, 0), &second = Block<D>::notes(block, 1);
+        const uint32_t seen0 = first.odd ? __shfl(live, c) : 0u, seen1 = second.odd ? __shfl(live, c + 32) : 0u;   // `bad` says nothing where a page is not odd
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            f32x16 d;
+        for (int j = 0; j < NB; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) d[i] = 0.f;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                u32x4_s one, sees;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t bad = not_a_number(codes[j][2 * u + (e >> 1)]) >> (16 * (e & 1));
-                    one[e] = (bad & 0x80u ? 0x3f80u : 0u) | (bad & 0x8000u ? 0x3f800000u : 0u);
-                    sees[e] = (live >> (8 * u + 2 * e) & 1 ? 0x3f80u : 0u) | (live >> (8 * u + 2 * e + 1) & 1 ? 0x3f800000u : 0u);
-                }
-                d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, one), __builtin_bit_cast(bf16x8, sees), d, 0, 0, 0);
+            for (int i = 0; i < 16; ++i) {
+                const int dim = 32 * j + 8 * (i >> 2) + 4 * h + (i & 3);
+                if ((first.bad[dim] & seen0) | (second.bad[dim] & seen1)) o[j][i] = NAN;
+                __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (d[i] > 0.f) o[j][i] = NAN;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) codes[j][e] &= ~((not_a_number(codes[j][e]) >> 7) * 0xffu);
-            __builtin_amdgcn_sched_barrier(0);
-        }
     }
 
     // The two halves' sums, and a reference that says whether there was a token
@@ -357,6 +342,15 @@ struct Places {
         if (m == -INFINITY && had) m = -FLT_MAX;
     }
 };
+
+// What a weighted sum is multiplied with: 1 / the weights' sum, 0 where there is no token.  Weights are 2^-kHead and more at the reference, so a sum is no less, or 0 where all
+// scores are minus infinity, which leaves not-a-numbers.
+__device__ __forceinline__ float chunk_factor(float sum, float top) { return sum == 0.f && top == -INFINITY ? 0.f : sum == 0.f ? NAN : 1.f / sum; }
+template <class T>
+__device__ __forceinline__ void store4(T* to, float a, float b, float c, float d) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = f32x4{a, b, c, d};
+    else *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(a, b), pack_bf16(c, d)};
+}
 
 // The range of a tile's part
 struct ChunkRange { int begin, end; };
@@ -378,9 +372,11 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    // positions from all_from to low are seen by all of the wave's places
+    // positions from all_from to low are seen by all of the wave's places, from any_from to high by any
     const int base = p.r.n - p.r.count, low = base + v0 / G, high = base + (min(v0 + 32, live) - 1) / G;
-    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
+    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0, any_from = a.window > 0 ? max(low - a.window + 1, 0) : 0;
+    // and the tile's positions from tile_from to tile_to by all of its places
+    const int tile_to = base + tile * kTile / G, tile_from = a.window > 0 ? max(base + (min((tile + 1) * kTile, live) - 1) / G - a.window + 1, 0) : 0;
     Places<T, D> w;
     w.load(a, p.r, head, v0 + c);
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
@@ -396,32 +392,24 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     };
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) request();
-    uint8_t* const own = lds + (wave >> 1) * Block<D>::BYTES + Block<D>::S + (wave & 1) * 256;   // the wave's page of a stage
-    auto block_at = [&](int stage, int half) { return lds + stage * STAGE + half * Block<D>::BYTES; };
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 2)) : "memory");
-    pages.widen(own, ST - 2);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const bool on = v0 < live;
     int at = 0;
-    // The next step has landed for every wave, and all are done with the one before this, whose place is filled again
-    auto turn = [&](int next) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 3)) : "memory");
-        pages.widen(own + next * STAGE, ST - 3);
+    for (int token = range.begin; token < range.end; token += 64) {
+        // The step has landed for every wave, and all are done with the one before, whose place is filled again
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 2)) : "memory");
+        pages.note(lds + at * STAGE + (wave >> 1) * Block<D>::BYTES, wave & 1, ST - 2, token + 16 * wave, p.r.n, token < tile_from || token + 63 > tile_to);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         request();
-    };
-    auto after = [&](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
-    if (v0 < live) {
-        f32x16 s = w.scores(block_at(0, 0)), s2;
-        for (int token = range.begin; token < range.end; token += 64) {
-            const int next = after(at);
-            const uint8_t *first = block_at(at, 0), *second = block_at(at, 1);
-            w.step(a, s, first, token, p.r.n, token >= all_from && token + 31 <= low && __all(page_there(first + Block<D>::S + h * 256)), second, s2);
-            turn(next);
-            w.step(a, s2, second, token + 32, p.r.n, token + 32 >= all_from && token + 63 <= low && __all(page_there(second + Block<D>::S + h * 256)), block_at(next, 0), s);
-            at = next;
+        if (on) {
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int from = token + 32 * half;
+                const uint8_t* block = lds + at * STAGE + half * Block<D>::BYTES;
+                if (from > high || from + 31 < any_from) continue;
+                w.step(a, block, from, from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()));
+            }
         }
-    } else {   // requests for the others
-        for (int token = range.begin; token < range.end; token += 64) turn(at = after(at));
+        if (++at == ST) at = 0;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     w.close();
@@ -430,16 +418,13 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
         if (p.r.splits == 1) {
             const int row = p.r.start + v / G;
             T* out = (T*)a.out + ((int64_t)row * a.Hq + head * G + v % G) * D;
+            const float f = chunk_factor(w.l, w.m);
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float x[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = kv8_quotient(w.o[j][4 * e + i], w.l, w.m);
-                    T* to = out + 32 * j + 8 * e + 4 * h;
-                    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
-                    else *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+                    const f32x16& o = w.o[j];
+                    store4(out + 32 * j + 8 * e + 4 * h, o[4 * e] * f, o[4 * e + 1] * f, o[4 * e + 2] * f, o[4 * e + 3] * f);
                 }
         } else {
             const int64_t place = slot * a.slot_rows + 32 * wave + c;
@@ -457,80 +442,78 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
 // Up to 32 places: each wave has all of them, and every fourth 32 tokens, which it requests for itself.
 template <class T, int D>
 __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& p, int head, int split, int64_t slot, uint8_t* lds) {
-    constexpr int ST = kFewStages, STAGE = Block<D>::BYTES, OPS = 2 * Block<D>::OPS, LD = D + 4;
+    constexpr int HALF = D / 2, LD = HALF + 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hkv, live = p.r.count * G;
     const ChunkRange range = chunk_range(a, p.r, 0, kFew, split, 32 * kWaves);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * ST * STAGE;
-    uint8_t* const ring = lds + wave * ST * STAGE;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * Block<D>::BYTES;
+    uint8_t* const block = lds + wave * Block<D>::BYTES;
     const int low = p.r.n - p.r.count, high = p.r.n - 1;
     const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
     Places<T, D> w;
     w.load(a, p.r, head, c);
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
-    int ahead = range.begin + 32 * wave, fill = 0;
+    int ahead = range.begin + 32 * wave;
     int page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
     PageRequests<D> pages;
     pages.init(a, head);
     auto request = [&]() {
-        pages.request(page0, 0, lds0 + fill * STAGE);
-        pages.request(page1, 1, lds0 + fill * STAGE);
+        pages.request(page0, 0, lds0);
+        pages.request(page1, 1, lds0);
         ahead += 32 * kWaves;
         page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
-        if (++fill == ST) fill = 0;
     };
-#pragma unroll
-    for (int s = 0; s < ST - 1; ++s) request();
-    int at = 0;
     for (int from = range.begin + 32 * wave; from < range.end; from += 32 * kWaves) {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OPS * (ST - 2)) : "memory");
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the last step read is written again
         request();
-        const uint8_t* block = ring + at * STAGE;
-        pages.widen(ring + at * STAGE + Block<D>::S, 2 * (ST - 1) + 1);
-        pages.widen(ring + at * STAGE + Block<D>::S + 256, 2 * (ST - 1));
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const bool partly = from < all_from || from + 31 > low;
+        pages.note(block, 0, 1, from, p.r.n, partly);
+        pages.note(block, 1, 0, from + kPageTokens, p.r.n, partly);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        f32x16 s = w.scores(block), none;
-        w.template step<false>(a, s, block, from, p.r.n, from >= all_from && from + 31 <= low && __all(page_there(block + Block<D>::S + h * 256)), nullptr, none);
-        if (++at == ST) at = 0;
+        w.step(a, block, from, !partly && __all(Block<D>::notes(block, h).plain()));
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     w.close();
-    __syncthreads();   // every wave is done with its ring
     float* sums = reinterpret_cast<float*>(lds);
     float2* ml = reinterpret_cast<float2*>(lds + kWaves * 32 * LD * 4);
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
+    for (int part = 0; part < 2; ++part) {   // half of the dims at a time
+        __syncthreads();   // every wave is done with what was there
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<f32x4*>(sums + (wave * 32 + c) * LD + 32 * j + 8 * e + 4 * h) = f32x4{w.o[j][4 * e], w.o[j][4 * e + 1], w.o[j][4 * e + 2], w.o[j][4 * e + 3]};
-    if (h == 0) ml[wave * 32 + c] = float2{w.m, w.l};
-    __syncthreads();
-    for (int u = threadIdx.x; u < live * (D / 4); u += 64 * kWaves) {
-        const int v = u / (D / 4), d = u % (D / 4) * 4;
-        float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < HALF / 32; ++j)
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i * 32 + v].x);
-        const float ref = top == -INFINITY ? 0.f : top;
+            for (int e = 0; e < 4; ++e) {
+                const f32x16& o = w.o[part * (HALF / 32) + j];
+                *reinterpret_cast<f32x4*>(sums + (wave * 32 + c) * LD + 32 * j + 8 * e + 4 * h) = f32x4{o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]};
+            }
+        if (h == 0) ml[wave * 32 + c] = float2{w.m, w.l};
+        __syncthreads();
+        for (int u = threadIdx.x; u < live * (HALF / 4); u += 64 * kWaves) {
+            const int v = u / (HALF / 4), d = u % (HALF / 4) * 4;
+            float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) {
-            const float2 y = ml[i * 32 + v];
-            const float f = __builtin_amdgcn_exp2f(y.x - ref);
-            const f32x4 o = *reinterpret_cast<const f32x4*>(sums + (i * 32 + v) * LD + d);
-            sum += f * y.y;
+            for (int i = 0; i < kWaves; ++i) top = fmaxf(top, ml[i * 32 + v].x);
+            const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] += f * o[e];
-        }
-        if (p.r.splits == 1) {
-            T* to = (T*)a.out + ((int64_t)(p.r.start + v / G) * a.Hq + head * G + v % G) * D + d;
+            for (int i = 0; i < kWaves; ++i) {
+                const float2 y = ml[i * 32 + v];
+                const float f = __builtin_amdgcn_exp2f(y.x - ref);
+                const f32x4 o = *reinterpret_cast<const f32x4*>(sums + (i * 32 + v) * LD + d);
+                sum += f * y.y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = kv8_quotient(x[e], sum, top);
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
-            else *reinterpret_cast<uint2*>(to) = uint2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-        } else {
-            const int64_t place = slot * a.slot_rows + v;
-            *reinterpret_cast<f32x4*>(a.partial + place * D + d) = f32x4{x[0], x[1], x[2], x[3]};
-            if (d == 0) reinterpret_cast<float2*>(a.partial + a.slots * a.slot_rows * D)[place] = float2{top, sum};
+                for (int e = 0; e < 4; ++e) x[e] += f * o[e];
+            }
+            if (p.r.splits == 1) {
+                T* to = (T*)a.out + ((int64_t)(p.r.start + v / G) * a.Hq + head * G + v % G) * D + part * HALF + d;
+                const float f = chunk_factor(sum, top);
+                store4(to, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+            } else {
+                const int64_t place = slot * a.slot_rows + v;
+                *reinterpret_cast<f32x4*>(a.partial + place * D + part * HALF + d) = f32x4{x[0], x[1], x[2], x[3]};
+                if (part == 0 && d == 0) reinterpret_cast<float2*>(a.partial + a.slots * a.slot_rows * D)[place] = float2{top, sum};
+            }
         }
     }
 }
@@ -578,9 +561,10 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_chunk_join_kernel(ChunkArgs a
             for (int e = 0; e < E; ++e) x[e] += g * a.partial[(at0 + s * step) * D + 64 * e + lane];
         }
         const int place = tile * places + v;
+        const float f1 = chunk_factor(sum, top);
         T* to = (T*)a.out + ((int64_t)(p.r.start + place / G) * a.Hq + head * G + place % G) * D;
 #pragma unroll
-        for (int e = 0; e < E; ++e) store_as(to + 64 * e + lane, kv8_quotient(x[e], sum, top));
+        for (int e = 0; e < E; ++e) store_as(to + 64 * e + lane, x[e] * f1);
     }
 }
 
