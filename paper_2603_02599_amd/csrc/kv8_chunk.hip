@@ -23,7 +23,7 @@ constexpr int kWaves = 4;
 constexpr float kHead = 6.f;         // powers of two
 constexpr int kMinSplit = 256;       // tokens of a part at least
 constexpr int kMaxSplits = 64;
-constexpr int kGroupsWanted = 1024;  // workgroups that parts are made for
+constexpr int kGroupsWanted = 512;   // workgroups that parts are made for
 
 struct ChunkArgs {
     const uint8_t *codes, *scales;
@@ -229,31 +229,41 @@ struct Places {
         had = 0;
     }
 
-    // The block of tokens at .. at + 31.  whole: every place of the wave sees all of them, and nothing has been taken out of it
-    __device__ __forceinline__ void step(const ChunkArgs& a, const uint8_t* block, int at, bool whole) {
-        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
-        const Notes& notes = Block<D>::notes(block, h);
+    // A block's keys on their way into operands
+    struct Keys {
+        u32x4_s codes[KS / 2];
+        float scale;
+        __device__ __forceinline__ void read(const uint8_t* block) {
+            const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+            scale = Block<D>::notes(block, token >> 4).powers[16 + (token & 15)];
+#pragma unroll
+            for (int w = 0; w < KS / 2; ++w) codes[w] = *reinterpret_cast<const u32x4_s*>(block + token * D + ((2 * w + h) ^ Block<D>::key(token)) * 16);
+        }
+    };
+    __device__ __forceinline__ void scores(const Keys& k, int i, f32x16& out) const {   // one step of 16 dims
+        const bf16x8 x = codes_to_bf16(k.codes[i >> 1][2 * (i & 1)], k.codes[i >> 1][2 * (i & 1) + 1], k.scale);
+#pragma unroll
+        for (int p = 0; p < P; ++p) out = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][i], out, 0, 0, 0);
+    }
+    __device__ __forceinline__ f32x16 scores(const uint8_t* block) const {
+        Keys k;
+        k.read(block);
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
-        {
-            const int token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
-            const float scale = Block<D>::notes(block, token >> 4).powers[16 + (token & 15)];
-            auto read = [&](int w) { return *reinterpret_cast<const u32x4_s*>(block + token * D + ((2 * w + h) ^ Block<D>::key(token)) * 16); };
-            u32x4_s next = read(0);
 #pragma unroll
-            for (int w = 0; w < KS / 2; ++w) {
-                const u32x4_s codes = next;
-                if (w + 1 < KS / 2) next = read(w + 1);
-                __builtin_amdgcn_sched_barrier(0);   // codes are converted where they are used: all at once they take the registers
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bf16x8 x = codes_to_bf16(codes[2 * u], codes[2 * u + 1], scale);
-#pragma unroll
-                    for (int p = 0; p < P; ++p) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][2 * w + u], s, 0, 0, 0);
-                }
-            }
-        }
+        for (int i = 0; i < KS; ++i) scores(k, i, s);
+        return s;
+    }
+
+    // Scores s of the block of tokens at .. at + 31 into weights and the output; meanwhile, NEXT, the scores s2 of the block behind, products and weights in
+    // turn.  whole: every place of the wave sees all of the tokens, and nothing has been taken out
+    template <bool NEXT>
+    __device__ __forceinline__ void step(const ChunkArgs& a, f32x16& s, const uint8_t* block, int at, bool whole, const uint8_t* behind, f32x16& s2) {
+        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+        const Notes& notes = Block<D>::notes(block, h);
+        Keys k;
+        if constexpr (NEXT) k.read(behind);
         uint32_t live = 0xffff;   // tokens that the lane's place sees
         if (!whole) {
             const int mine = at + 16 * h, from = max(lo - mine, 0), to = min(hi - mine, 15);
@@ -286,8 +296,14 @@ struct Places {
         u32x4_s codes[NB];
         u32x4_s words[P][2];
         f32x4 vs;
+        if constexpr (NEXT) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s2[i] = 0.f;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            if constexpr (NEXT)
+                if (j % (8 / KS) == 0) scores(k, j / (8 / KS), s2);
             if (j % 2 == 0) vs = *reinterpret_cast<const f32x4*>(notes.powers + 2 * j);
             float x[2];
 #pragma unroll
@@ -372,9 +388,9 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    // positions from all_from to low are seen by all of the wave's places, from any_from to high by any
+    // positions from all_from to low are seen by all of the wave's places
     const int base = p.r.n - p.r.count, low = base + v0 / G, high = base + (min(v0 + 32, live) - 1) / G;
-    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0, any_from = a.window > 0 ? max(low - a.window + 1, 0) : 0;
+    const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
     // and the tile's positions from tile_from to tile_to by all of its places
     const int tile_to = base + tile * kTile / G, tile_from = a.window > 0 ? max(base + (min((tile + 1) * kTile, live) - 1) / G - a.window + 1, 0) : 0;
     Places<T, D> w;
@@ -392,24 +408,34 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     };
 #pragma unroll
     for (int s = 0; s < ST - 1; ++s) request();
-    const bool on = v0 < live;
-    int at = 0;
-    for (int token = range.begin; token < range.end; token += 64) {
-        // The step has landed for every wave, and all are done with the one before, whose place is filled again
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 2)) : "memory");
-        pages.note(lds + at * STAGE + (wave >> 1) * Block<D>::BYTES, wave & 1, ST - 2, token + 16 * wave, p.r.n, token < tile_from || token + 63 > tile_to);
+    auto note = [&](int stage, int ago, int token) {
+        pages.note(lds + stage * STAGE + (wave >> 1) * Block<D>::BYTES, wave & 1, ago, token + 16 * wave, p.r.n, token < tile_from || token + 63 > tile_to);
+    };
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 2)) : "memory");
+    note(0, ST - 2, range.begin);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // The next step has landed for every wave, and all are done with the one before this, whose place is filled again
+    auto turn = [&](int next, int token) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 3)) : "memory");
+        note(next, ST - 3, token);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         request();
-        if (on) {
-#pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                const int from = token + 32 * half;
-                const uint8_t* block = lds + at * STAGE + half * Block<D>::BYTES;
-                if (from > high || from + 31 < any_from) continue;
-                w.step(a, block, from, from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()));
-            }
+    };
+    auto after = [&](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
+    int at = 0;
+    if (v0 < live) {
+        auto whole = [&](const uint8_t* block, int from) { return from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()); };
+        f32x16 s = w.scores(lds), s2;
+        for (int token = range.begin; token < range.end; token += 64) {
+            const int next = after(at);
+            const uint8_t *first = lds + at * STAGE, *second = first + Block<D>::BYTES;
+            w.template step<true>(a, s, first, token, whole(first, token), second, s2);
+            turn(next, token + 64);
+            w.template step<true>(a, s2, second, token + 32, whole(second, token + 32), lds + next * STAGE, s);
+            at = next;
         }
-        if (++at == ST) at = 0;
+    } else {   // requests for the others
+        for (int token = range.begin; token < range.end; token += 64) turn(at = after(at), token + 64);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     w.close();
@@ -472,7 +498,8 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
         pages.note(block, 0, 1, from, p.r.n, partly);
         pages.note(block, 1, 0, from + kPageTokens, p.r.n, partly);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        w.step(a, block, from, !partly && __all(Block<D>::notes(block, h).plain()));
+        f32x16 s = w.scores(block), none;
+        w.template step<false>(a, s, block, from, !partly && __all(Block<D>::notes(block, h).plain()), nullptr, none);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     w.close();
