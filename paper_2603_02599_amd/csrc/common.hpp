@@ -150,6 +150,13 @@ __device__ __forceinline__ u32x4_s load_stream(const u32x4_s* p) { return __buil
 __device__ __forceinline__ void lds_dma16(const void* base, uint32_t lane_bytes, uint32_t lds_byte) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_byte), "v"(lane_bytes), "s"(base) : "memory", "m0");
 }
+// N of them, each 1 KiB behind the one before in memory and in LDS: the instruction's offset counts for both.
+template <int N>
+__device__ __forceinline__ void lds_dma16(const void* base, uint32_t lane_bytes, uint32_t lds_byte) {
+    static_assert(N == 1 || N == 2, "");
+    if constexpr (N == 1) lds_dma16(base, lane_bytes, lds_byte);
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024" ::"s"(lds_byte), "v"(lane_bytes), "s"(base) : "memory", "m0");
+}
 // The same with 4 bytes a lane: lane i's land at lds_byte + 4 i.
 __device__ __forceinline__ void lds_dma4(const void* base, uint32_t lane_bytes, uint32_t lds_byte) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte), "v"(lane_bytes), "s"(base) : "memory", "m0");

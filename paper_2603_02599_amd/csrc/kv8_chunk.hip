@@ -146,15 +146,16 @@ struct PageRequests {
         there = 0;
     }
     __device__ __forceinline__ void request(int page, int half, uint32_t block) {
-        const bool on = (unsigned)page < (unsigned)n_pages;
-        there = there << 1 | (on ? 1u : 0u);
-        const uint8_t* k = on ? codes + page * k_page : (const uint8_t*)g_no_page;
-        const uint8_t* v = on ? codes + v_off + page * v_page : (const uint8_t*)g_no_page;
-        const uint8_t* s = on ? scales + page * s_page : (const uint8_t*)g_no_page;
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) lds_dma16(k + j * 1024, half ? k_lane[1] : k_lane[0], block + half * 16 * D + j * 1024);
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) lds_dma16(v + j * 1024, v_lane, block + Block<D>::V + half * 16 * D + j * 1024);
+        const uint8_t *k = (const uint8_t*)g_no_page, *v = k, *s = k;
+        there <<= 1;
+        if ((unsigned)page < (unsigned)n_pages) {
+            k = codes + (uint64_t)(uint32_t)page * (uint32_t)k_page;   // a page of a layer is less than 2^32 bytes
+            v = k + v_off;
+            s = scales + (uint64_t)(uint32_t)page * (uint32_t)s_page;
+            there |= 1;
+        }
+        lds_dma16<D / 64>(k, half ? k_lane[1] : k_lane[0], block + half * 16 * D);
+        lds_dma16<D / 64>(v, v_lane, block + Block<D>::V + half * 16 * D);
         lds_dma4(s, s_lane, block + Block<D>::S + half * 256);
     }
     // Notes of a page that has landed, requested `ago` pages ago, whose first token is `at`.  Powers and values from token n on, which nobody has written, become zeros; where some places see
@@ -382,7 +383,8 @@ __device__ __forceinline__ ChunkRange chunk_range(const ChunkArgs& a, const Chun
 // Four waves of 32 places each over the same tokens, 64 a step: wave w requests the step's page w.
 template <class T, int D>
 __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace& p, int head, int tile, int split, int64_t slot, uint8_t* lds) {
-    constexpr int ST = kWideStages, STAGE = 2 * Block<D>::BYTES, OPS = Block<D>::OPS;
+    static_assert(kWideStages == 4, "");
+    constexpr int STAGE = 2 * Block<D>::BYTES, OPS = Block<D>::OPS;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hkv, v0 = tile * kTile + 32 * wave, live = p.r.count * G;
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
@@ -404,38 +406,45 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
         pages.request(page, wave & 1, lds0 + fill * STAGE + (wave >> 1) * Block<D>::BYTES);
         ahead += 64;
         page = page_at(ahead);
-        if (++fill == ST) fill = 0;
+        fill = fill + 1 & 3;
     };
 #pragma unroll
-    for (int s = 0; s < ST - 1; ++s) request();
+    for (int s = 0; s < 3; ++s) request();
     auto note = [&](int stage, int ago, int token) {
         pages.note(lds + stage * STAGE + (wave >> 1) * Block<D>::BYTES, wave & 1, ago, token + 16 * wave, p.r.n, token < tile_from || token + 63 > tile_to);
     };
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 2)) : "memory");
-    note(0, ST - 2, range.begin);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
+    note(0, 2, range.begin);
+    note(1, 1, range.begin + 64);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    // The next step has landed for every wave, and all are done with the one before this, whose place is filled again
-    auto turn = [&](int next, int token) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS * (ST - 3)) : "memory");
-        note(next, ST - 3, token);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        request();
-    };
-    auto after = [&](int stage) { return stage + 1 == ST ? 0 : stage + 1; };
+    // A step: the one three behind it is requested in the place of the one before it, with which all are done, the one two behind it has landed and is noted, the next one's
+    // first scores are computed.
     int at = 0;
+    auto before = [&]() {
+        request();
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
+    };
+    auto turn = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        at = at + 1 & 3;
+    };
     if (v0 < live) {
         auto whole = [&](const uint8_t* block, int from) { return from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()); };
         f32x16 s = w.scores(lds), s2;
         for (int token = range.begin; token < range.end; token += 64) {
-            const int next = after(at);
             const uint8_t *first = lds + at * STAGE, *second = first + Block<D>::BYTES;
+            before();
             w.template step<true>(a, s, first, token, whole(first, token), second, s2);
-            turn(next, token + 64);
-            w.template step<true>(a, s2, second, token + 32, whole(second, token + 32), lds + next * STAGE, s);
-            at = next;
+            note(at + 2 & 3, 1, token + 128);
+            w.template step<true>(a, s2, second, token + 32, whole(second, token + 32), lds + (at + 1 & 3) * STAGE, s);
+            turn();
         }
     } else {   // requests for the others
-        for (int token = range.begin; token < range.end; token += 64) turn(at = after(at), token + 64);
+        for (int token = range.begin; token < range.end; token += 64) {
+            before();
+            note(at + 2 & 3, 1, token + 128);
+            turn();
+        }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     w.close();
