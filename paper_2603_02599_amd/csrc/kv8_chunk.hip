@@ -53,6 +53,19 @@ __device__ __forceinline__ ChunkRequest chunk_request(const ChunkArgs& a, int b)
     return r;
 }
 
+// Sums over the lanes up to each
+__device__ __forceinline__ int lanes_before(int v) {
+    const auto moved = [](int x, auto ctrl, auto rows) { return __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };   // 0 where nothing moves to
+    typedef std::integral_constant<int, 0xf> All;
+    v += moved(v, std::integral_constant<int, 0x111>{}, All{});   // from 1, 2, 4 and 8 lanes before, within rows of sixteen
+    v += moved(v, std::integral_constant<int, 0x112>{}, All{});
+    v += moved(v, std::integral_constant<int, 0x114>{}, All{});
+    v += moved(v, std::integral_constant<int, 0x118>{}, All{});
+    v += moved(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // a row's last lane to the row behind it
+    v += moved(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // lane 31 to the upper half
+    return v;
+}
+
 struct ChunkPlace {
     ChunkRequest r;
     int b, index;           // request (-1: behind the last), and which of its items or tiles
@@ -67,11 +80,8 @@ __device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, int index) 
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
         const ChunkRequest r = chunk_request(a, b0 + lane);
         int t = r.tiles, s = r.tiles * r.splits;
-#pragma unroll
-        for (int o = 1; o < 64; o *= 2) {
-            const int x = __shfl_up(t, o), y = __shfl_up(s, o);
-            if (lane >= o) t += x, s += y;
-        }
+        t = lanes_before(t);
+        s = lanes_before(s);
         const long long mine = TILES ? (long long)tiles + t : items + s;
         const uint64_t past = __ballot(mine > index);
         if (past) {
@@ -257,11 +267,39 @@ struct Places {
         return s;
     }
 
+    // The output's products with a block's values: two of 32 dims.  Nothing but the matrix cores is short here, so they go first: the other wave of the SIMD has vector work to do
+    // meanwhile (2048 of 8191 tokens 292 -> 284 us).
+    typedef u32x4_s Weights[P][2];
+    __device__ __forceinline__ u32x4_s values(const uint8_t* block, int j) const {
+        const int lane = threadIdx.x & 63;
+        return *reinterpret_cast<const u32x4_s*>(block + Block<D>::V + (lane >> 5) * 16 * D + (32 * j + (lane & 31)) * 16);
+    }
+    __device__ __forceinline__ void add(const u32x4_s& codes, const Weights& w, int j, int u) {
+        const bf16x8 x = codes_to_bf16(codes[2 * u], codes[2 * u + 1]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, w[p][u]), o[j], 0, 0, 0);
+    }
+    __device__ __forceinline__ void add(const uint8_t* block, const Weights& w) {
+        u32x4_s codes = values(block, 0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const u32x4_s now = codes;
+            if (j + 1 < NB) codes = values(block, j + 1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                __builtin_amdgcn_sched_barrier(0);
+                add(now, w, j, u);
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+    }
+
     // Scores s of the block of tokens at .. at + 31 into weights and the output; meanwhile, NEXT, the scores s2 of the block behind, products and weights in
     // turn.  whole: every place of the wave sees all of the tokens, and nothing has been taken out
     template <bool NEXT>
     __device__ __forceinline__ void step(const ChunkArgs& a, f32x16& s, const uint8_t* block, int at, bool whole, const uint8_t* behind, f32x16& s2) {
-        const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+        const int h = (threadIdx.x & 63) >> 5;
         const Notes& notes = Block<D>::notes(block, h);
         Keys k;
         if constexpr (NEXT) k.read(behind);
@@ -293,9 +331,7 @@ struct Places {
                 for (int i = 0; i < 16; ++i) o[j][i] *= f;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        const uint8_t* v = block + Block<D>::V + h * 16 * D + c * 16;
-        u32x4_s codes[NB];
-        u32x4_s words[P][2];
+        Weights words;
         f32x4 vs;
         if constexpr (NEXT) {
 #pragma unroll
@@ -303,9 +339,9 @@ struct Places {
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+            if (j % 2 == 0) vs = *reinterpret_cast<const f32x4*>(notes.powers + 2 * j);
             if constexpr (NEXT)
                 if (j % (8 / KS) == 0) scores(k, j / (8 / KS), s2);
-            if (j % 2 == 0) vs = *reinterpret_cast<const f32x4*>(notes.powers + 2 * j);
             float x[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * j + e], a.c, -ref));
@@ -318,19 +354,10 @@ struct Places {
                 words[1][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
                 words[2][j >> 2][j & 3] = pack_bf16(x[0] - bf16_lo(words[1][j >> 2][j & 3]), x[1] - bf16_hi(words[1][j >> 2][j & 3]));
             }
-            if (j >= 8 - NB) codes[j - 8 + NB] = *reinterpret_cast<const u32x4_s*>(v + (j - 8 + NB) * 512);
             __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("" : "+v"(l));   // summed here: left to itself the compiler sums later, all in a row
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                __builtin_amdgcn_sched_barrier(0);
-                const bf16x8 x = codes_to_bf16(codes[j][2 * u], codes[j][2 * u + 1]);
-#pragma unroll
-                for (int p = 0; p < P; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, words[p][u]), o[j], 0, 0, 0);
-            }
+        add(block, words);
     }
 
     // Not-a-numbers among a block's values into the output of the places that see them
@@ -408,42 +435,38 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
         page = page_at(ahead);
         fill = fill + 1 & 3;
     };
-#pragma unroll
-    for (int s = 0; s < 3; ++s) request();
     auto note = [&](int stage, int ago, int token) {
         pages.note(lds + stage * STAGE + (wave >> 1) * Block<D>::BYTES, wave & 1, ago, token + 16 * wave, p.r.n, token < tile_from || token + 63 > tile_to);
     };
+    request();
+    request();
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
-    note(0, 2, range.begin);
-    note(1, 1, range.begin + 64);
+    note(0, 1, range.begin);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    // A step: the one three behind it is requested in the place of the one before it, with which all are done, the one two behind it has landed and is noted, the next one's
-    // first scores are computed.
+    // A step: the one two behind it is requested in the place of the one two before it, with which all are done.  Between its blocks the next one has landed and is
+    // noted, for all waves, and its first scores are computed with the second block.
     int at = 0;
-    auto before = [&]() {
-        request();
+    auto turn = [&](int token) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
-    };
-    auto turn = [&]() {
+        note(at + 1 & 3, 1, token + 64);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        at = at + 1 & 3;
     };
     if (v0 < live) {
         auto whole = [&](const uint8_t* block, int from) { return from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()); };
         f32x16 s = w.scores(lds), s2;
         for (int token = range.begin; token < range.end; token += 64) {
             const uint8_t *first = lds + at * STAGE, *second = first + Block<D>::BYTES;
-            before();
+            request();
             w.template step<true>(a, s, first, token, whole(first, token), second, s2);
-            note(at + 2 & 3, 1, token + 128);
-            w.template step<true>(a, s2, second, token + 32, whole(second, token + 32), lds + (at + 1 & 3) * STAGE, s);
-            turn();
+            turn(token);
+            at = at + 1 & 3;
+            w.template step<true>(a, s2, second, token + 32, whole(second, token + 32), lds + at * STAGE, s);
         }
     } else {   // requests for the others
         for (int token = range.begin; token < range.end; token += 64) {
-            before();
-            note(at + 2 & 3, 1, token + 128);
-            turn();
+            request();
+            turn(token);
+            at = at + 1 & 3;
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -571,36 +594,35 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) 
     }
 }
 
-// out = sum over a tile's parts, a wave a place at a time
+// out = sum over a tile's parts, four dims a lane; its places are dealt to gridDim.y workgroups
 template <class T, int D>
-__global__ __launch_bounds__(64 * kWaves) void kv8_chunk_join_kernel(ChunkArgs a) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.Hq / a.Hkv;
-    const int head = blockIdx.x % a.Hkv;
+__global__ __launch_bounds__(256) void kv8_chunk_join_kernel(ChunkArgs a) {
+    const int G = a.Hq / a.Hkv, head = blockIdx.x % a.Hkv;
     const ChunkPlace p = chunk_find<true>(a, blockIdx.x / a.Hkv);
     if (p.b < 0 || p.r.splits == 1) return;
     const int tile = p.index, places = p.r.count * G <= kFew ? kFew : kTile, live = min(p.r.count * G - tile * places, places);
     const int64_t slot = (p.items + (int64_t)tile * p.r.splits) * a.Hkv + head;
     if (slot + (int64_t)(p.r.splits - 1) * a.Hkv >= a.slots) return;
     const float2* ml = reinterpret_cast<const float2*>(a.partial + a.slots * a.slot_rows * D);
-    constexpr int E = D / 64;
-    for (int v = blockIdx.y * kWaves + wave; v < live; v += kWaves * gridDim.y) {
-        const int64_t at0 = slot * a.slot_rows + v, step = (int64_t)a.Hkv * a.slot_rows;
-        const float2 mine = lane < p.r.splits ? ml[at0 + lane * step] : float2{-INFINITY, 0.f};
-        const float top = wave_max(mine.x), ref = top == -INFINITY ? 0.f : top;
-        const float f = __builtin_amdgcn_exp2f(mine.x - ref), sum = wave_sum(f * mine.y);
-        float x[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = 0.f;
+    constexpr int LANES = D / 4;   // of a place
+    const int64_t step = (int64_t)a.Hkv * a.slot_rows;
+    for (int i = blockIdx.y * (256 / LANES) + threadIdx.x / LANES; i < live; i += gridDim.y * (256 / LANES)) {
+        const int64_t at0 = slot * a.slot_rows + i;
+        const int d = threadIdx.x % LANES * 4;
+        float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
         for (int s = 0; s < p.r.splits; ++s) {
-            const float g = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), s));
+            const float2 y = ml[at0 + s * step];
+            const f32x4 o = *reinterpret_cast<const f32x4*>(a.partial + (at0 + s * step) * D + d);
+            const float grown = fmaxf(top, y.x), ref = grown == -INFINITY ? 0.f : grown;
+            const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(y.x - ref);
+            top = grown;
+            sum = sum * f + y.y * g;
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] += g * a.partial[(at0 + s * step) * D + 64 * e + lane];
+            for (int e = 0; e < 4; ++e) x[e] = x[e] * f + o[e] * g;
         }
-        const int place = tile * places + v;
-        const float f1 = chunk_factor(sum, top);
-        T* to = (T*)a.out + ((int64_t)(p.r.start + place / G) * a.Hq + head * G + place % G) * D;
-#pragma unroll
-        for (int e = 0; e < E; ++e) store_as(to + 64 * e + lane, x[e] * f1);
+        const int v = tile * places + i;
+        const float f = chunk_factor(sum, top);
+        store4((T*)a.out + ((int64_t)(p.r.start + v / G) * a.Hq + head * G + v % G) * D + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
     }
 }
 
@@ -637,7 +659,7 @@ static hipError_t chunk_attend(const ChunkArgs& a, int64_t tiles, hipStream_t st
     const unsigned grid = (unsigned)(std::min<int64_t>(items, std::max<int64_t>(8192 / a.Hkv, 1)) * a.Hkv);
     hipLaunchKernelGGL((kv8_chunk_kernel<T, D>), dim3(grid), dim3(64 * kWaves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)(a.slot_rows / 8)), dim3(64 * kWaves), 0, st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)(a.slot_rows / 32)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
