@@ -595,7 +595,7 @@ size_t sun_kv8_chunk_attention_workspace_bytes(const sun_model_cfg* cfg, int bat
  * Cached numbers enter exactly (a key's product with its power of two as a bf16 number); weights of the softmax carry 8 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
  * Under SUN_VALIDATE row starts, counts and tables are copied to the host (synchronises) and checked.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, batch outside [1, 1024], rows < 1, max_pages outside [1, 2^26], window < 0, dtype, q or out not
- * 16-byte aligned, q the same as out, more rows than one launch takes: 2^24 are taken for up to 32 query heads), SUN_ERR_WORKSPACE (too small or not 256-byte aligned);
+ * 16-byte aligned, q the same as out, more rows than one launch takes: 2^23 are taken for up to 32 query heads), SUN_ERR_WORKSPACE (too small or not 256-byte aligned);
  * under SUN_VALIDATE also SUN_ERR_SEQ_LEN (row starts that fall or lie outside [0, rows], more rows than positions, counts) and SUN_ERR_PAGE_RANGE.
  */
 int sun_kv8_chunk_attention(const sun_kv8_pool* pool, int layer, int batch, int rows, int dtype, const void* q, const int32_t* row_starts,

@@ -8,7 +8,7 @@ import torch
 
 import lowbit_ref as R
 from paper_2603_02599_amd import binding as sun
-from test_gpu_kv8 import DEV, DT, HEADS, Cache, host, i32, make_shape
+from test_gpu_kv8 import DEV, DT, HEADS, Cache, host, i32, make_shape, two_tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -206,3 +206,315 @@ def test_long_caches_in_parts(hq, hkv, d, counts, lens, dtype):
     cache.fill(0, lens)
     check(cache, 0, counts, lens, dtype)
     check(cache, 0, counts, lens, dtype, window=2500)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_other_requests_hold_does_not_matter(dtype):
+    lens, counts = [500, 20, 3000, 64, 700], [40, 3, 2, 64, 1]
+    cache = Cache(make_shape(8, 2, 128), lens)
+    cache.fill(0, lens)
+    starts = starts_of(counts)
+    q = queries(cache.shape, int(starts[-1]), dtype)
+    a = attend(cache, 0, q, starts, lens)
+    assert torch.equal(a, attend(cache, 0, q, starts, lens))
+    b = attend(cache, 0, q, starts, [500, 3, 2, 64, 1])
+    for r in (0, 3):
+        assert torch.equal(a[starts[r]:starts[r + 1]], b[starts[r]:starts[r + 1]])
+    # another order of the same requests
+    order = [2, 3, 0, 4, 1]
+    moved = torch.cat([q[starts[r]:starts[r + 1]] for r in order])
+    c = attend(cache, 0, moved, starts_of([counts[r] for r in order]), [lens[r] for r in order], table=cache.dev_table[order].contiguous())
+    assert torch.equal(c, torch.cat([a[starts[r]:starts[r + 1]] for r in order]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_requests_and_room_for_far_more(dtype):
+    """1024 requests, and tables far wider than the caches are long."""
+    rng = np.random.default_rng(4)
+    lens = rng.integers(1, 40, 1024).tolist()
+    counts = [int(min(n, rng.integers(0, 4))) for n in lens]
+    counts[700] = lens[700]
+    cache = Cache(make_shape(4, 2, 64), lens)
+    cache.fill(0, lens)
+    check(cache, 0, counts, lens, dtype, pad=1)
+    cache = Cache(make_shape(8, 1, 128), [700, 90], extra_cols=60000)
+    cache.fill(0, [700, 90])
+    check(cache, 0, [3, 90], [700, 90], dtype)
+    check(cache, 0, [300, 1], [700, 90], dtype, window=200)
+
+
+def test_row_starts_that_are_none_stay_inside():
+    """Falling, negative and too large ones: rows outside what the arrays hold are neither read nor written, and the other requests are right."""
+    lens, counts = [50, 300, 40, 17], [5, 40, 3, 2]
+    cache = Cache(make_shape(8, 2, 128), lens)
+    cache.fill(0, lens)
+    starts = starts_of(counts)
+    q = queries(cache.shape, 50, "bf16")
+    good = attend(cache, 0, q, starts, lens)
+    room = torch.full((60, q.shape[1]), 33.0, device=DEV, dtype=torch.bfloat16)
+    for bad in ([0, 5, 45, 48, 2 ** 31 - 1], [-7, 5, 45, 48, 50], [0, 5, 45, 20, 10], [50, 0, 50, 0, 50], [60, 70, 80, 90, 100]):
+        room.fill_(33.0)
+        attend(cache, 0, q, bad, lens, out=room[:50])
+        assert (room[50:] == 33).all()
+        if bad[:3] == [0, 5, 45]:
+            assert torch.equal(room[:45], good[:45])
+
+
+def test_checks_of_device_arrays():
+    cache = Cache(make_shape(4, 2, 64), [40, 40])
+    cache.fill(0, [40, 40])
+    q = queries(cache.shape, 10, "f32")
+    for starts, n, window, status in (([0, 5, 11], [40, 40], 0, 6), ([0, 5, 4], [40, 40], 0, 6), ([-1, 5, 10], [40, 40], 0, 6), ([0, 5, 10], [4, 40], 0, 6), ([0, 5, 10], [40, -1], 0, 6),
+                                      ([0, 5, 10], [40, 100], 0, 6), ([0, 5, 10], [40, 50], 0, 5), ([0, 1, 2], [50, 40], 2, 5)):
+        with pytest.raises(sun.SunError) as e:
+            attend(cache, 0, q, starts, n, window, flags=sun.SUN_VALIDATE)
+        assert e.value.status == status, (starts, n)
+    cache.table[:, 0] = -1   # in front of what a window lets them see
+    cache.dev_table = i32(cache.table)
+    attend(cache, 0, q, [0, 5, 10], [40, 40], 16, flags=sun.SUN_VALIDATE)
+    cache.table[1, :] = -1
+    cache.dev_table = i32(cache.table)
+    attend(cache, 0, q, [0, 5, 5], [40, 40], 16, flags=sun.SUN_VALIDATE)   # a request without new rows reads nothing
+
+
+def test_binding_refuses_other_shapes_types_and_devices():
+    cache = Cache(make_shape(4, 2, 64), [40, 40])
+    cache.fill(0, [40, 40])
+    q, at = torch.zeros(5, 256, device=DEV), i32([40, 40])
+    ws = torch.zeros(sun.sun_kv8_chunk_attention_workspace_bytes(cache.cfg, 2, 5, cache.table.shape[1]), dtype=torch.uint8, device=DEV)
+    ok = dict(q=q, row_starts=i32([0, 2, 5]), page_tables=cache.dev_table, n_tokens=at, out=q.clone(), workspace=ws)
+    sun.sun_kv8_chunk_attention(cache.pool, 0, **ok)
+    for change in (dict(q=q.bfloat16()), dict(q=q.half(), out=q.half()), dict(out=q.bfloat16()), dict(out=q[:4]), dict(out=q), dict(n_tokens=at.long()), dict(n_tokens=i32([1])), dict(row_starts=i32([0, 5])),
+                   dict(row_starts=i32([0, 2, 5]).long()), dict(page_tables=cache.dev_table[:1]), dict(page_tables=cache.dev_table[0]), dict(q=torch.zeros(5, 512, device=DEV)[:, ::2]),
+                   dict(q=q[0]), dict(workspace=ws.cpu()), dict(q=q.cpu()), dict(window=1 << 31), dict(window=-1)):
+        with pytest.raises(sun.SunError) as e:
+            sun.sun_kv8_chunk_attention(cache.pool, 0, **{**ok, **change})
+        assert e.value.status == 2, change
+
+
+def attend_two_tokens(cache, q):
+    """A chunk of both tokens of every request: the last rows, which see both."""
+    batch, hq, d = q.shape
+    rows = torch.from_numpy(np.repeat(q.reshape(batch, -1), 2, 0)).to(DEV)
+    out = attend(cache, 0, rows, starts_of([2] * batch), [2] * batch)
+    return host(out).reshape(batch, 2, hq, d)[:, 1]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_32_bit_queries_and_weights_carry_24_bits(d):
+    """Scores that are what the last 8 of a query's 24 bits leave, and values that cancel but for what the weights' last bits leave."""
+    q_a, q_b = R.close_queries(12, 8)
+    places = [(0, d - 1), (5, 6), (33, 2), (d // 2, 1), (31, 32), (17, 16)] * 2
+    q = np.zeros((12, 8, d), np.float32)
+    for r, (a, b) in enumerate(places):
+        q[r, :, a], q[r, :, b] = q_a[r], q_b[r]
+    cache = two_tokens([[(0, a, 0x38), (0, b, 0xb8)] for a, b in places], (0x38, 0), d, 8, 12)
+    ref, off = R.close_queries_out(q_a, q_b, d)
+    assert (np.abs(attend_two_tokens(cache, q) - ref[..., None]) <= off[..., None]).all()
+    gaps = R.close_gaps(12, 8, d)
+    q = np.zeros((12, 8, d), np.float32)
+    for r in range(12):
+        q[r, :, 3 * r] = gaps[r]
+    cache = two_tokens([[(1, 3 * r, 0xb8)] for r in range(12)], (0x38, 0xb8), d, 8, 12)
+    ref, off = R.close_gaps_out(gaps, d)
+    assert (np.abs(attend_two_tokens(cache, q) - ref[..., None]) <= off[..., None]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pages_beyond_32_bit_offsets(dtype):
+    """Pages at the end of a pool of more than 2^32 bytes a layer: the same results as in a small pool."""
+    shape = make_shape(16, 8, 128)
+    small = Cache(shape, [40, 900], poison=False)
+    small.fill(1, [40, 900])
+    n_pages = (9 << 30) // 2 // sun.sun_kv8_pool_bytes(small.cfg, 1) * 2 + 7
+    mem = torch.zeros(sun.sun_kv8_pool_bytes(small.cfg, n_pages), dtype=torch.uint8, device=DEV)
+    pool = sun.sun_kv8_pool_create(small.cfg, mem)
+    lay, first = pool.layout(), n_pages - small.n_pages
+    assert lay.k_layer > 1 << 32 and lay.n_pages == n_pages
+    for off, layer, page, to_off, to_layer, to_page in ((lay.k_off, lay.k_layer, lay.k_page, small.lay.k_off, small.lay.k_layer, small.lay.k_page),
+                                                       (lay.ks_off, lay.s_layer, lay.s_page, small.lay.ks_off, small.lay.s_layer, small.lay.s_page)):
+        mem[off + layer + first * page:][:small.n_pages * page].copy_(small.mem[to_off + to_layer:][:small.n_pages * to_page])
+    q = queries(shape, 240, dtype)
+    outs = []
+    for p, table in ((small.pool, small.dev_table), (pool, torch.where(small.dev_table >= 0, small.dev_table + first, small.dev_table))):
+        out = torch.zeros_like(q)
+        ws = torch.zeros(sun.sun_kv8_chunk_attention_workspace_bytes(small.cfg, 2, 240, table.shape[1]), dtype=torch.uint8, device=DEV)
+        sun.sun_kv8_chunk_attention(p, 1, q, i32([0, 10, 240]), table, i32([40, 900]), out, ws)
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs) and outs[0].abs().max() > 0
+
+
+# ------------------------------------------------------------------ together
+
+class Layer:
+    """A layer over chunks of new tokens, as a caller that runs it itself puts it together: projection, append, chunk attention, output projection onto the residual
+    stream, gated pair, down projection onto the residual stream."""
+
+    def __init__(self, lens, counts, dtype, hidden=256, ffn=352, hq=8, hkv=2, d=64, seed=0, pad=2):
+        self.cache = Cache(make_shape(hq, hkv, d, qk_norm=True), [n + c * 4 for n, c in zip(lens, counts)])
+        self.cache.fill(0, lens)
+        self.hq, self.hkv, self.d, self.dtype, self.counts = hq, hkv, d, DT[dtype], counts
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        weights = lambda n, k: sun.sun_mx4_quantize(torch.randn(n, k, generator=g, device=DEV) * k ** -0.5)
+        self.wqkv, self.wo, self.gate, self.up, self.down = weights((hq + 2 * hkv) * d, hidden), weights(hidden, hq * d), weights(ffn, hidden), weights(ffn, hidden), weights(hidden, ffn)
+        self.bias = torch.randn(hidden, generator=g, device=DEV) * 0.1
+        self.gains = [(1 + 0.1 * torch.randn(d, generator=g, device=DEV)).to(self.dtype) for _ in range(2)]
+        rows = sum(counts) + pad
+        empty = lambda n, t=self.dtype: torch.zeros(rows, n, dtype=t, device=DEV)
+        self.x = torch.randn(rows, hidden, generator=g, device=DEV).to(self.dtype)
+        self.stream = torch.randn(rows, hidden, generator=g, device=DEV)      # 32 bits
+        self.starts, self.lens = i32(starts_of(counts)), i32(lens)
+        self.new = i32(counts)
+        self.req = i32(np.concatenate([np.repeat(np.arange(len(lens)), counts), np.zeros(pad, int)]))
+        self.step_of = i32(np.concatenate([*[np.arange(c) for c in counts], np.full(pad, -1 << 20)]))   # padding stays below 0
+        self.n, self.pos = i32(lens) * 0, self.req * 0
+        self.qkv, self.q, self.att, self.mid = empty((hq + 2 * hkv) * d), empty(hq * d), empty(hq * d), empty(ffn)
+        self.after_o, self.act = empty(hidden, torch.float32), empty(hidden)
+        width = self.cache.table.shape[1]
+        nbytes = max(sun.sun_mx4_linear_workspace_bytes(max(hidden, (hq + 2 * hkv) * d), max(hidden, ffn, hq * d), rows), sun.sun_mx4_gated_workspace_bytes(ffn, hidden, rows),
+                     sun.sun_mx4_linear_workspace_bytes(hidden, ffn, rows), sun.sun_mx4_linear_workspace_bytes(hidden, hq * d, rows),
+                     sun.sun_mx4_linear_workspace_bytes((hq + 2 * hkv) * d, hidden, rows), sun.sun_kv8_chunk_attention_workspace_bytes(self.cache.cfg, len(lens), rows, width))
+        self.ws = torch.zeros(nbytes, dtype=torch.uint8, device=DEV)
+
+    def run(self):
+        qd, kd = self.hq * self.d, self.hkv * self.d
+        torch.add(self.lens[self.req], self.step_of, out=self.pos)
+        torch.add(self.lens, self.new, out=self.n)
+        sun.sun_mx4_linear(*self.wqkv, self.x, self.qkv, self.ws)
+        q, k, v = self.qkv[:, :qd], self.qkv[:, qd:qd + kd], self.qkv[:, qd + kd:]
+        sun.sun_kv8_append(self.cache.pool, 0, q, k, v, self.pos, self.req, self.cache.dev_table, self.q, *self.gains)
+        sun.sun_kv8_chunk_attention(self.cache.pool, 0, self.q, self.starts, self.cache.dev_table, self.n, self.att, self.ws)
+        sun.sun_mx4_linear_fused(*self.wo, self.att, self.after_o, self.ws, residual=self.stream)
+        self.act.copy_(self.after_o)
+        sun.sun_mx4_gated(*self.gate, *self.up, self.act, self.mid, self.ws)
+        sun.sun_mx4_linear_fused(*self.down, self.mid, self.after_o, self.ws, bias=self.bias, residual=self.after_o)
+        self.lens.copy_(self.n)
+
+
+def product(w, x):
+    values = R.mx4_values(w[0].cpu().numpy(), w[1].cpu().numpy())
+    return x @ values.T, (3 * x.shape[1] + 8) * 2.0 ** -24 * (np.abs(x) @ np.abs(values).T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_layer_over_chunks(dtype):
+    """Every operator's result against the plain form of its own inputs, over three steps; padding rows go through the products alone."""
+    lens, counts = [0, 15, 500, 33], [40, 1, 4, 0]
+    b = Layer(lens, counts, dtype)
+    half = R.HALF[dtype]
+    for step in range(3):
+        stream = host(b.stream)
+        b.run()
+        torch.cuda.synchronize()
+        views = b.cache.views()
+        at = 0
+        for i, c in enumerate(counts):
+            n = lens[i] + c * (step + 1)
+            assert int(b.lens[i]) == n
+            if c:
+                q = host(b.q[at:at + c]).reshape(c, b.hq, b.d)
+                ref, mass, reach = reference(q, views, 0, b.cache.table[i], n, 0, b.cache.shape, b.cache.n_pages)
+                assert (np.abs(host(b.att[at:at + c]).reshape(q.shape) - ref) <= bound(ref, mass, reach, n, b.d, dtype)).all()
+            at += c
+        g, g_off = product(b.gate, host(b.act))
+        u, u_off = product(b.up, host(b.act))
+        a = g / (1 + np.exp(-g))
+        off = (1.13 * g_off + np.abs(a) * (6 * np.abs(g) + 8) * 2.0 ** -24) * (np.abs(u) + u_off) + np.abs(a) * u_off + np.abs(a * u) * (half * 1.01 + 2.0 ** -23)
+        assert (np.abs(host(b.mid) - a * u) <= off + 1e-37).all()
+        o, o_off = product(b.wo, host(b.att))
+        mid = stream + o   # what the stream was before the down projection, up to o's error
+        d, d_off = product(b.down, host(b.mid))
+        ref = mid + d + host(b.bias)
+        assert (np.abs(host(b.after_o) - ref) <= o_off + d_off + (np.abs(mid) + np.abs(d) + np.abs(ref) + 1) * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layer_in_a_graph(dtype):
+    """Captured and replayed with the program's own eager work between: every replay's bits are the eager run's."""
+    lens, counts = [0, 15, 500, 33], [40, 1, 4, 0]
+    eager, graphed = Layer(lens, counts, dtype), Layer(lens, counts, dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    start = (graphed.lens.clone(), graphed.cache.mem.clone())
+    with torch.cuda.stream(side):
+        graphed.run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.run()
+    graphed.lens.copy_(start[0])
+    graphed.cache.mem.copy_(start[1])
+    for step in range(3):
+        x = torch.randn_like(eager.x.float()).to(eager.x.dtype)
+        eager.x.copy_(x)
+        graphed.x.copy_(x)
+        eager.run()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in ((eager.after_o, graphed.after_o), (eager.att, graphed.att), (eager.mid, graphed.mid), (eager.cache.mem, graphed.cache.mem), (eager.lens, graphed.lens)):
+            assert torch.equal(a, b), step
+
+
+def test_layers_on_streams():
+    """On another stream than the current one, and two at once with workspaces of their own: what they give alone."""
+    setups = [([40, 700, 3], [5, 2, 1]), ([2000, 5], [70, 5])]
+    alone, together = ([Layer(*s, "bf16", seed=i) for i, s in enumerate(setups)] for _ in range(2))
+    for b in alone:
+        for _ in range(3):
+            b.run()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in setups]
+    for _ in range(3):
+        for b, s in zip(together, streams):
+            with torch.cuda.stream(s):
+                b.run()
+    torch.cuda.synchronize()
+    for a, b in zip(alone, together):
+        assert torch.equal(a.after_o, b.after_o) and torch.equal(a.att, b.att) and torch.equal(a.cache.mem, b.cache.mem)
+
+
+def test_calls_take_a_stream():
+    """stream= names the stream of a call: work queued in front of it there is seen."""
+    lens, counts = [3000, 90], [100, 90]
+    cache = Cache(make_shape(8, 2, 128), lens)
+    cache.fill(0, lens)
+    q = queries(cache.shape, 190, "bf16")
+    want = attend(cache, 0, q, starts_of(counts), lens)
+    side = torch.cuda.Stream()
+    late = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        late.copy_(q)
+    got = attend(cache, 0, late, starts_of(counts), lens, stream=side)
+    assert torch.equal(want, got)
+
+
+def test_two_graphs_share_a_workspace():
+    """Graphs replayed one behind the other on a stream may use the same workspace."""
+    lens, counts = [[5000, 90], [4000, 700, 3]], [[3, 2], [100, 2, 1]]
+    setups = []
+    for n, c in zip(lens, counts):
+        cache = Cache(make_shape(8, 2, 128), n)
+        cache.fill(0, n)
+        setups.append((cache, queries(cache.shape, sum(c), "bf16"), i32(starts_of(c)), i32(n)))
+    nbytes = max(sun.sun_kv8_chunk_attention_workspace_bytes(cache.cfg, len(n), q.shape[0], cache.table.shape[1]) for (cache, q, _, n) in setups)
+    ws = torch.full((nbytes,), 0xff, dtype=torch.uint8, device=DEV)
+    outs, graphs = [], []
+    for cache, q, starts, n in setups:
+        out = torch.zeros_like(q)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            sun.sun_kv8_chunk_attention(cache.pool, 0, q, starts, cache.dev_table, n, out, ws)
+        outs.append(out)
+        graphs.append(g)
+    for step in range(3):
+        for (cache, q, starts, n), seed in zip(setups, (5, 6)):
+            q.copy_(queries(cache.shape, q.shape[0], "bf16", seed + step))
+        want = [attend(cache, 0, q, host(starts), host(n)) for cache, q, starts, n in setups]
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs)), step
