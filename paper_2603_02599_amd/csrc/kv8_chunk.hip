@@ -124,7 +124,7 @@ __device__ __forceinline__ uint32_t not_a_number(uint32_t codes) { return ((code
 constexpr int kWideStages = 4;
 template <int D>
 struct ChunkLds {   // two workgroups on a compute unit
-    static constexpr int WIDE = kWideStages * 2 * Block<D>::BYTES, FEW = kWaves * Block<D>::BYTES, SUMS = kWaves * 32 * (D / 2 + 4) * 4 + kWaves * 32 * 8;
+    static constexpr int WIDE = kWideStages * 2 * Block<D>::BYTES, FEW = kWaves * 2 * Block<D>::BYTES, SUMS = kWaves * 32 * (D / 2 + 4) * 4 + kWaves * 32 * 8;
     static constexpr int BYTES = WIDE;
     static_assert(WIDE >= FEW && WIDE >= SUMS && 2 * WIDE <= 160 * 1024, "");
 };
@@ -505,30 +505,32 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
     const int G = a.Hq / a.Hkv, live = p.r.count * G;
     const ChunkRange range = chunk_range(a, p.r, 0, kFew, split, 32 * kWaves);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * Block<D>::BYTES;
-    uint8_t* const block = lds + wave * Block<D>::BYTES;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * 2 * Block<D>::BYTES;
     const int low = p.r.n - p.r.count, high = p.r.n - 1;
     const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
     Places<T, D> w;
-    w.load(a, p.r, head, c);
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
-    int ahead = range.begin + 32 * wave;
+    int ahead = range.begin + 32 * wave, fill = 0;
     int page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
     PageRequests<D> pages;
     pages.init(a, head);
     auto request = [&]() {
-        pages.request(page0, 0, lds0);
-        pages.request(page1, 1, lds0);
+        pages.request(page0, 0, lds0 + fill * Block<D>::BYTES);
+        pages.request(page1, 1, lds0 + fill * Block<D>::BYTES);
         ahead += 32 * kWaves;
         page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
+        fill ^= 1;
     };
+    w.load(a, p.r, head, c);
+    if (range.begin + 32 * wave < range.end) request();
     for (int from = range.begin + 32 * wave; from < range.end; from += 32 * kWaves) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the last step read is written again
+        uint8_t* const block = lds + (wave * 2 + (fill ^ 1)) * Block<D>::BYTES;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the block before was read from is written again
         request();
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * Block<D>::OPS) : "memory");
         const bool partly = from < all_from || from + 31 > low;
-        pages.note(block, 0, 1, from, p.r.n, partly);
-        pages.note(block, 1, 0, from + kPageTokens, p.r.n, partly);
+        pages.note(block, 0, 3, from, p.r.n, partly);
+        pages.note(block, 1, 2, from + kPageTokens, p.r.n, partly);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         f32x16 s = w.scores(block), none;
         w.template step<false>(a, s, block, from, !partly && __all(Block<D>::notes(block, h).plain()), nullptr, none);
