@@ -776,9 +776,7 @@ def sun_mx4_gated(gate_codes, gate_scales, up_codes, up_scales, x, out, workspac
     """out [rows, N] = act(x [rows, K] Wg^T) * (x Wu^T); x and out float32 or bfloat16 each, rows at any stride."""
     dev = _gpu(gate_codes)
     pg, sg, n, k = _mx4(gate_codes, gate_scales, dev)
-    if up_codes.shape != gate_codes.shape:
-        _refuse(f"up_codes must be {tuple(gate_codes.shape)} as gate_codes, is {tuple(up_codes.shape)}")
-    pu, su, _, _ = _mx4(up_codes, up_scales, dev)
+    pu, su = _want("up_codes", up_codes, dev, torch.uint8, gate_codes.shape), _want("up_scales", up_scales, dev, torch.uint8, gate_scales.shape)
     if x.dim() != 2:
         _refuse("x must be [rows, K]")
     rows, tx, to = x.shape[0], x.dtype, out.dtype

@@ -423,7 +423,6 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     // and the tile's positions from tile_from to tile_to by all of its places
     const int tile_to = base + tile * kTile / G, tile_from = a.window > 0 ? max(base + (min((tile + 1) * kTile, live) - 1) / G - a.window + 1, 0) : 0;
     Places<T, D> w;
-    w.load(a, p.r, head, v0 + c);
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
     int ahead = range.begin + wave * kPageTokens, fill = 0;
     int page = page_at(ahead);
@@ -440,6 +439,7 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     };
     request();
     request();
+    w.load(a, p.r, head, v0 + c);   // behind the requests, whose way it shares
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(OPS) : "memory");
     note(0, 1, range.begin);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -521,8 +521,8 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
         page0 = page_at(ahead), page1 = page_at(ahead + kPageTokens);
         fill ^= 1;
     };
-    w.load(a, p.r, head, c);
     if (range.begin + 32 * wave < range.end) request();
+    w.load(a, p.r, head, c);   // behind the request, whose way it shares
     for (int from = range.begin + 32 * wave; from < range.end; from += 32 * kWaves) {
         uint8_t* const block = lds + (wave * 2 + (fill ^ 1)) * Block<D>::BYTES;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what the block before was read from is written again

@@ -434,9 +434,9 @@ def test_layer_in_a_graph(dtype):
     """Captured and replayed with the program's own eager work between: every replay's bits are the eager run's."""
     lens, counts = [0, 15, 500, 33], [40, 1, 4, 0]
     eager, graphed = Layer(lens, counts, dtype), Layer(lens, counts, dtype)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
     start = (graphed.lens.clone(), graphed.cache.mem.clone())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())   # behind the copies: the run changes what they are of
     with torch.cuda.stream(side):
         graphed.run()
     torch.cuda.current_stream().wait_stream(side)
