@@ -242,14 +242,17 @@ struct Places {
 
     // A block's keys on their way into operands
     struct Keys {
-        u32x4_s codes[KS / 2];
+        const uint8_t* at;
+        int key;
         float scale;
-        __device__ __forceinline__ void read(const uint8_t* block) {
-            const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5, token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+        u32x4_s codes[KS / 2];
+        __device__ __forceinline__ Keys(const uint8_t* block) {
+            const int lane = threadIdx.x & 63, c = lane & 31, token = 16 * (c >> 2 & 1) + 4 * (c >> 3) + (c & 3);
+            at = block + token * D;
+            key = Block<D>::key(token) ^ (lane >> 5);
             scale = Block<D>::notes(block, token >> 4).powers[16 + (token & 15)];
-#pragma unroll
-            for (int w = 0; w < KS / 2; ++w) codes[w] = *reinterpret_cast<const u32x4_s*>(block + token * D + ((2 * w + h) ^ Block<D>::key(token)) * 16);
         }
+        __device__ __forceinline__ void read(int w) { codes[w] = *reinterpret_cast<const u32x4_s*>(at + ((2 * w) ^ key) * 16); }
     };
     __device__ __forceinline__ void scores(const Keys& k, int i, f32x16& out) const {   // one step of 16 dims
         const bf16x8 x = codes_to_bf16(k.codes[i >> 1][2 * (i & 1)], k.codes[i >> 1][2 * (i & 1) + 1], k.scale);
@@ -257,13 +260,18 @@ struct Places {
         for (int p = 0; p < P; ++p) out = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[p][i], out, 0, 0, 0);
     }
     __device__ __forceinline__ f32x16 scores(const uint8_t* block) const {
-        Keys k;
-        k.read(block);
+        Keys k(block);
         f32x16 s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        k.read(0);
 #pragma unroll
-        for (int i = 0; i < KS; ++i) scores(k, i, s);
+        for (int w = 0; w < KS / 2; ++w) {
+            if (w + 1 < KS / 2) k.read(w + 1);
+            __builtin_amdgcn_sched_barrier(0);   // all at once they take the registers
+            scores(k, 2 * w, s);
+            scores(k, 2 * w + 1, s);
+        }
         return s;
     }
 
@@ -301,8 +309,11 @@ struct Places {
     __device__ __forceinline__ void step(const ChunkArgs& a, f32x16& s, const uint8_t* block, int at, bool whole, const uint8_t* behind, f32x16& s2) {
         const int h = (threadIdx.x & 63) >> 5;
         const Notes& notes = Block<D>::notes(block, h);
-        Keys k;
-        if constexpr (NEXT) k.read(behind);
+        Keys k(NEXT ? behind : block);
+        if constexpr (NEXT) {
+#pragma unroll
+            for (int i = 0; i < KS / 2; ++i) k.read(i);
+        }
         uint32_t live = 0xffff;   // tokens that the lane's place sees
         if (!whole) {
             const int mine = at + 16 * h, from = max(lo - mine, 0), to = min(hi - mine, 15);
@@ -453,14 +464,18 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     };
     if (v0 < live) {
         auto whole = [&](const uint8_t* block, int from) { return from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()); };
+        // 32-bit queries and weights take the registers that scores ahead of their block need, and there the matrix cores are what is short
+        constexpr bool NEXT = sizeof(T) == 2;
         f32x16 s = w.scores(lds), s2;
         for (int token = range.begin; token < range.end; token += 64) {
             const uint8_t *first = lds + at * STAGE, *second = first + Block<D>::BYTES;
             request();
-            w.template step<true>(a, s, first, token, whole(first, token), second, s2);
+            w.template step<NEXT>(a, s, first, token, whole(first, token), second, s2);
             turn(token);
             at = at + 1 & 3;
-            w.template step<true>(a, s2, second, token + 32, whole(second, token + 32), lds + at * STAGE, s);
+            if constexpr (!NEXT) s2 = w.scores(second);
+            w.template step<NEXT>(a, s2, second, token + 32, whole(second, token + 32), lds + at * STAGE, s);
+            if constexpr (!NEXT) s = w.scores(lds + at * STAGE);
         }
     } else {   // requests for the others
         for (int token = range.begin; token < range.end; token += 64) {
@@ -681,7 +696,7 @@ hipError_t launch_kv8_chunk_attention(const Kv8Pool& pool, int layer, int batch,
     a.s_page = L.s_page, a.s_head = L.s_head, a.vs_off = L.vs_off - L.ks_off;
     a.q = q, a.row_starts = row_starts, a.page_tables = page_tables, a.n_tokens = n_tokens, a.out = out, a.partial = partial;
     a.batch = batch, a.rows = rows, a.max_pages = max_pages, a.n_pages = (int)L.n_pages;
-    a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads, a.window = window;
+    a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads, a.window = std::min(window, 1 << 30);   // no cache is longer, and positions less a window fit 32 bits
     a.splits = chunk_splits(c, batch, rows, max_pages);
     a.slot_rows = chunk_slot_rows(c, rows);
     const int64_t tiles = chunk_tiles(c, batch, rows);

@@ -144,7 +144,8 @@ def test_lost_pages_and_counts_beyond(dtype):
     cache.dev_table = i32(cache.table)
     _, out = check(cache, 0, counts, lens, dtype)
     assert (out[80:90] == 0).all() and (out[90:106] == 0).all()
-    check(cache, 0, counts, [100, 12, 4, 100, -7, 0], dtype)
+    for window in (0, 2 ** 31 - 1, 2 ** 30, 3):
+        check(cache, 0, counts, [100, 12, 4, 100, -7, 0], dtype, window=window)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
