@@ -1733,7 +1733,7 @@ int sun_mx4_linear_fused(const void* codes, const void* scales, int N, int K, in
     return run_mx4_linear(m, N, x_dtype, out_dtype, workspace, workspace_bytes, stream);
 }
 
-size_t sun_mx4_gated_workspace_bytes(int N, int K, int rows) { return N > 1 << 27 ? 0 : sun_mx4_linear_workspace_bytes(2 * N, K, rows); }
+size_t sun_mx4_gated_workspace_bytes(int N, int K, int rows) { return N < 1 || N > 1 << 27 ? 0 : sun_mx4_linear_workspace_bytes(2 * N, K, rows); }
 
 int sun_mx4_gated(const void* gate_codes, const void* gate_scales, const void* up_codes, const void* up_scales, int N, int K, int rows,
                   const void* x, int x_dtype, int64_t ld_x, int activation, void* out, int out_dtype, int64_t ld_out, void* workspace,

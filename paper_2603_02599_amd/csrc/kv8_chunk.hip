@@ -27,7 +27,7 @@ constexpr int kGroupsWanted = 512;   // workgroups that parts are made for
 
 struct ChunkArgs {
     const uint8_t *codes, *scales;
-    int64_t k_page, k_head, v_off, v_page, v_head, s_page, s_head, vs_off;
+    int64_t k_page, k_head, v_off, v_head, s_page, s_head, vs_off;   // a page's keys and values lie as far apart as any page's
     const void* q;
     const int32_t *row_starts, *page_tables, *n_tokens;
     void* out;
@@ -73,7 +73,7 @@ struct ChunkPlace {
 };
 // Item `index` of all requests' (a tile's part; TILES: a tile).  The whole wave calls it.
 template <bool TILES>
-__device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, int index) {
+__device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, long long index) {
     const int lane = threadIdx.x & 63;
     long long items = 0;
     int tiles = 0;
@@ -136,7 +136,7 @@ static __device__ uint32_t g_no_page[512] = {};
 template <int D>
 struct PageRequests {
     const uint8_t *codes, *scales;   // the head's
-    int64_t k_page, v_off, v_page, s_page;
+    int64_t k_page, v_off, s_page;
     int n_pages;
     uint32_t k_lane[2], v_lane, s_lane;   // keys by half of the block
     uint32_t there;                       // bit i: whether the page that was requested i pages ago is
@@ -145,7 +145,7 @@ struct PageRequests {
         const int lane = threadIdx.x & 63;
         codes = a.codes + head * a.k_head;
         scales = a.scales + head * a.s_head;
-        k_page = a.k_page, v_off = a.v_off + head * (a.v_head - a.k_head), v_page = a.v_page, s_page = a.s_page;
+        k_page = a.k_page, v_off = a.v_off + head * (a.v_head - a.k_head), s_page = a.s_page;
         n_pages = a.n_pages;
         constexpr int PIECES = D / 16;
         const int token = lane / PIECES;   // more tokens of a page have the same key
@@ -166,7 +166,7 @@ struct PageRequests {
         }
         lds_dma16<D / 64>(k, half ? k_lane[1] : k_lane[0], block + half * 16 * D);
         lds_dma16<D / 64>(v, v_lane, block + Block<D>::V + half * 16 * D);
-        lds_dma4(s, s_lane, block + Block<D>::S + half * 256);
+        lds_dma4(s, there & 1 ? s_lane : 0u, block + Block<D>::S + half * 256);   // values' powers may lie further behind than what stands for a page is long
     }
     // Notes of a page that has landed, requested `ago` pages ago, whose first token is `at`.  Powers and values from token n on, which nobody has written, become zeros; where some places see
     // a token and others do not (`partly`), values that are not numbers are noted and become zeros: their product with a weight of 0 would not be.
@@ -598,7 +598,7 @@ template <class T, int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ChunkLds<D>::BYTES];
     const int head = blockIdx.x % a.Hkv;
-    for (int item = blockIdx.x / a.Hkv;; item += gridDim.x / a.Hkv) {
+    for (long long item = blockIdx.x / a.Hkv;; item += gridDim.x / a.Hkv) {
         const ChunkPlace p = chunk_find<false>(a, item);
         if (p.b < 0) return;
         const int split = p.index % p.r.splits, turn = p.index / p.r.splits, half = (p.r.tiles + 1) / 2;
@@ -692,7 +692,7 @@ hipError_t launch_kv8_chunk_attention(const Kv8Pool& pool, int layer, int batch,
     a.codes = pool.base + L.k_off + layer * L.k_layer;
     a.scales = pool.base + L.ks_off + layer * L.s_layer;
     a.k_page = L.k_page, a.k_head = L.k_head;
-    a.v_off = L.v_off - L.k_off, a.v_page = L.v_page, a.v_head = L.v_head;
+    a.v_off = L.v_off - L.k_off, a.v_head = L.v_head;
     a.s_page = L.s_page, a.s_head = L.s_head, a.vs_off = L.vs_off - L.ks_off;
     a.q = q, a.row_starts = row_starts, a.page_tables = page_tables, a.n_tokens = n_tokens, a.out = out, a.partial = partial;
     a.batch = batch, a.rows = rows, a.max_pages = max_pages, a.n_pages = (int)L.n_pages;

@@ -73,15 +73,12 @@ __device__ __forceinline__ float kv8_quotient(float v, float sum, float top) { r
 
 static __device__ u32x4_s g_zeros = {0, 0, 0, 0};   // what lanes are given whose place in memory is not there
 
-// Requests from memory straight into LDS, the address a lane's own: 16 bytes a lane (lane i's land at lds_byte + 16 i), a word, or a byte, which
-// lands as a word (both at lds_byte + 4 i).  Whoever reads the place waits for vmcnt and the barrier by hand.
+// Requests from memory straight into LDS, the address a lane's own: 16 bytes a lane (lane i's land at lds_byte + 16 i), or a byte, which
+// lands as a word (at lds_byte + 4 i).  Whoever reads the place waits for vmcnt and the barrier by hand.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"   // m0 is a reserved register, see lds_dma16
 __device__ __forceinline__ void lds_fetch16(const void* p, uint32_t lds_byte) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");
-}
-__device__ __forceinline__ void lds_fetch4(const void* p, uint32_t lds_byte) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");
 }
 __device__ __forceinline__ void lds_fetch1(const void* p, uint32_t lds_byte) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds_byte), "v"(p) : "memory", "m0");

@@ -148,6 +148,17 @@ def test_lost_pages_and_counts_beyond(dtype):
         check(cache, 0, counts, [100, 12, 4, 100, -7, 0], dtype, window=window)
 
 
+@pytest.mark.parametrize("counts", [[5, 1], [60, 33]])
+def test_lost_pages_of_many_heads(counts):
+    """More heads than a page's stand-in has powers for: the values' powers of a page lie 16 bytes a head behind its keys'."""
+    cache = Cache(make_shape(192, 192, 64), [70, 40])
+    cache.fill(0, [70, 40])
+    cache.table[0, 1] = -1
+    cache.table[1, 2] = cache.n_pages
+    cache.dev_table = i32(cache.table)
+    check(cache, 0, counts, [70, 40], "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_not_a_numbers_stay_where_they_belong(d, dtype):
