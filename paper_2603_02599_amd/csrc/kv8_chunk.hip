@@ -10,6 +10,7 @@
 // (24 bits) in 32-bit ones.  Maximum, sum and output are in 32 bits, the sum over the weights as they are multiplied.
 // The reference that scores are taken against is raised to kHead above the maximum when a score passes it, so that it is raised seldom and a weight is never above 1.
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include "kernels.hpp"
@@ -25,6 +26,16 @@ constexpr int kMinSplit = 256;       // tokens of a part at least
 constexpr int kMaxSplits = 64;
 constexpr int kGroupsWanted = 512;   // workgroups that parts are made for
 
+// Division by a number that the host knows: a product, and one more where what is left says so.  The dozen divisions in front of a tile's first request took it over a microsecond.
+struct Divider {
+    uint32_t d, m;   // m = min(2^32 / d, 2^32 - 1): the product's upper word is the quotient or one less
+    static Divider of(int d) { return Divider{(uint32_t)d, d == 1 ? ~0u : (uint32_t)((1ull << 32) / d)}; }
+    __device__ __forceinline__ int quotient(int v) const {
+        const uint32_t q = __umulhi((uint32_t)v, m);
+        return (int)(q + ((uint32_t)v - q * d >= d));
+    }
+};
+
 struct ChunkArgs {
     const uint8_t *codes, *scales;
     int64_t k_page, k_head, v_off, v_head, s_page, s_head, vs_off;   // a page's keys and values lie as far apart as any page's
@@ -34,6 +45,8 @@ struct ChunkArgs {
     float* partial;      // [slot][slot_rows][D], behind them (reference in powers of two, sum) pairs [slot][slot_rows]
     int64_t slots;
     int batch, rows, max_pages, n_pages, Hq, Hkv, window, splits, slot_rows;
+    bool sorted;
+    Divider G, heads;    // query heads of a KV head, KV heads
     float c;             // log2(e) / sqrt(D)
 };
 
@@ -46,7 +59,7 @@ __device__ __forceinline__ ChunkRequest chunk_request(const ChunkArgs& a, int b)
     r.start = min(max(a.row_starts[b], 0), a.rows);
     r.count = max(min(a.row_starts[b + 1], a.rows) - r.start, 0);
     r.n = (int)min((long long)max(a.n_tokens[b], 0), (long long)a.max_pages * kPageTokens);
-    const int places = r.count * (a.Hq / a.Hkv);
+    const int places = r.count * a.G.d;
     r.tiles = places <= kFew ? places > 0 : (places + kTile - 1) / kTile;
     const long long first = a.window > 0 ? max((long long)r.n - r.count - a.window + 1, 0ll) : 0;
     r.splits = max(1, min(a.splits, (int)((r.n - first + kMinSplit - 1) / kMinSplit)));
@@ -101,6 +114,50 @@ __device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, long long i
     ChunkPlace none{};
     none.b = -1;
     return none;
+}
+
+// Tile `index` of all requests' in the order of their lengths in steps of 64 tokens, the longest first, where that gains: what starts last has to be short.  For up to kSorted requests,
+// one a lane, without parts, and few rounds of workgroups (the host decides); false where no request is long.  Against requests in turn: prompts of 583 to 1500 tokens 73 -> 66 us,
+// four drafted tokens of 64 requests 72 -> 68, 128 of 1000 to 2500 of sixteen 101 -> 88, but 32 prompts of 128 33 -> 42, whose workgroups then all wait and all compute at the
+// same time, and sixteen prompts of 200 to 1700 (eight rounds) 239 -> 243.  Finding a tile takes 2000 cycles, chunk_find 1300.  The whole wave calls it.
+constexpr int kSorted = 64, kSortedFrom = 512, kSortedGroups = 2560;
+__device__ __forceinline__ bool chunk_longest(const ChunkArgs& a, int index, ChunkPlace& p) {
+    const ChunkRequest r = chunk_request(a, threadIdx.x & 63);
+    const int G = a.G.d, base = max(r.n - r.count, 0), most = min(r.count, r.n), cap = a.window > 0 ? a.window / 64 + 2 : INT_MAX;
+    auto longer = [&](int steps) {   // the lane's request's tiles that end behind so many steps
+        const int rows = steps * 64 - base;
+        return steps > cap || rows > most ? 0 : rows <= 0 ? r.tiles : r.tiles - (rows * G + kTile - 1) / kTile + 1;
+    };
+    auto sum = [](int v) { return __builtin_amdgcn_readlane(lanes_before(v), 63); };
+    if (!__any(r.tiles && r.n >= kSortedFrom)) return false;
+    p = ChunkPlace{};
+    p.b = -1;
+    const int total = sum(r.tiles);
+    if (index >= total) return true;
+    // Where all are on the chip at once, two workgroups a compute unit, the second half comes the other way round, so that a unit has a long and a short one
+    const int half = (total + 1) / 2;
+    if (total * a.Hkv <= 512 && index >= half) index = total - 1 - (index - half);
+    int lo = 0, hi = a.max_pages / 4 + 2, in_front = 0;   // more than `index` tiles end behind lo, in_front behind hi and no more than `index`
+    while (hi - lo > 1) {
+        const int each = (hi - lo + 3) / 4;
+        int at[3], n[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) at[i] = min(lo + (i + 1) * each, hi), n[i] = sum(longer(at[i]));
+#pragma unroll
+        for (int i = 2; i >= 0; --i)
+            if (n[i] <= index) hi = at[i], in_front = n[i];
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (n[i] > index) lo = at[i];
+    }
+    index -= in_front;
+    const int behind = longer(hi), mine = longer(lo) - behind, past = lanes_before(mine);
+    const int l = __ffsll((unsigned long long)__ballot(past > index)) - 1;
+    auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+    p.r = ChunkRequest{of(r.start), of(r.count), of(r.n), of(r.tiles), 1};
+    p.b = l;
+    p.index = of(r.tiles) - 1 - of(behind) - (index - (of(past) - of(mine)));
+    return true;
 }
 
 // ---------------------------------------------------------------- attention of one part
@@ -212,12 +269,12 @@ struct Places {
     uint32_t had;      // not 0: one of them was there
 
     __device__ __forceinline__ void load(const ChunkArgs& a, const ChunkRequest& r, int head, int v) {
-        const int G = a.Hq / a.Hkv, h = (threadIdx.x & 63) >> 5;
+        const int G = a.G.d, h = (threadIdx.x & 63) >> 5;
         const bool on = v < r.count * G;
-        const int row = on ? v / G : 0, pos = r.n - r.count + row;
+        const int row = on ? a.G.quotient(v) : 0, pos = r.n - r.count + row;
         hi = on ? pos : -1;
         lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
-        const T* p = (const T*)a.q + ((int64_t)(r.start + row) * a.Hq + head * G + (on ? v % G : 0)) * D + 16 * h;
+        const T* p = (const T*)a.q + ((int64_t)(r.start + row) * a.Hq + head * G + (on ? v - row * G : 0)) * D + 16 * h;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             if constexpr (F32) {
@@ -410,10 +467,10 @@ __device__ __forceinline__ void store4(T* to, float a, float b, float c, float d
 // The range of a tile's part
 struct ChunkRange { int begin, end; };
 __device__ __forceinline__ ChunkRange chunk_range(const ChunkArgs& a, const ChunkRequest& r, int places0, int places, int split, int step) {
-    const int G = a.Hq / a.Hkv, last = min(places0 + places, r.count * G) - 1;
-    const int hi = r.n - r.count + last / G + 1, low = a.window > 0 ? max(r.n - r.count + places0 / G - a.window + 1, 0) : 0;
+    const int last = min(places0 + places, r.count * (int)a.G.d) - 1;
+    const int hi = r.n - r.count + a.G.quotient(last) + 1, low = a.window > 0 ? max(r.n - r.count + a.G.quotient(places0) - a.window + 1, 0) : 0;
     const int first = low / kPageTokens * kPageTokens, span = max(hi - first, 0);
-    const int per = ((span + r.splits - 1) / r.splits + step - 1) / step * step;
+    const int per = ((r.splits == 1 ? span : (span + r.splits - 1) / r.splits) + step - 1) / step * step;
     const long long begin = first + (long long)split * per;
     return ChunkRange{(int)min(begin, (long long)max(hi, 0)), (int)min(begin + per, (long long)max(hi, 0))};
 }
@@ -424,15 +481,15 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     static_assert(kWideStages == 4, "");
     constexpr int STAGE = 2 * Block<D>::BYTES, OPS = Block<D>::OPS;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    const int G = a.Hq / a.Hkv, v0 = tile * kTile + 32 * wave, live = p.r.count * G;
+    const int G = a.G.d, v0 = tile * kTile + 32 * wave, live = p.r.count * G;
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
     // positions from all_from to low are seen by all of the wave's places
-    const int base = p.r.n - p.r.count, low = base + v0 / G, high = base + (min(v0 + 32, live) - 1) / G;
+    const int base = p.r.n - p.r.count, low = base + a.G.quotient(v0), high = base + a.G.quotient(min(v0 + 32, live) - 1);
     const int all_from = a.window > 0 ? max(high - a.window + 1, 0) : 0;
     // and the tile's positions from tile_from to tile_to by all of its places
-    const int tile_to = base + tile * kTile / G, tile_from = a.window > 0 ? max(base + (min((tile + 1) * kTile, live) - 1) / G - a.window + 1, 0) : 0;
+    const int tile_to = base + a.G.quotient(tile * kTile), tile_from = a.window > 0 ? max(base + a.G.quotient(min((tile + 1) * kTile, live) - 1) - a.window + 1, 0) : 0;
     Places<T, D> w;
     auto page_at = [&](int token) { return token < range.end ? load_uniform(table + min(token / kPageTokens, a.max_pages - 1)) : -1; };
     int ahead = range.begin + wave * kPageTokens, fill = 0;
@@ -489,8 +546,8 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     const int v = v0 + c;
     if (v < live) {
         if (p.r.splits == 1) {
-            const int row = p.r.start + v / G;
-            T* out = (T*)a.out + ((int64_t)row * a.Hq + head * G + v % G) * D;
+            const int row = a.G.quotient(v);
+            T* out = (T*)a.out + ((int64_t)(p.r.start + row) * a.Hq + head * G + v - row * G) * D;
             const float f = chunk_factor(w.l, w.m);
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
@@ -517,7 +574,7 @@ template <class T, int D>
 __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& p, int head, int split, int64_t slot, uint8_t* lds) {
     constexpr int HALF = D / 2, LD = HALF + 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    const int G = a.Hq / a.Hkv, live = p.r.count * G;
+    const int G = a.G.d, live = p.r.count * G;
     const ChunkRange range = chunk_range(a, p.r, 0, kFew, split, 32 * kWaves);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds + wave * 2 * Block<D>::BYTES;
@@ -582,7 +639,8 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
                 for (int e = 0; e < 4; ++e) x[e] += f * o[e];
             }
             if (p.r.splits == 1) {
-                T* to = (T*)a.out + ((int64_t)(p.r.start + v / G) * a.Hq + head * G + v % G) * D + part * HALF + d;
+                const int row = a.G.quotient(v);
+                T* to = (T*)a.out + ((int64_t)(p.r.start + row) * a.Hq + head * G + v - row * G) * D + part * HALF + d;
                 const float f = chunk_factor(sum, top);
                 store4(to, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
             } else {
@@ -597,29 +655,28 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
 template <class T, int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ChunkLds<D>::BYTES];
-    const int head = blockIdx.x % a.Hkv;
-    for (long long item = blockIdx.x / a.Hkv;; item += gridDim.x / a.Hkv) {
-        const ChunkPlace p = chunk_find<false>(a, item);
-        if (p.b < 0) return;
-        const int split = p.index % p.r.splits, turn = p.index / p.r.splits, half = (p.r.tiles + 1) / 2;
-        // The longest first.  Where all of a request's are on the chip at once, two workgroups a compute unit, the second half comes the other way round, so that a unit has a long and a
-        // short one (2048 of 8191 tokens 283 -> 274 us).
-        const bool paired = p.r.tiles * p.r.splits * a.Hkv <= 512;
-        const int tile = paired && turn >= half ? turn - half : p.r.tiles - 1 - turn;
-        const int64_t slot = (p.items + (int64_t)tile * p.r.splits + split) * a.Hkv + head;
-        if (p.r.splits == 1 || slot < a.slots) {   // row starts that are none could name more
-            if (p.r.count * (a.Hq / a.Hkv) <= kFew) chunk_few<T, D>(a, p, head, split, slot, lds);
-            else chunk_wide<T, D>(a, p, head, tile, split, slot, lds);
-        }
-        __syncthreads();
-    }
+    // No loop over items: what it keeps in scalar registers has others spilled (four drafted tokens of 64 requests 69 -> 66.5 us, 14B heads in 32 bits 103 -> 99)
+    const int item = a.heads.quotient(blockIdx.x), head = blockIdx.x - item * a.Hkv;
+    ChunkPlace p;
+    const bool sorted = a.sorted && chunk_longest(a, item, p);
+    if (!sorted) p = chunk_find<false>(a, item);
+    if (p.b < 0) return;
+    // The longest first.  Where all of a request's are on the chip at once, two workgroups a compute unit, the second half comes the other way round, so that a unit has a long and a
+    // short one (2048 of 8191 tokens 283 -> 274 us).
+    const int turn = p.r.splits == 1 ? p.index : p.index / p.r.splits, split = p.index - turn * p.r.splits, half = (p.r.tiles + 1) / 2;
+    const bool paired = p.r.tiles * p.r.splits * a.Hkv <= 512;
+    const int tile = sorted ? p.index : paired && turn >= half ? turn - half : p.r.tiles - 1 - turn;
+    const int64_t slot = (p.items + (int64_t)tile * p.r.splits + split) * a.Hkv + head;
+    if (p.r.splits > 1 && slot >= a.slots) return;   // row starts that are none could name more
+    if (p.r.count * (int)a.G.d <= kFew) chunk_few<T, D>(a, p, head, split, slot, lds);
+    else chunk_wide<T, D>(a, p, head, tile, split, slot, lds);
 }
 
 // out = sum over a tile's parts, four dims a lane; its places are dealt to gridDim.y workgroups
 template <class T, int D>
 __global__ __launch_bounds__(256) void kv8_chunk_join_kernel(ChunkArgs a) {
-    const int G = a.Hq / a.Hkv, head = blockIdx.x % a.Hkv;
-    const ChunkPlace p = chunk_find<true>(a, blockIdx.x / a.Hkv);
+    const int G = a.G.d, item = a.heads.quotient(blockIdx.x), head = blockIdx.x - item * a.Hkv;
+    const ChunkPlace p = chunk_find<true>(a, item);
     if (p.b < 0 || p.r.splits == 1) return;
     const int tile = p.index, places = p.r.count * G <= kFew ? kFew : kTile, live = min(p.r.count * G - tile * places, places);
     const int64_t slot = (p.items + (int64_t)tile * p.r.splits) * a.Hkv + head;
@@ -641,9 +698,9 @@ __global__ __launch_bounds__(256) void kv8_chunk_join_kernel(ChunkArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] = x[e] * f + o[e] * g;
         }
-        const int v = tile * places + i;
+        const int v = tile * places + i, row = a.G.quotient(v);
         const float f = chunk_factor(sum, top);
-        store4((T*)a.out + ((int64_t)(p.r.start + v / G) * a.Hq + head * G + v % G) * D + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+        store4((T*)a.out + ((int64_t)(p.r.start + row) * a.Hq + head * G + v - row * G) * D + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
     }
 }
 
@@ -676,8 +733,7 @@ size_t kv8_chunk_workspace_up_to(const sun_model_cfg& c, int batch, int rows, in
 
 template <class T, int D>
 static hipError_t chunk_attend(const ChunkArgs& a, int64_t tiles, hipStream_t st) {
-    const int64_t items = tiles * a.splits;
-    const unsigned grid = (unsigned)(std::min<int64_t>(items, std::max<int64_t>(8192 / a.Hkv, 1)) * a.Hkv);
+    const unsigned grid = (unsigned)(tiles * a.splits * a.Hkv);   // not 2^23: parts are for fewer than kGroupsWanted groups
     hipLaunchKernelGGL((kv8_chunk_kernel<T, D>), dim3(grid), dim3(64 * kWaves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)(a.slot_rows / 32)), dim3(256), 0, st, a);
@@ -697,9 +753,11 @@ hipError_t launch_kv8_chunk_attention(const Kv8Pool& pool, int layer, int batch,
     a.q = q, a.row_starts = row_starts, a.page_tables = page_tables, a.n_tokens = n_tokens, a.out = out, a.partial = partial;
     a.batch = batch, a.rows = rows, a.max_pages = max_pages, a.n_pages = (int)L.n_pages;
     a.Hq = c.n_q_heads, a.Hkv = c.n_kv_heads, a.window = std::min(window, 1 << 30);   // no cache is longer, and positions less a window fit 32 bits
+    a.G = Divider::of(c.n_q_heads / c.n_kv_heads), a.heads = Divider::of(c.n_kv_heads);
     a.splits = chunk_splits(c, batch, rows, max_pages);
     a.slot_rows = chunk_slot_rows(c, rows);
     const int64_t tiles = chunk_tiles(c, batch, rows);
+    a.sorted = a.splits == 1 && batch > 1 && batch <= kSorted && tiles * a.Hkv <= kSortedGroups;
     a.slots = a.splits > 1 ? tiles * a.Hkv * a.splits : 0;
     a.c = 1.4426950408889634f / sqrtf((float)c.head_dim);
     if (f32) return c.head_dim == 128 ? chunk_attend<float, 128>(a, tiles, st) : chunk_attend<float, 64>(a, tiles, st);
