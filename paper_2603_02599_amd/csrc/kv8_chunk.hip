@@ -22,7 +22,7 @@ constexpr int kTile = 128;           // places of a workgroup: 32 to a wave
 constexpr int kFew = 32;             // requests of so many places at most: the four waves share them and take tokens in turn
 constexpr int kWaves = 4;
 constexpr float kHead = 6.f;         // powers of two
-constexpr int kMinSplit = 256;       // tokens of a part at least
+constexpr int kMinSplit = 512;       // tokens of a part at least
 constexpr int kMaxSplits = 64;
 constexpr int kGroupsWanted = 512;   // workgroups that parts are made for
 
@@ -672,7 +672,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) 
     else chunk_wide<T, D>(a, p, head, tile, split, slot, lds);
 }
 
-// out = sum over a tile's parts, four dims a lane; its places are dealt to gridDim.y workgroups
+// out = sum over a tile's parts, four dims a lane; its places are dealt to gridDim.y workgroups.  Memory's latency is what bounds it: with eight parts on their way and eight places a
+// workgroup 4 of 8191 tokens (32 parts) take 32 -> 16 us with their attention, 8 of 32768 (64) 101 -> 30, against one part and four times the places.
 template <class T, int D>
 __global__ __launch_bounds__(256) void kv8_chunk_join_kernel(ChunkArgs a) {
     const int G = a.G.d, item = a.heads.quotient(blockIdx.x), head = blockIdx.x - item * a.Hkv;
@@ -688,16 +689,33 @@ __global__ __launch_bounds__(256) void kv8_chunk_join_kernel(ChunkArgs a) {
         const int64_t at0 = slot * a.slot_rows + i;
         const int d = threadIdx.x % LANES * 4;
         float top = -INFINITY, sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < p.r.splits; ++s) {
-            const float2 y = ml[at0 + s * step];
-            const f32x4 o = *reinterpret_cast<const f32x4*>(a.partial + (at0 + s * step) * D + d);
-            const float grown = fmaxf(top, y.x), ref = grown == -INFINITY ? 0.f : grown;
-            const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(y.x - ref);
-            top = grown;
-            sum = sum * f + y.y * g;
+        int s0 = 0;
+        auto parts = [&](auto n) {   // so many of them, all on their way before the first is waited for
+            constexpr int N = decltype(n)::value;
+            float2 y[N];
+            f32x4 o[N];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = x[e] * f + o[e] * g;
-        }
+            for (int s = 0; s < N; ++s) {
+                const int64_t at = at0 + (s0 + s) * step;
+                y[s] = ml[at];
+                o[s] = *reinterpret_cast<const f32x4*>(a.partial + at * D + d);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < N; ++s) {
+                const float grown = fmaxf(top, y[s].x), ref = grown == -INFINITY ? 0.f : grown;
+                const float f = __builtin_amdgcn_exp2f(top - ref), g = __builtin_amdgcn_exp2f(y[s].x - ref);
+                top = grown;
+                sum = sum * f + y[s].y * g;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = x[e] * f + o[s][e] * g;
+            }
+            s0 += N;
+        };
+        while (s0 + 8 <= p.r.splits) parts(std::integral_constant<int, 8>{});
+        if (s0 + 4 <= p.r.splits) parts(std::integral_constant<int, 4>{});
+        if (s0 + 2 <= p.r.splits) parts(std::integral_constant<int, 2>{});
+        if (s0 < p.r.splits) parts(std::integral_constant<int, 1>{});
         const int v = tile * places + i, row = a.G.quotient(v);
         const float f = chunk_factor(sum, top);
         store4((T*)a.out + ((int64_t)(p.r.start + row) * a.Hq + head * G + v - row * G) * D + d, x[0] * f, x[1] * f, x[2] * f, x[3] * f);
@@ -736,7 +754,10 @@ static hipError_t chunk_attend(const ChunkArgs& a, int64_t tiles, hipStream_t st
     const unsigned grid = (unsigned)(tiles * a.splits * a.Hkv);   // not 2^23: parts are for fewer than kGroupsWanted groups
     hipLaunchKernelGGL((kv8_chunk_kernel<T, D>), dim3(grid), dim3(64 * kWaves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)(a.slot_rows / 32)), dim3(256), 0, st, a);
+    // Workgroups of a joined tile: a pass of eight places each where tiles are few (64 of 8191 tokens 40 -> 34 us against four of them), four where every further one would look for
+    // its tile again (1024 of 8191 tokens 165 us, with sixteen 170)
+    const int64_t joining = std::min<int64_t>(a.slot_rows / 8, std::max<int64_t>(4, 1024 / (tiles * a.Hkv)));
+    if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)joining), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
