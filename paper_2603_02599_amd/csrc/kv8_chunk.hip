@@ -8,7 +8,13 @@
 // No value moves between lanes but for the maximum of the two halves h.  Codes become bf16 exactly, a key's power is applied while its codes are converted (a lane has one
 // token's), a value's power to its weight.  bf16 queries enter as they are, 32-bit ones as three planes of 8 bits, exact; a weight of the softmax is bf16(p) in bf16 calls, three planes
 // (24 bits) in 32-bit ones.  Maximum, sum and output are in 32 bits, the sum over the weights as they are multiplied.
-// The reference that scores are taken against is raised to kHead above the maximum when a score passes it, so that it is raised seldom and a weight is never above 1.
+// The reference that scores are taken against is raised to HEAD above the maximum when a score passes it, so that it is raised seldom and a weight is never above 1.
+//
+// What bounds it, 8B heads (32 and 8 of 128) in bf16: 2048 of 8191 tokens take 272 to 284 us, 0.85 to 0.88 PFLOP/s, and there the vector ALU (75 % busy; matrix cores 36 %), which
+// converts a block's 64 codes a lane and takes sixteen exponentials, maxima, sums and roundings for each 16 products: a block measures 443 ns for the two waves of a SIMD, as the
+// instructions alone do.  The matrix instruction for 8-bit operands would need no conversion, but adds products to 2^-13 of their largest, which loses scores' last bits.
+// Four drafted tokens of 64 requests take 66 us, 333 MB at 5.0 TB/s, where reading alone takes 57.  32-bit calls multiply three times (14B heads, window 1000: 98 us, 67 of them the
+// planes' products at the rate of a large product).  Short prompts are bound by what stands in front of a tile's first product, a chain of five loads.
 #include <float.h>
 #include <limits.h>
 #include <math.h>
@@ -18,13 +24,18 @@
 
 namespace sun {
 
-constexpr int kTile = 128;           // places of a workgroup: 32 to a wave
+// A workgroup's share and what it takes.  128 places, 32 to each of four waves, with two workgroups on a compute unit (77 KB of LDS, up to 256 registers): one's vector work runs beside the
+// other's products.  Eight waves of 256 places, whose blocks are converted once for all of them in LDS, took 340 us for 2048 of 8191 tokens against 299, three workgroups a
+// compute unit need 168 registers, which is fewer than there are operands.
+constexpr int kTile = 128;
 constexpr int kFew = 32;             // requests of so many places at most: the four waves share them and take tokens in turn
 constexpr int kWaves = 4;
-constexpr float kHead = 6.f;         // powers of two
-constexpr int kMinSplit = 512;       // tokens of a part at least
+// Parts of long caches, for 512 workgroups (384 / 512 / 768 / 1024: 24 requests with prompts among them 96 / 78 / 78 / 81 us, four drafted tokens of 64 requests 67 / 67 / 83 / 83, 14B heads
+// in 32 bits 102 / 102 / 126 / 126, where each further part is written and joined and the workgroups do not come out even), of 512 tokens at least (256: 64 of 8191 tokens 33 us
+// against 31, 512 of 512 22 against 21; 128: 4 of 8191 20 against 16).
+constexpr int kMinSplit = 512;
 constexpr int kMaxSplits = 64;
-constexpr int kGroupsWanted = 512;   // workgroups that parts are made for
+constexpr int kGroupsWanted = 512;
 
 // Division by a number that the host knows: a product, and one more where what is left says so.  The dozen divisions in front of a tile's first request took it over a microsecond.
 struct Divider {
@@ -261,6 +272,8 @@ struct PageRequests {
 template <class T, int D>
 struct Places {
     static constexpr bool F32 = sizeof(T) == 4;
+    // In powers of two: 0 / 6 / 10 take 2048 of 8191 tokens 297 / 285 / 280 us.  An exponential's argument, up to HEAD, rounds to 24 bits of itself, so 32-bit weights have less of it.
+    static constexpr float HEAD = F32 ? 6.f : 10.f;
     static constexpr int P = F32 ? 3 : 1, KS = D / 16, NB = D / 32;   // planes, steps of 16 dims, blocks of 32 dims
     bf16x8 q[P][KS];
     f32x16 o[NB];
@@ -389,7 +402,7 @@ struct Places {
             top = fmaxf(x, y) * a.c;
         }
         if (__any(top > m)) {
-            const float grown = top > m ? top + kHead : m;
+            const float grown = top > m ? top + HEAD : m;
             const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
             m = grown;
             l *= f;
@@ -455,7 +468,7 @@ struct Places {
     }
 };
 
-// What a weighted sum is multiplied with: 1 / the weights' sum, 0 where there is no token.  Weights are 2^-kHead and more at the reference, so a sum is no less, or 0 where all
+// What a weighted sum is multiplied with: 1 / the weights' sum, 0 where there is no token.  Weights are 2^-HEAD and more at the reference, so a sum is no less, or 0 where all
 // scores are minus infinity, which leaves not-a-numbers.
 __device__ __forceinline__ float chunk_factor(float sum, float top) { return sum == 0.f && top == -INFINITY ? 0.f : sum == 0.f ? NAN : 1.f / sum; }
 template <class T>
@@ -481,7 +494,10 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     static_assert(kWideStages == 4, "");
     constexpr int STAGE = 2 * Block<D>::BYTES, OPS = Block<D>::OPS;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
-    const int G = a.G.d, v0 = tile * kTile + 32 * wave, live = p.r.count * G;
+    const int G = a.G.d, live = p.r.count * G;
+    // Up to 64 places: two waves have the same ones, and one of a step's two blocks each (nine new tokens of 64 requests of 2000 80 -> 69 us, sixteen 82 -> 76)
+    const bool pairs = live - tile * kTile <= 64;
+    const int v0 = tile * kTile + 32 * (pairs ? wave & 1 : wave);
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
     const int32_t* table = a.page_tables + (int64_t)p.b * a.max_pages;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
@@ -523,16 +539,29 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
         auto whole = [&](const uint8_t* block, int from) { return from >= all_from && from + 31 <= low && __all(Block<D>::notes(block, h).plain()); };
         // 32-bit queries and weights take the registers that scores ahead of their block need, and there the matrix cores are what is short
         constexpr bool NEXT = sizeof(T) == 2;
-        f32x16 s = w.scores(lds), s2;
-        for (int token = range.begin; token < range.end; token += 64) {
-            const uint8_t *first = lds + at * STAGE, *second = first + Block<D>::BYTES;
-            request();
-            w.template step<NEXT>(a, s, first, token, whole(first, token), second, s2);
-            turn(token);
-            at = at + 1 & 3;
-            if constexpr (!NEXT) s2 = w.scores(second);
-            w.template step<NEXT>(a, s2, second, token + 32, whole(second, token + 32), lds + at * STAGE, s);
-            if constexpr (!NEXT) s = w.scores(lds + at * STAGE);
+        f32x16 s, s2;
+        if (pairs) {
+            const int mine = wave >> 1;
+            for (int token = range.begin; token < range.end; token += 64) {
+                const uint8_t* block = lds + at * STAGE + mine * Block<D>::BYTES;
+                request();
+                s = w.scores(block);
+                w.template step<false>(a, s, block, token + 32 * mine, whole(block, token + 32 * mine), nullptr, s2);
+                turn(token);
+                at = at + 1 & 3;
+            }
+        } else {
+            s = w.scores(lds);
+            for (int token = range.begin; token < range.end; token += 64) {
+                const uint8_t *first = lds + at * STAGE, *second = first + Block<D>::BYTES;
+                request();
+                w.template step<NEXT>(a, s, first, token, whole(first, token), second, s2);
+                turn(token);
+                at = at + 1 & 3;
+                if constexpr (!NEXT) s2 = w.scores(second);
+                w.template step<NEXT>(a, s2, second, token + 32, whole(second, token + 32), lds + at * STAGE, s);
+                if constexpr (!NEXT) s = w.scores(lds + at * STAGE);
+            }
         }
     } else {   // requests for the others
         for (int token = range.begin; token < range.end; token += 64) {
@@ -543,6 +572,28 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     w.close();
+    if (pairs) {   // the second of a pair gives the first what it has
+        constexpr int NB = D / 32;
+        float* sums = reinterpret_cast<float*>(lds) + (wave & 1) * (NB * 16 + 2) * 64 + lane;
+        static_assert(2 * (NB * 16 + 2) * 256 <= ChunkLds<D>::BYTES, "");
+        __syncthreads();   // every wave is done with what was there
+        if (wave >= 2) {
+            sums[0] = w.m, sums[64] = w.l;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[(2 + 16 * j + i) * 64] = w.o[j][i];
+        }
+        __syncthreads();
+        if (wave >= 2) return;
+        const float m = sums[0], top = fmaxf(w.m, m), ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(w.m - ref), g = __builtin_amdgcn_exp2f(m - ref);
+        w.m = top;
+        w.l = w.l * f + sums[64] * g;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w.o[j][i] = w.o[j][i] * f + sums[(2 + 16 * j + i) * 64] * g;
+    }
     const int v = v0 + c;
     if (v < live) {
         if (p.r.splits == 1) {
@@ -557,7 +608,7 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
                     store4(out + 32 * j + 8 * e + 4 * h, o[4 * e] * f, o[4 * e + 1] * f, o[4 * e + 2] * f, o[4 * e + 3] * f);
                 }
         } else {
-            const int64_t place = slot * a.slot_rows + 32 * wave + c;
+            const int64_t place = slot * a.slot_rows + v - tile * kTile;
             float* out = a.partial + place * D;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
