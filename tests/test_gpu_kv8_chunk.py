@@ -212,6 +212,18 @@ def test_scores_far_apart_and_equal(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq, hkv", [(16, 16), (32, 8)])
+def test_tiles_of_many_lengths(hq, hkv, dtype):
+    """Enough groups of heads and tiles for no parts, so that tiles start by their lengths: long, short and empty requests, some with fewer positions than rows, with and without a window."""
+    lens = [600, 3, 900, 0, 513, 64, 700, 1, 130, 40, 520, 512, 33, 200, 0, 5, 640, 1, 100, 16]
+    counts = [600, 3, 300, 5, 1, 64, 0, 1, 130, 60, 33, 512, 33, 9, 0, 5, 16, 1, 100, 17]
+    cache = Cache(make_shape(hq, hkv, 64), lens, extra_cols=0)
+    cache.fill(0, lens)
+    for window in (0, 90, 700):
+        check(cache, 0, counts, lens, dtype, window=window, pad=20 if hq == hkv else 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hq, hkv, d, counts, lens", [(8, 2, 128, [3], [9000]), (4, 1, 64, [40, 1], [9001, 3]), (32, 8, 128, [70], [4100]), (5, 1, 128, [600, 0, 9], [8000, 0, 7000])])
 def test_long_caches_in_parts(hq, hkv, d, counts, lens, dtype):
     cache = Cache(make_shape(hq, hkv, d), lens)
