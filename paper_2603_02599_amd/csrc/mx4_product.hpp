@@ -575,25 +575,47 @@ __global__ __launch_bounds__(64 * WR * WN, 2) void mx4_tile_kernel(Mx4Args a) {
                                      lds + wave * PASS * NT * 1024);
 }
 
-// out = sum of the parts along k, in their order
+// out = sum of the parts along k, in their order: four columns a lane, up to eight parts on their way at a time
 template <class T, Epilogue E>
 __global__ __launch_bounds__(256) void mx4_join_kernel(Mx4Args a, int splits) {
-    const int64_t total = (int64_t)a.rows * a.N, stride = (int64_t)gridDim.x * 256;
+    constexpr int PAIR = E == GATED ? 2 : 1;
+    const int quads = (a.N + 3) / 4;
+    const int64_t total = (int64_t)a.rows * quads, stride = (int64_t)gridDim.x * 256, part = (int64_t)a.rows * a.N * PAIR;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += stride) {
-        const int64_t row = u / a.N;
-        const int n = (int)(u % a.N);
-        float v, up = 0.f;
-        if constexpr (E == GATED) {
-            const float* p = a.part + row * 2 * a.N + n;
-            up = p[a.N];
-            v = p[0];
-            for (int z = 1; z < splits; ++z) v += p[z * 2 * total], up += p[z * 2 * total + a.N];
-        } else {
-            v = a.part[u];
-            for (int z = 1; z < splits; ++z) v += a.part[z * total + u];
-        }
-        if constexpr (E == PLAIN) store_as((T*)a.out + row * a.ld_out + n, v);
-        else finish_one<E>(a, row, n, v, up);
+        const int64_t row = total >> 32 ? u / quads : (uint32_t)u / (uint32_t)quads;
+        const int n = 4 * (int)(u - row * quads);
+        const float* at = a.part + row * PAIR * a.N + n;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f}, up = v;
+        int z = 0;
+        auto parts = [&](auto count) {
+            constexpr int Z = decltype(count)::value;
+            f32x4 x[Z][PAIR];
+#pragma unroll
+            for (int i = 0; i < Z; ++i)
+#pragma unroll
+                for (int m = 0; m < PAIR; ++m) {
+                    const float* p = at + (z + i) * part + m * a.N;
+                    if (a.N % 4 == 0) x[i][m] = *reinterpret_cast<const f32x4*>(p);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[i][m][e] = n + e < a.N ? p[e] : 0.f;
+                }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < Z; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = z + i == 0 ? x[i][0][e] : v[e] + x[i][0][e];
+                    if constexpr (E == GATED) up[e] = z + i == 0 ? x[i][1][e] : up[e] + x[i][1][e];
+                }
+            z += Z;
+        };
+        while (z + 8 <= splits) parts(std::integral_constant<int, 8>{});
+        if (z + 4 <= splits) parts(std::integral_constant<int, 4>{});
+        if (z + 2 <= splits) parts(std::integral_constant<int, 2>{});
+        if (z < splits) parts(std::integral_constant<int, 1>{});
+        if constexpr (E == PLAIN) store_quad<T>(a, (T*)a.out, a.ld_out, a.wide, row, n, v);
+        else finish_quad<E>(a, row, n, v, up);
     }
 }
 
@@ -632,7 +654,7 @@ static hipError_t multiply(const Mx4Args& a, const Mx4Plan& p, hipStream_t st) {
     }
     if (hipError_t e = hipGetLastError()) return e;
     if (p.splits > 1) {
-        const int64_t total = (int64_t)a.rows * a.N;
+        const int64_t total = (int64_t)a.rows * ((a.N + 3) / 4);
         hipLaunchKernelGGL((mx4_join_kernel<T, E>), dim3((unsigned)std::min<int64_t>((total + 255) / 256, 8192)), dim3(256), 0, st, a, p.splits);
     }
     return hipGetLastError();
