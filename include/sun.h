@@ -57,7 +57,8 @@ enum {
 
 enum { SUN_F32 = 0, SUN_BF16 = 1 };
 
-/* Activations: x; x / (1 + e^-x); x (1 + erf(x / sqrt 2)) / 2, its erf good to 1.5e-7; x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+/* Activations: x; x / (1 + e^-x); x (1 + erf(x / sqrt 2)) / 2, its erf good to 1.5e-7;
+ * x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
 enum { SUN_ACT_NONE = 0, SUN_ACT_SILU = 1, SUN_ACT_GELU = 2, SUN_ACT_GELU_TANH = 3 };
 
 /* step flags */
@@ -588,15 +589,16 @@ size_t sun_kv8_chunk_attention_workspace_bytes(const sun_model_cfg* cfg, int bat
  *   n_tokens   dev int32 [batch]: cached positions, the new ones among them, cut to [0, max_pages*16]
  *   window     a row at position p attends to positions 0 .. p, with window > 0 to the last `window` of them alone: table entries of pages
  *              in front of what a request's first row sees are not read as pages (they may be -1)
- *   out        dev [rows, Hq*d], which must not overlap q; a row that sees no token (a position below 0, every page lost) gets zeros, a head whose query is not finite
- *              not-a-numbers where it sees one.  Rows of no request are left as they are
- * Tokens of a page outside the pool are left out; what a row does not see cannot change its output, not-a-numbers included.  A request's result depends on
- * `batch`, `rows`, max_pages and its own rows, not on the other requests.
- * Cached numbers enter exactly (a key or value times its power of two is a bf16 number; one of 2^128 and more is infinite); weights of the softmax carry 8 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
+ *   out        dev [rows, Hq*d], which must not overlap q; a row that sees no token (a position below 0, every page lost) gets
+ *              zeros, a head whose query is not finite not-a-numbers where it sees one.  Rows of no request are left as they are
+ * Tokens of a page outside the pool are left out; what a row does not see cannot change its output, not-a-numbers included.
+ * A request's result depends on `batch`, `rows`, max_pages and its own rows, not on the other requests.
+ * Cached numbers enter exactly (a key or value times its power of two is a bf16 number; one of 2^128 and more is infinite);
+ * weights of the softmax carry 8 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
  * Under SUN_VALIDATE row starts, counts and tables are copied to the host (synchronises) and checked.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, batch outside [1, 1024], rows < 1, max_pages outside [1, 2^26], window < 0, dtype, q or out not
- * 16-byte aligned, q the same as out, more rows than one launch takes: 2^23 are taken for up to 32 query heads), SUN_ERR_WORKSPACE (too small or not 256-byte aligned);
- * under SUN_VALIDATE also SUN_ERR_SEQ_LEN (row starts that fall or lie outside [0, rows], more rows than positions, counts) and SUN_ERR_PAGE_RANGE.
+ * 16-byte aligned, q the same as out, more rows than one launch takes: 2^23 are taken for up to 32 query heads),
+ * SUN_ERR_WORKSPACE (too small or not 256-byte aligned); under SUN_VALIDATE also SUN_ERR_SEQ_LEN (row starts that fall or lie outside [0, rows], more rows than positions, counts) and SUN_ERR_PAGE_RANGE.
  */
 int sun_kv8_chunk_attention(const sun_kv8_pool* pool, int layer, int batch, int rows, int dtype, const void* q, const int32_t* row_starts,
                             const int32_t* page_tables, int max_pages, const int32_t* n_tokens, int window, void* out, void* workspace,
@@ -639,8 +641,8 @@ int sun_mx4_linear(const void* codes, const void* scales, int N, int K, int rows
                    void* out, int out_dtype, int64_t ld_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * out[b, n] = act(sum_k W[n, k] x[b, k] + bias[n]) + residual[b, n]: sun_mx4_linear with what stands behind a projection in its epilogue, the product in its
- * arithmetic, the rest in 32 bits, rounded once.  Workspace: sun_mx4_linear_workspace_bytes.
+ * out[b, n] = act(sum_k W[n, k] x[b, k] + bias[n]) + residual[b, n]: sun_mx4_linear with what stands behind a projection in
+ * its epilogue, the product in its arithmetic, the rest in 32 bits, rounded once.  Workspace: sun_mx4_linear_workspace_bytes.
  *   bias        dev [N], of out's type, or NULL
  *   activation  SUN_ACT_*
  *   residual    dev [rows, N], of out's type, row stride ld_residual elements, or NULL; may be out itself at out's stride, and must not overlap
@@ -657,8 +659,8 @@ size_t sun_mx4_gated_workspace_bytes(int N, int K, int rows);
 
 /*
  * out[b, n] = act(sum_k Wg[n, k] x[b, k]) * (sum_k Wu[n, k] x[b, k]): the first half of a gated feed-forward block in one kernel, Wg and Wu [N, K] in the
- * format above, separate or the halves of one array.  Arithmetic, types, strides and refusals as in sun_mx4_linear (N at most 2^27, 2 N columns against its limits); the
- * activation and the product are in 32 bits, rounded once.
+ * format above, separate or the halves of one array.  Arithmetic, types, strides and refusals as in sun_mx4_linear (N at most
+ * 2^27, 2 N columns against its limits); the activation and the product are in 32 bits, rounded once.
  */
 int sun_mx4_gated(const void* gate_codes, const void* gate_scales, const void* up_codes, const void* up_scales, int N, int K, int rows,
                   const void* x, int x_dtype, int64_t ld_x, int activation, void* out, int out_dtype, int64_t ld_out, void* workspace,

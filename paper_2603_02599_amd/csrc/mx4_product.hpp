@@ -40,7 +40,7 @@ struct Mx4Args {
 
 // What happens to a sum before it is rounded and stored.  GATED: tiles of 16 columns are the gate's and the up projection's in turn, so that a lane has both sums of a
 // column; N counts pairs, and parts along k are stored gate first, [rows][2 N].  The kernels are bound by what bounds them without: a pair of 14336 x 4096 at 1 / 64 / 2048 rows in
-// bf16 takes 13.4 / 22 / 396 us (28672 x 4096 stored without one 13.1 / 22 / 394 to 423), of 13824 x 5120 at 150 in 32 bits 131, 5120 x 13824 at 333 with a residual 64.
+// bf16 takes 13.4 / 22 / 396 us (28672 x 4096 stored without one 13.1 / 22 / 394 to 423), of 13824 x 5120 at 150 in 32 bits 131, 5120 x 13824 at 333 with a residual 62.
 enum Epilogue { PLAIN, FUSED, GATED };
 
 // SiLU: x / (1 + e^-x).  GELU by tanh: x / (1 + e^(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3).  GELU: with C = erfc(|x| / sqrt 2), x - x C / 2 and, below 0, x C / 2; C by the
