@@ -592,6 +592,7 @@ size_t sun_kv8_chunk_attention_workspace_bytes(const sun_model_cfg* cfg, int bat
  *   out        dev [rows, Hq*d], which must not overlap q; a row that sees no token (a position below 0, every page lost) gets
  *              zeros, a head whose query is not finite not-a-numbers where it sees one.  Rows of no request are left as they are
  * Tokens of a page outside the pool are left out; what a row does not see cannot change its output, not-a-numbers included.
+ * A scale byte of 255, which sun_kv8_append never writes, makes not-a-numbers of a key, or of all of the token's values, for the rows that see it.
  * A request's result depends on `batch`, `rows`, max_pages and its own rows, not on the other requests.
  * Cached numbers enter exactly (a key or value times its power of two is a bf16 number; one of 2^128 and more is infinite);
  * weights of the softmax carry 8 bits for SUN_BF16 and 24 for SUN_F32, sums 32.

@@ -238,18 +238,21 @@ struct PageRequests {
     }
     // Notes of a page that has landed, requested `ago` pages ago, whose first token is `at`.  Powers and values from token n on, which nobody has written, become zeros; where some places see
     // a token and others do not (`partly`), values that are not numbers are noted and become zeros: their product with a weight of 0 would not be.
+    // A power of 255 is none: its token's values are all noted as no numbers, whoever sees them.
     __device__ __forceinline__ void note(uint8_t* block, int half, int ago, int at, int n, bool partly) const {
         const int lane = threadIdx.x & 63;
         Notes& notes = reinterpret_cast<Notes*>(block + Block<D>::N)[half];
         const uint8_t* s = block + Block<D>::S + half * 256;
-        if (lane < 32) notes.powers[lane] = at + (lane & 15) < n ? __uint_as_float((uint32_t)s[lane ^ 16] << 23) : 0.f;   // keys behind values
+        const uint32_t byte = lane < 32 && at + (lane & 15) < n ? s[lane ^ 16] : 0;   // keys behind values
+        const uint32_t lost = (uint32_t)__ballot(byte == 255) & 0xffffu;   // tokens whose values have no power
+        if (lane < 32) notes.powers[lane] = lost >> lane & 1 ? 0.f : __uint_as_float(byte << 23);
         bool any = false;
-        if (partly) {
+        if (partly || lost) {
 #pragma unroll 1
             for (int dim = lane; dim < D; dim += 64) {
                 u32x4_s* p = reinterpret_cast<u32x4_s*>(block + Block<D>::V + half * 16 * D + dim * 16);
                 u32x4_s x = *p;
-                uint32_t mask = 0;
+                uint32_t mask = lost;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int written = min(max(n - at - 4 * e, 0), 4);
