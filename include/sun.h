@@ -594,8 +594,8 @@ size_t sun_kv8_chunk_attention_workspace_bytes(const sun_model_cfg* cfg, int bat
  * Tokens of a page outside the pool are left out; what a row does not see cannot change its output, not-a-numbers included.
  * A scale byte of 255, which sun_kv8_append never writes, makes not-a-numbers of a key, or of all of the token's values, for the rows that see it.
  * A request's result depends on `batch`, `rows`, max_pages and its own rows, not on the other requests.
- * Cached numbers enter exactly (a key or value times its power of two is a bf16 number; one of 2^128 and more is infinite);
- * weights of the softmax carry 8 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
+ * Cached numbers enter exactly (scale bytes 27 to 247, which sun_kv8_append writes; a key of 2^128, to which the largest 32-bit numbers round, is infinite);
+ * weights of the softmax carry 16 bits for SUN_BF16 and 24 for SUN_F32, sums 32.
  * Under SUN_VALIDATE row starts, counts and tables are copied to the host (synchronises) and checked.
  * Errors: SUN_ERR_NULL, SUN_ERR_SHAPE (layer, batch outside [1, 1024], rows < 1, max_pages outside [1, 2^26], window < 0, dtype, q or out not
  * 16-byte aligned, q the same as out, more rows than one launch takes: 2^23 are taken for up to 32 query heads),

@@ -6,8 +6,10 @@
 //           scores are those of one page's tokens in their order, and
 //   output  O^T = V^T P^T: the same lane is P's operand for those tokens, V [dim][token] gives lane (dim, h) the page's sixteen in one read.
 // No value moves between lanes but for the maximum of the two halves h.  Codes become bf16 exactly, a key's power is applied while its codes are converted (a lane has one
-// token's), a value's power to its weight.  bf16 queries enter as they are, 32-bit ones as three planes of 8 bits, exact; a weight of the softmax is bf16(p) in bf16 calls, three planes
-// (24 bits) in 32-bit ones.  Maximum, sum and output are in 32 bits, the sum over the weights as they are multiplied.
+// token's), a value's power to its weight.  bf16 queries enter as they are, 32-bit ones as three planes of 8 bits, exact; a weight of the softmax is two planes
+// (16 bits, as in the attention of single tokens: bf16 of it and bf16 of what is left) in bf16 calls, three (24 bits) in 32-bit ones.  With one plane, which is 8 bits, weights that are alike all round the
+// same way, and an output is off by up to 2^-8 of itself beside its own rounding: 2048 of 8191 tokens took 272 us then, 360 with two.  Maximum, sum and output are in 32 bits, the sum over the weights before they
+// are rounded.
 // The reference that scores are taken against is raised to HEAD above the maximum when a score passes it, so that it is raised seldom and a weight is never above 1.
 //
 // What bounds it, 8B heads (32 and 8 of 128) in bf16: 2048 of 8191 tokens take 272 to 284 us, 0.85 to 0.88 PFLOP/s, and there the vector ALU (75 % busy; matrix cores 36 %), which
@@ -277,7 +279,7 @@ struct Places {
     static constexpr bool F32 = sizeof(T) == 4;
     // In powers of two: 0 / 6 / 10 take 2048 of 8191 tokens 297 / 285 / 280 us.  An exponential's argument, up to HEAD, rounds to 24 bits of itself, so 32-bit weights have less of it.
     static constexpr float HEAD = F32 ? 6.f : 10.f;
-    static constexpr int P = F32 ? 3 : 1, KS = D / 16, NB = D / 32;   // planes, steps of 16 dims, blocks of 32 dims
+    static constexpr int P = F32 ? 3 : 1, W = F32 ? 3 : 2, KS = D / 16, NB = D / 32;   // planes of a query and of a weight, steps of 16 dims, blocks of 32 dims
     bf16x8 q[P][KS];
     f32x16 o[NB];
     float m, l;        // the reference in powers of two, the lane's half of the sum
@@ -350,7 +352,7 @@ struct Places {
 
     // The output's products with a block's values: two of 32 dims.  Nothing but the matrix cores is short here, so they go first: the other wave of the SIMD has vector work to do
     // meanwhile (2048 of 8191 tokens 292 -> 284 us).
-    typedef u32x4_s Weights[P][2];
+    typedef u32x4_s Weights[W][2];
     __device__ __forceinline__ u32x4_s values(const uint8_t* block, int j) const {
         const int lane = threadIdx.x & 63;
         return *reinterpret_cast<const u32x4_s*>(block + Block<D>::V + (lane >> 5) * 16 * D + (32 * j + (lane & 31)) * 16);
@@ -358,7 +360,7 @@ struct Places {
     __device__ __forceinline__ void add(const u32x4_s& codes, const Weights& w, int j, int u) {
         const bf16x8 x = codes_to_bf16(codes[2 * u], codes[2 * u + 1]);
 #pragma unroll
-        for (int p = 0; p < P; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, w[p][u]), o[j], 0, 0, 0);
+        for (int p = 0; p < W; ++p) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, w[p][u]), o[j], 0, 0, 0);
     }
     __device__ __forceinline__ void add(const uint8_t* block, const Weights& w) {
         u32x4_s codes = values(block, 0);
@@ -432,11 +434,11 @@ struct Places {
             l += x[0] + x[1];
 #pragma unroll
             for (int e = 0; e < 2; ++e) x[e] *= vs[(2 * j + e) & 3];
-            words[0][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
-            if constexpr (F32) {
-                x[0] -= bf16_lo(words[0][j >> 2][j & 3]), x[1] -= bf16_hi(words[0][j >> 2][j & 3]);
-                words[1][j >> 2][j & 3] = pack_bf16(x[0], x[1]);
-                words[2][j >> 2][j & 3] = pack_bf16(x[0] - bf16_lo(words[1][j >> 2][j & 3]), x[1] - bf16_hi(words[1][j >> 2][j & 3]));
+#pragma unroll
+            for (int p = 0; p < W; ++p) {
+                const uint32_t word = pack_bf16(x[0], x[1]);
+                words[p][j >> 2][j & 3] = word;
+                x[0] -= bf16_lo(word), x[1] -= bf16_hi(word);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
