@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 ACTS = {"none": sun.SUN_ACT_NONE, "silu": sun.SUN_ACT_SILU, "gelu": sun.SUN_ACT_GELU, "gelu_tanh": sun.SUN_ACT_GELU_TANH}
-# a size for each kernel: up to 16 rows with 16, 32 and 64 columns a workgroup; up to 32, 64 and 128 rows; tiles; k split in each of the latter
+# up to 16 rows with 16, 32 and 64 columns a workgroup; up to 32, 64 and 128 rows with 64 columns; tiles of 128 x 128; k split in each of the latter (test_mx4_plans_cpu.py has a size for every kernel)
 SIZES = [(1, 32, 1), (17, 96, 5), (4500, 160, 7), (8200, 160, 3), (33, 160, 17), (129, 1376, 33), (257, 544, 65), (300, 4096, 20), (300, 4096, 60), (300, 4096, 100), (129, 2080, 130),
          (300, 4096, 200), (515, 352, 700), (1000, 4096, 333)]
 
