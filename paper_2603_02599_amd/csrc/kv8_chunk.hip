@@ -8,15 +8,18 @@
 // No value moves between lanes but for the maximum of the two halves h.  Codes become bf16 exactly, a key's power is applied while its codes are converted (a lane has one
 // token's), a value's power to its weight.  bf16 queries enter as they are, 32-bit ones as three planes of 8 bits, exact; a weight of the softmax is two planes
 // (16 bits, as in the attention of single tokens: bf16 of it and bf16 of what is left) in bf16 calls, three (24 bits) in 32-bit ones.  With one plane, which is 8 bits, weights that are alike all round the
-// same way, and an output is off by up to 2^-8 of itself beside its own rounding: 2048 of 8191 tokens took 272 us then, 360 with two.  Maximum, sum and output are in 32 bits, the sum over the weights before they
+// same way, and an output is off by up to 2^-8 of itself beside its own rounding: 2048 of 8191 tokens took 266 us so against 352 with two.  Maximum, sum and output are in 32 bits, the sum over the weights before they
 // are rounded.
 // The reference that scores are taken against is raised to HEAD above the maximum when a score passes it, so that it is raised seldom and a weight is never above 1.
 //
-// What bounds it, 8B heads (32 and 8 of 128) in bf16: 2048 of 8191 tokens take 272 to 284 us, 0.85 to 0.88 PFLOP/s, and there the vector ALU (75 % busy; matrix cores 36 %), which
-// converts a block's 64 codes a lane and takes sixteen exponentials, maxima, sums and roundings for each 16 products: a block measures 443 ns for the two waves of a SIMD, as the
-// instructions alone do.  The matrix instruction for 8-bit operands would need no conversion, but adds products to 2^-13 of their largest, which loses scores' last bits.
-// Four drafted tokens of 64 requests take 66 us, 333 MB at 5.0 TB/s, where reading alone takes 57.  32-bit calls multiply three times (14B heads, window 1000: 98 us, 67 of them the
-// planes' products at the rate of a large product).  Short prompts are bound by what stands in front of a tile's first product, a chain of five loads.
+// What bounds it, 8B heads (32 and 8 of 128) in bf16: 2048 of 8191 tokens take 350 to 370 us from card to card, 0.65 to 0.69 PFLOP/s, and there vector instructions and products one after another.
+// A wave converts a block's 128 codes a lane, half of them keys', and takes 16 exponentials, maxima, sums and roundings for its 24 products; a block of 32 tokens takes the two waves of a SIMD 3580 cycles,
+// in which matrix cores are busy for 43 % and vector instructions, products' issue among them, active for 72 %.  Alone, a conversion measures 4.3 cycles, an exponential 8, others 3 and a product 34, in all 3400 for both waves: next to
+// nothing runs beside anything, although two waves of independent products and multiply-adds do overlap (24 and 192 of each: 0.70 and 0.50 us alone, 0.85 together).  Products right behind their
+// conversions, a conversion ahead, by dims or by halves of the tokens, scores in front of the weights and no priorities all take the same to 3 %.
+// The matrix instruction for 8-bit operands would need no conversion, but adds products to 2^-13 of their largest, which loses scores' last bits.
+// Four drafted tokens of 64 requests take 70 us, 333 MB at 4.8 TB/s, where reading alone takes 57.  32-bit calls multiply three times (14B heads, window 1000: 98 to 101 us, 67 of them the
+// planes' products at the rate of a large product).  Short prompts are bound by what stands in front of a tile's first product, a chain of five loads, and by their longest tile.
 #include <float.h>
 #include <limits.h>
 #include <math.h>
@@ -26,15 +29,16 @@
 
 namespace sun {
 
-// A workgroup's share and what it takes.  128 places, 32 to each of four waves, with two workgroups on a compute unit (77 KB of LDS, up to 256 registers): one's vector work runs beside the
-// other's products.  Eight waves of 256 places, whose blocks are converted once for all of them in LDS, took 340 us for 2048 of 8191 tokens against 299, three workgroups a
-// compute unit need 168 registers, which is fewer than there are operands.
+// A workgroup's share and what it takes.  128 places, 32 to each of four waves, with two workgroups on a compute unit (77 KB of LDS, up to 256 registers): one computes while the
+// other waits.  Eight waves of 256 places, whose blocks are converted once for all of them in LDS, took 340 us for 2048 of 8191 tokens against 299 (with
+// weights of one plane), three workgroups a compute unit need 168 registers, which is fewer than there are operands.
 constexpr int kTile = 128;
 constexpr int kFew = 32;             // requests of so many places at most: the four waves share them and take tokens in turn
 constexpr int kWaves = 4;
-// Parts of long caches, for 512 workgroups (384 / 512 / 768 / 1024: 24 requests with prompts among them 96 / 78 / 78 / 81 us, four drafted tokens of 64 requests 67 / 67 / 83 / 83, 14B heads
-// in 32 bits 102 / 102 / 126 / 126, where each further part is written and joined and the workgroups do not come out even), of 512 tokens at least (256: 64 of 8191 tokens 33 us
-// against 31, 512 of 512 22 against 21; 128: 4 of 8191 20 against 16).
+// Parts of long caches, for 512 workgroups (384 / 512 / 768 / 1024: 24 requests with prompts among them 116 / 87 / 87 / 91 us, four drafted tokens of 64 requests 71 / 71 / 86 / 86, 14B heads
+// in 32 bits 101 / 101 / 125 / 125, where each further part is written and joined and the workgroups do not come out even), of 512 tokens at least (256: 64 of 8191 tokens 36 us
+// against 33, 512 of 512 23.6 against 23.4; 128: 4 of 8191 20 against 16).  All requests of a call may have as many, whatever their lengths, and with 512 groups of heads and tiles none has: measured
+// with lengths within a factor of eight of each other.  One long cache among many short ones is read by the workgroups of its own tiles and heads alone.
 constexpr int kMinSplit = 512;
 constexpr int kMaxSplits = 64;
 constexpr int kGroupsWanted = 512;
@@ -130,9 +134,9 @@ __device__ __forceinline__ ChunkPlace chunk_find(const ChunkArgs& a, long long i
 }
 
 // Tile `index` of all requests' in the order of their lengths in steps of 64 tokens, the longest first, where that gains: what starts last has to be short.  For up to kSorted requests,
-// one a lane, without parts, and few rounds of workgroups (the host decides); false where no request is long.  Against requests in turn: prompts of 583 to 1500 tokens 73 -> 66 us,
-// four drafted tokens of 64 requests 72 -> 68, 128 of 1000 to 2500 of sixteen 101 -> 88, but 32 prompts of 128 33 -> 42, whose workgroups then all wait and all compute at the
-// same time, and sixteen prompts of 200 to 1700 (eight rounds) 239 -> 243.  Finding a tile takes 2000 cycles, chunk_find 1300.  The whole wave calls it.
+// one a lane (a limit of the search, not of what gains), without parts, and few rounds of workgroups (the host decides); false where no request is long.  Against requests in turn: prompts of 583 to 1500 tokens 78 -> 76 us,
+// four drafted tokens of 64 requests 74 -> 71, 128 of 1000 to 2500 of sixteen 117 -> 103, but 32 prompts of 128 34 -> 43, whose workgroups then all wait and all compute at the
+// same time; sixteen prompts of 200 to 1700 (eight rounds) 284 and 280.  Finding a tile takes 2000 cycles, chunk_find 1300.  The whole wave calls it.
 constexpr int kSorted = 64, kSortedFrom = 512, kSortedGroups = 2560;
 __device__ __forceinline__ bool chunk_longest(const ChunkArgs& a, int index, ChunkPlace& p) {
     const ChunkRequest r = chunk_request(a, threadIdx.x & 63);
@@ -277,7 +281,7 @@ struct PageRequests {
 template <class T, int D>
 struct Places {
     static constexpr bool F32 = sizeof(T) == 4;
-    // In powers of two: 0 / 6 / 10 take 2048 of 8191 tokens 297 / 285 / 280 us.  An exponential's argument, up to HEAD, rounds to 24 bits of itself, so 32-bit weights have less of it.
+    // In powers of two: 0 / 6 / 10 take 2048 of 8191 tokens 384 / 372 / 368 us.  An exponential's argument, up to HEAD, rounds to 24 bits of itself, so 32-bit weights have less of it.
     static constexpr float HEAD = F32 ? 6.f : 10.f;
     static constexpr int P = F32 ? 3 : 1, W = F32 ? 3 : 2, KS = D / 16, NB = D / 32;   // planes of a query and of a weight, steps of 16 dims, blocks of 32 dims
     bf16x8 q[P][KS];
@@ -350,8 +354,7 @@ struct Places {
         return s;
     }
 
-    // The output's products with a block's values: two of 32 dims.  Nothing but the matrix cores is short here, so they go first: the other wave of the SIMD has vector work to do
-    // meanwhile (2048 of 8191 tokens 292 -> 284 us).
+    // The output's products with a block's values: two of 32 dims.  Nothing but the matrix cores is short here, so they go first (2048 of 8191 tokens 372 -> 368 us).
     typedef u32x4_s Weights[W][2];
     __device__ __forceinline__ u32x4_s values(const uint8_t* block, int j) const {
         const int lane = threadIdx.x & 63;
@@ -500,7 +503,7 @@ __device__ __forceinline__ void chunk_wide(const ChunkArgs& a, const ChunkPlace&
     constexpr int STAGE = 2 * Block<D>::BYTES, OPS = Block<D>::OPS;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, h = lane >> 5;
     const int G = a.G.d, live = p.r.count * G;
-    // Up to 64 places: two waves have the same ones, and one of a step's two blocks each (nine new tokens of 64 requests of 2000 80 -> 69 us, sixteen 82 -> 76)
+    // Up to 64 places: two waves have the same ones, and one of a step's two blocks each (nine new tokens of 64 requests of 2000 99 -> 82 us, sixteen 99 -> 84)
     const bool pairs = live - tile * kTile <= 64;
     const int v0 = tile * kTile + 32 * (pairs ? wave & 1 : wave);
     const ChunkRange range = chunk_range(a, p.r, tile * kTile, kTile, split, 64);
@@ -711,14 +714,14 @@ __device__ __forceinline__ void chunk_few(const ChunkArgs& a, const ChunkPlace& 
 template <class T, int D>
 __global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ChunkLds<D>::BYTES];
-    // No loop over items: what it keeps in scalar registers has others spilled (four drafted tokens of 64 requests 69 -> 66.5 us, 14B heads in 32 bits 103 -> 99)
+    // No loop over items: what it keeps in scalar registers has others spilled (with weights of one plane four drafted tokens of 64 requests 69 -> 66.5 us, 14B heads in 32 bits 103 -> 99)
     const int item = a.heads.quotient(blockIdx.x), head = blockIdx.x - item * a.Hkv;
     ChunkPlace p;
     const bool sorted = a.sorted && chunk_longest(a, item, p);
     if (!sorted) p = chunk_find<false>(a, item);
     if (p.b < 0) return;
     // The longest first.  Where all of a request's are on the chip at once, two workgroups a compute unit, the second half comes the other way round, so that a unit has a long and a
-    // short one (2048 of 8191 tokens 283 -> 274 us).
+    // short one (2048 of 8191 tokens 380 -> 368 us).
     const int turn = p.r.splits == 1 ? p.index : p.index / p.r.splits, split = p.index - turn * p.r.splits, half = (p.r.tiles + 1) / 2;
     const bool paired = p.r.tiles * p.r.splits * a.Hkv <= 512;
     const int tile = sorted ? p.index : paired && turn >= half ? turn - half : p.r.tiles - 1 - turn;
@@ -729,7 +732,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv8_chunk_kernel(ChunkArgs a) 
 }
 
 // out = sum over a tile's parts, four dims a lane; its places are dealt to gridDim.y workgroups.  Memory's latency is what bounds it: with eight parts on their way and eight places a
-// workgroup 4 of 8191 tokens (32 parts) take 32 -> 16 us with their attention, 8 of 32768 (64) 101 -> 30, against one part and four times the places.
+// workgroup 4 of 8191 tokens (32 parts) take 32 -> 16 us with their attention, 8 of 32768 (64) 101 -> 28, against one part and four times the places.
 template <class T, int D>
 __global__ __launch_bounds__(256) void kv8_chunk_join_kernel(ChunkArgs a) {
     const int G = a.G.d, item = a.heads.quotient(blockIdx.x), head = blockIdx.x - item * a.Hkv;
@@ -810,8 +813,8 @@ static hipError_t chunk_attend(const ChunkArgs& a, int64_t tiles, hipStream_t st
     const unsigned grid = (unsigned)(tiles * a.splits * a.Hkv);   // not 2^23: parts are for fewer than kGroupsWanted groups
     hipLaunchKernelGGL((kv8_chunk_kernel<T, D>), dim3(grid), dim3(64 * kWaves), 0, st, a);
     if (hipError_t e = hipGetLastError()) return e;
-    // Workgroups of a joined tile: a pass of eight places each where tiles are few (64 of 8191 tokens 40 -> 34 us against four of them), four where every further one would look for
-    // its tile again (1024 of 8191 tokens 165 us, with sixteen 170)
+    // Workgroups of a joined tile: a pass of eight places each where tiles are few (64 of 8191 tokens 36 -> 33 us against four of them), four where every further one would look for
+    // its tile again (1024 of 8191 tokens 211 us, with sixteen 216)
     const int64_t joining = std::min<int64_t>(a.slot_rows / 8, std::max<int64_t>(4, 1024 / (tiles * a.Hkv)));
     if (a.splits > 1) hipLaunchKernelGGL((kv8_chunk_join_kernel<T, D>), dim3((unsigned)(tiles * a.Hkv), (unsigned)joining), dim3(256), 0, st, a);
     return hipGetLastError();
